@@ -368,6 +368,119 @@ bns_status bns_set_option(const char* name, int32_t value);
  * -1 for an unknown name. */
 int32_t bns_get_option(const char* name);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * The last layers of a language model: the root-mean-square norm of the residual stream, the loss over the vocabulary
+ * without its logits, and the loss against a teacher's top logits.
+ *
+ * The conventions at the top hold (device pointers of at least 16-byte alignment, the caller's workspace, work enqueued on
+ * `stream`, one status, fp32 arithmetic, no floating-point atomics: results are bit-identical from run to run), with these additions.
+ * Matrices are row-major; the strides are in elements from row to row, 0 stands for dense rows, anything else is at least the row's length
+ * (rows may begin at any element).  A matrix of no rows is allowed: its pointers may be NULL and sums over it are zero.
+ * Kernels here never wait for other blocks, keep nothing in the workspace from call to call and can be captured into a graph.
+ * In place: an output may be the very tensor (address and stride) of an input where a function says so; any other overlap of an
+ * output matrix with an input matrix or another output matrix is BNS_EINVAL.  Vectors and the workspace are the caller's duty. */
+
+typedef enum { BNS_OUT_SAME = 0, BNS_OUT_E4M3 = 1 } bns_rms_out;
+
+/* Rows of `width` elements.  Limits: rows < 2^31, width <= 16384, strides < 2^31. */
+typedef struct {
+    int64_t rows;
+    int64_t x_stride;        /* x */
+    int64_t residual_stride; /* residual; backward: dsum */
+    int64_t sum_stride;      /* sum; backward: dx */
+    int64_t y_stride;        /* y; backward: dy */
+    int32_t width;
+    int32_t dtype;        /* bns_dtype of x, residual, sum, dx, dy, dsum and, with BNS_OUT_SAME, y */
+    int32_t weight_dtype; /* bns_dtype of weight */
+    int32_t out;          /* bns_rms_out: the type of y (forward only) */
+    int32_t group;        /* BNS_OUT_E4M3: 32, 64 or 128 neighbouring elements share a scale (the last group of a row may be
+                             shorter), 0: the whole row does; else 0 */
+    int32_t pow2_scales;  /* BNS_OUT_E4M3: 1: scales are rounded up to a power of two; else 0 */
+    float eps;            /* >= 0 */
+} bns_rms;
+
+/* Residual addition and root-mean-square norm of every row:
+ *   s = x + residual (s = x where residual is NULL)      rstd = 1 / sqrt(mean(s^2) + eps)      v = weight * s * rstd
+ * s is held in fp32 on its way to the norm; sum receives it rounded to dtype.
+ * y = v rounded to dtype, or in 8 bits (OCP e4m3: 4 exponent bits, 3 mantissa bits, largest value 448) with
+ *   scales[group] = max(max |v| / 448, 2^-126)           y = e4m3(v / scales[group]), round to nearest even
+ * so that v = y * scales up to that rounding.  scales is float[rows][ceil(width / group)], dense (float[rows] for group = 0).
+ * Elements that are NaN stay NaN in y; scales are those of the others.
+ * in: x, residual (may be NULL), weight[width].  out: sum (may be NULL; must be without residual), y, scales (BNS_OUT_E4M3, else NULL),
+ * rstd[rows] (may be NULL).  In place: sum on x or on residual; y on x (BNS_OUT_SAME, no sum on it). */
+bns_status bns_rms_forward(const bns_rms* rms, const void* x, const void* residual, const void* weight,
+                           void* sum, void* y, float* scales, float* rstd, void* stream);
+
+/* Bytes of workspace of bns_rms_backward; 0 for an invalid description. */
+size_t bns_rms_workspace_bytes(const bns_rms* rms);
+
+/* Gradients, with x the normalised rows (the forward call's sum, or its x where it had no residual), x^ = x * rstd:
+ *   dx = rstd * (weight * dy - x^ * mean(weight * dy * x^)) + dsum            dweight = sum over the rows of dy * x^
+ * dx is the gradient of x and of residual alike; dsum (may be NULL) is the gradient that reaches sum by its other uses.
+ * (With BNS_OUT_E4M3 this is the gradient of v: the rounding to 8 bits counts as the identity.)
+ * in: x, weight, rstd, dy, dsum.  out: dx, dweight[width].  In place: dx on dy or on dsum. */
+bns_status bns_rms_backward(const bns_rms* rms, const void* x, const void* weight, const float* rstd,
+                            const void* dy, const void* dsum, void* dx, float* dweight,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* `tokens` hidden states against a vocabulary.  Limits: tokens <= 2^20, width <= 65536, vocab < 2^24, strides < 2^31. */
+typedef struct {
+    int64_t tokens;
+    int64_t hidden_stride; /* hidden (the gradients are dense) */
+    int64_t weight_stride; /* weight */
+    int32_t width;
+    int32_t vocab;
+    int32_t dtype;         /* bns_dtype of hidden, weight, dhidden, dweight */
+    int32_t piece;         /* rows of weight that the workspace holds something for at a time; 0: the library's choice */
+} bns_head;
+
+/* Bytes of workspace of bns_head_forward and bns_head_backward (the larger of the two); 0 for an invalid description. */
+size_t bns_head_workspace_bytes(const bns_head* head);
+
+/* Softmax cross entropy of the logits z = hidden weight^T, which are never stored whole:
+ *   lse[t] = log sum over v of exp(z[t][v])              loss[t] = lse[t] - z[t][targets[t]]
+ * A token whose target lies outside [0, vocab) is left out: its loss is 0 (its lse is not).
+ * Products of bf16 are summed in fp32; f32 operands enter the matrix units as three bf16 parts each, the six products
+ * that reach an fp32 result's last bits.
+ * in: hidden[tokens][width], weight[vocab][width], targets[tokens].  out: loss[tokens], lse[tokens]. */
+bns_status bns_head_forward(const bns_head* head, const void* hidden, const void* weight, const int64_t* targets,
+                            float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sum over t of dloss[t] * loss[t], with the logits computed again piece by piece:
+ *   g[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - [v = targets[t]])      (0 for tokens that are left out, whatever they hold)
+ *   dhidden = g weight                                                   dweight = g^T hidden
+ * With bf16 operands g is rounded to bf16 before the two products, whose sums are fp32.
+ * in: hidden, weight, targets, lse (of the forward call), dloss[tokens].  out: dhidden, dweight (dense). */
+bns_status bns_head_backward(const bns_head* head, const void* hidden, const void* weight, const int64_t* targets,
+                             const float* lse, const float* dloss, void* dhidden, void* dweight,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of logits and, for each, `k` logits of a teacher.  Limits: tokens < 2^31, vocab < 2^30, 1 <= k <= 1024, strides < 2^31. */
+typedef struct {
+    int64_t tokens;
+    int64_t logits_stride;  /* logits */
+    int64_t dlogits_stride; /* dlogits */
+    int32_t vocab;
+    int32_t k;
+    int32_t dtype;          /* bns_dtype of logits, dlogits */
+    float temperature;      /* > 0 */
+} bns_distill;
+
+/* Distillation from a teacher's top logits.  With tau = temperature, over the row's entries j whose id lies in [0, vocab):
+ *   q = softmax(teacher / tau)        p = softmax(logits / tau) over the vocabulary        lse = log sum exp(logits / tau)
+ *   loss[t] = tau^2 * sum over j of q_j (log q_j - log p[id_j])
+ * A row without such an entry has loss 0 and gradient 0.  An id may occur more than once: its q add up in the gradient.
+ * dlogits = tau * dloss[t] * (p - q), in the same pass over the logits, where dlogits is given (then dloss is needed too).
+ * in: logits[tokens][vocab], ids[tokens][k], teacher[tokens][k] (dense), dloss[tokens] (NULL without dlogits).
+ * out: loss[tokens], lse[tokens], dlogits (may be NULL).  In place: dlogits on logits. */
+bns_status bns_distill_forward(const bns_distill* distill, const void* logits, const int64_t* ids, const float* teacher,
+                               const float* dloss, float* loss, float* lse, void* dlogits, void* stream);
+
+/* The gradient on its own, from the lse of the forward call.
+ * in: logits, ids, teacher, lse, dloss.  out: dlogits.  In place: dlogits on logits. */
+bns_status bns_distill_backward(const bns_distill* distill, const void* logits, const int64_t* ids, const float* teacher,
+                                const float* lse, const float* dloss, void* dlogits, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,6 +26,7 @@ BNS_OK, BNS_EINVAL, BNS_EUNSUPPORTED, BNS_EWORKSPACE, BNS_EDEVICE = range(5)
 BNS_FULL, BNS_NS, BNS_BS, BNS_FS, BNS_VDN = range(5)
 BNS_F32, BNS_BF16 = 0, 1
 BNS_NCHW, BNS_NHWC = 0, 1
+BNS_OUT_SAME, BNS_OUT_E4M3 = 0, 1
 
 
 class bns_shape(C.Structure):
@@ -43,6 +44,22 @@ class bns_box(C.Structure):
                 ("w0", C.c_int32), ("w_cnt", C.c_int32)]
 
 
+class bns_rms(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("x_stride", C.c_int64), ("residual_stride", C.c_int64), ("sum_stride", C.c_int64),
+                ("y_stride", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32), ("weight_dtype", C.c_int32), ("out", C.c_int32),
+                ("group", C.c_int32), ("pow2_scales", C.c_int32), ("eps", C.c_float)]
+
+
+class bns_head(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("hidden_stride", C.c_int64), ("weight_stride", C.c_int64), ("width", C.c_int32),
+                ("vocab", C.c_int32), ("dtype", C.c_int32), ("piece", C.c_int32)]
+
+
+class bns_distill(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("logits_stride", C.c_int64), ("dlogits_stride", C.c_int64), ("vocab", C.c_int32),
+                ("k", C.c_int32), ("dtype", C.c_int32), ("temperature", C.c_float)]
+
+
 class BnsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -53,6 +70,7 @@ class BnsError(RuntimeError):
 _lib = _call = None
 _P = C.c_void_p
 _SHP, _SPC = C.POINTER(bns_shape), C.POINTER(bns_spec)
+_RMS, _HEAD, _DISTILL = C.POINTER(bns_rms), C.POINTER(bns_head), C.POINTER(bns_distill)
 _PROTOS = {
     "bns_status_string": (C.c_char_p, [C.c_int]),
     "bns_sample_index": (C.c_int, [_SHP, _SPC, C.c_uint64, C.POINTER(bns_box)]),
@@ -78,6 +96,14 @@ _PROTOS = {
     "bns_copy_reference": (C.c_int, [_P, _P, C.c_size_t, _P]),
     "bns_set_option": (C.c_int, [C.c_char_p, C.c_int32]),
     "bns_get_option": (C.c_int32, [C.c_char_p]),
+    "bns_rms_forward": (C.c_int, [_RMS, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "bns_rms_workspace_bytes": (C.c_size_t, [_RMS]),
+    "bns_rms_backward": (C.c_int, [_RMS, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "bns_head_workspace_bytes": (C.c_size_t, [_HEAD]),
+    "bns_head_forward": (C.c_int, [_HEAD, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "bns_head_backward": (C.c_int, [_HEAD, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "bns_distill_forward": (C.c_int, [_DISTILL, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "bns_distill_backward": (C.c_int, [_DISTILL, _P, _P, _P, _P, _P, _P, _P]),
 }
 
 
@@ -342,6 +368,68 @@ def bns_set_option(name: str, value: int):
 
 def bns_get_option(name: str) -> int:
     return int(load().bns_get_option(name.encode()))
+
+
+# --------------------------------------------------------------------------------------
+# the last layers of a language model
+# --------------------------------------------------------------------------------------
+_DTYPES = {"f32": BNS_F32, "bf16": BNS_BF16}
+
+
+def _dtype(d):
+    return _DTYPES[d] if isinstance(d, str) else d
+
+
+def make_rms(rows, width, dtype="bf16", *, weight_dtype="f32", out="same", group=0, pow2_scales=False, eps=1e-6, x_stride=0, residual_stride=0,
+             sum_stride=0, y_stride=0) -> bns_rms:
+    return bns_rms(rows, x_stride, residual_stride, sum_stride, y_stride, width, _dtype(dtype), _dtype(weight_dtype),
+                   {"same": BNS_OUT_SAME, "e4m3": BNS_OUT_E4M3}[out] if isinstance(out, str) else out, group, int(pow2_scales), eps)
+
+
+def make_head(tokens, width, vocab, dtype="bf16", *, piece=0, hidden_stride=0, weight_stride=0) -> bns_head:
+    return bns_head(tokens, hidden_stride, weight_stride, width, vocab, _dtype(dtype), piece)
+
+
+def make_distill(tokens, vocab, k, dtype="bf16", *, temperature=1.0, logits_stride=0, dlogits_stride=0) -> bns_distill:
+    return bns_distill(tokens, logits_stride, dlogits_stride, vocab, k, _dtype(dtype), temperature)
+
+
+def bns_rms_forward(rms, x, residual, weight, sum, y, scales, rstd):
+    _check(load().bns_rms_forward(C.byref(rms), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum), _ptr(y), _ptr(scales), _ptr(rstd), _stream(x)),
+           "bns_rms_forward")
+
+
+def bns_rms_workspace_bytes(rms) -> int:
+    return int(load().bns_rms_workspace_bytes(C.byref(rms)))
+
+
+def bns_rms_backward(rms, x, weight, rstd, dy, dsum, dx, dweight, workspace):
+    _check(load().bns_rms_backward(C.byref(rms), _ptr(x), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dsum), _ptr(dx), _ptr(dweight), _ptr(workspace),
+                                   workspace.nbytes, _stream(x)), "bns_rms_backward")
+
+
+def bns_head_workspace_bytes(head) -> int:
+    return int(load().bns_head_workspace_bytes(C.byref(head)))
+
+
+def bns_head_forward(head, hidden, weight, targets, loss, lse, workspace):
+    _check(load().bns_head_forward(C.byref(head), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(workspace),
+                                   workspace.nbytes, _stream(hidden)), "bns_head_forward")
+
+
+def bns_head_backward(head, hidden, weight, targets, lse, dloss, dhidden, dweight, workspace):
+    _check(load().bns_head_backward(C.byref(head), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(lse), _ptr(dloss), _ptr(dhidden), _ptr(dweight),
+                                    _ptr(workspace), workspace.nbytes, _stream(hidden)), "bns_head_backward")
+
+
+def bns_distill_forward(distill, logits, ids, teacher, dloss, loss, lse, dlogits):
+    _check(load().bns_distill_forward(C.byref(distill), _ptr(logits), _ptr(ids), _ptr(teacher), _ptr(dloss), _ptr(loss), _ptr(lse), _ptr(dlogits),
+                                      _stream(logits)), "bns_distill_forward")
+
+
+def bns_distill_backward(distill, logits, ids, teacher, lse, dloss, dlogits):
+    _check(load().bns_distill_backward(C.byref(distill), _ptr(logits), _ptr(ids), _ptr(teacher), _ptr(lse), _ptr(dloss), _ptr(dlogits),
+                                       _stream(logits)), "bns_distill_backward")
 
 
 # --------------------------------------------------------------------------------------

@@ -1,0 +1,397 @@
+// Distillation from a teacher's top logits: the loss with the logits' gradient from the same pass, and the gradient on its own.  See
+// include/bns.h for the equations.
+//
+// Both read every logit once and write every gradient once, so HBM bounds them.  Forward: a block takes a row and keeps it in registers
+// as it is stored (256 KB of the 512 KB of a compute unit), so that maximum, sum and gradient come from one read; longer rows are read
+// again, which the memory-side cache serves.  Wave 0 works the teacher's distribution out while the row is on its way.  The gradient is
+// written as if the teacher were not there, then the few elements that it touches once more.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "bns_internal.hpp"
+#include "bns_lm_device.hpp"
+#include "bns_lm_validate.hpp"
+
+using namespace bns;
+
+namespace {
+
+constexpr int kMostEntries = 1024;
+constexpr float kLeast = -3e38f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+struct DistillArgs {
+    const void* logits;
+    const int64_t* ids;
+    const float *teacher, *dloss;
+    const float* lse_in;        // backward
+    float *loss, *lse;          // forward
+    void* dlogits;
+    int64_t tokens, logits_stride, dlogits_stride;
+    int32_t vocab, k;
+    int32_t segment;            // backward: elements per block, a multiple of 8
+    float tau;
+};
+
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes of a row as they are stored; elements behind its end are -infinity.
+template <typename T>
+struct Words;
+template <>
+struct Words<float> {
+    static constexpr int kElems = 4;
+    typedef u4 u4e __attribute__((aligned(4)));
+    static __device__ __forceinline__ u4 load(const float* p, int left) {
+        if (left >= 4) return *reinterpret_cast<const u4e*>(p);
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+        const uint32_t none = 0xff800000u;
+        return u4{left > 0 ? w[0] : none, left > 1 ? w[1] : none, left > 2 ? w[2] : none, none};
+    }
+    static __device__ __forceinline__ void unpack(u4 w, float (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(w[i]);
+    }
+    static __device__ __forceinline__ void store(float* p, int left, const float (&f)[4]) {
+        if (left >= 4) {
+            *reinterpret_cast<u4e*>(p) = u4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) p[i] = f[i];
+        }
+    }
+    static __device__ __forceinline__ void put(float* p, float f) { *p = f; }
+};
+template <>
+struct Words<bf16_t> {
+    static constexpr int kElems = 8;
+    typedef u4 u4e __attribute__((aligned(2)));
+    static __device__ __forceinline__ u4 load(const bf16_t* p, int left) {
+        if (left >= 8) return *reinterpret_cast<const u4e*>(p);
+        u4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = 2 * i < left ? p[2 * i].bits : 0xff80u, hi = 2 * i + 1 < left ? p[2 * i + 1].bits : 0xff80u;
+            w[i] = lo | hi << 16;
+        }
+        return w;
+    }
+    static __device__ __forceinline__ void unpack(u4 w, float (&f)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ void store(bf16_t* p, int left, const float (&f)[8]) { Row8<bf16_t>::store(p, left, f); }
+    static __device__ __forceinline__ void put(bf16_t* p, float f) { p->bits = uint16_t(f32_to_bf16(f)); }
+};
+
+// The teacher's part of a row, worked out by one wave.
+struct Teacher {
+    int32_t id[kMostEntries];   // -1: no entry
+    float q[kMostEntries];
+    float z[kMostEntries];      // the student's logit there (only of ids in [v0, v1))
+    float cross;                // sum q (log q - z / tau)
+    int32_t some;               // whether the row has an entry
+};
+
+template <typename T>
+__device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, int64_t row, const T* logits, int v0, int v1, bool cross) {
+    const int lane = threadIdx.x;
+    const int64_t* ids = a.ids + row * a.k;
+    const float* u = a.teacher + row * a.k;
+    const float c = kLog2e / a.tau;
+    float most = -__builtin_inff();
+    bool some = false;
+    for (int j = lane; j < a.k; j += kWave) {
+        const int64_t id = ids[j];
+        const float v = u[j];
+        const bool valid = id >= 0 && id < a.vocab && !(v == -__builtin_inff());
+        s.id[j] = valid ? int32_t(id) : -1;
+        s.q[j] = v;
+        if (valid) {
+            if (id >= v0 && id < v1) s.z[j] = load_scalar<T>(logits + id);
+            some = true;
+            most = fmaxf(most, v);
+        }
+    }
+    most = fmaxf(wave_max(most), -3e38f);
+    float sum = 0.f;
+    for (int j = lane; j < a.k; j += kWave)
+        if (s.id[j] >= 0) sum += __builtin_amdgcn_exp2f((s.q[j] - most) * c);
+    const float total = wave_sum(sum), inv = 1.f / total, log2_total = __builtin_amdgcn_logf(total);
+    float x = 0.f;
+    for (int j = lane; j < a.k; j += kWave) {
+        if (s.id[j] < 0) {
+            s.q[j] = 0.f;
+            continue;
+        }
+        const float e = (s.q[j] - most) * c, q = __builtin_amdgcn_exp2f(e) * inv;
+        s.q[j] = q;
+        if (cross && !(q == 0.f)) x += q * ((e - log2_total) * kLn2 - s.z[j] / a.tau);
+    }
+    x = cross ? wave_sum(x) : 0.f;
+    const bool any = __any(some);
+    if (lane == 0) {
+        s.cross = x;
+        s.some = any;
+    }
+}
+
+// The gradient where the teacher has entries: what all entries of one id add up to is taken off the student's probability.
+template <typename T>
+__device__ __forceinline__ void fix_entries(const Teacher& s, const DistillArgs& a, T* dlogits, int v0, int v1, float lse2, float scale) {
+    const float c = kLog2e / a.tau;
+    for (int j = threadIdx.x; j < a.k; j += blockDim.x) {
+        const int id = s.id[j];
+        if (id < v0 || id >= v1) continue;
+        float q = 0.f;
+        for (int i = 0; i < a.k; ++i) q += s.id[i] == id ? s.q[i] : 0.f;
+        Words<T>::put(dlogits + id, scale * (__builtin_amdgcn_exp2f(fmaf(s.z[j], c, -lse2)) - q));
+    }
+}
+
+// Keeps the compiler from carrying the words' values, twice their size in bf16, from one use of the row to the next.
+template <int N>
+__device__ __forceinline__ void keep_packed(u4 (&w)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
+}
+
+// NV: 16-byte words per thread that hold the row; 0: the row is read again.
+template <typename T, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a) {
+    constexpr int E = Words<T>::kElems, kWaves = THREADS / kWave;
+    __shared__ Teacher teacher;
+    __shared__ float part[2][kWaves];
+    const int tid = threadIdx.x, wave = tid / kWave;
+    const float c = kLog2e / a.tau;
+    for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
+        const T* z = static_cast<const T*>(a.logits) + row * a.logits_stride;
+        u4 held[NV > 0 ? NV : 1];
+        // The row's last word is moved back so that it ends with the row, and so are those behind it: all are on their way before any is
+        // looked at.  What they hold twice does not change a maximum, is left out of the sum and written twice with the same bits.
+        int t = tid;        // (opaque, here and before each use: nothing that follows from it is kept in registers from row to row)
+        asm volatile("" : "+v"(t));
+        if (NV > 0) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int v = (j * THREADS + t) * E;
+                held[j] = Words<T>::load(z + min(v, a.vocab - E), E);
+            }
+        }
+        if (wave == 0) work_teacher(teacher, a, row, z, 0, a.vocab, true);
+        // maximum of z / tau in powers of two, and sum of exp2 of what lies below it; a wave that meets only -infinity has a finite maximum
+        float m = -__builtin_inff(), l = 0.f;
+        if (NV > 0) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float f[E];
+                Words<T>::unpack(held[j], f);
+#pragma unroll
+                for (int i = 0; i < E; ++i) m = fmaxf(m, f[i]);
+                __builtin_amdgcn_sched_barrier(0);      // (registers: one word's values at a time)
+            }
+            m = fmaxf(wave_max(m) * c, kLeast);
+            keep_packed(held);
+            asm volatile("" : "+v"(t));
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float f[E];
+                Words<T>::unpack(held[j], f);
+#pragma unroll
+                for (int i = 0; i < E; ++i) f[i] = __builtin_amdgcn_exp2f(fmaf(f[i], c, -m));
+                if ((j + 1) * THREADS * E > a.vocab) {
+                    const int twice = (j * THREADS + t + 1) * E - a.vocab;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) f[i] = i < twice ? 0.f : f[i];
+                }
+#pragma unroll
+                for (int i = 0; i < E; ++i) l += f[i];
+                asm volatile("" : "+v"(l));             // (added here and now, for the same reason)
+            }
+        } else {
+            m = kLeast;
+            for (int v = tid * E; v < a.vocab; v += THREADS * E) {
+                float f[E], most = -__builtin_inff();
+                Words<T>::unpack(Words<T>::load(z + v, a.vocab - v), f);
+#pragma unroll
+                for (int i = 0; i < E; ++i) most = fmaxf(most, f[i]);
+                most = fmaxf(m, most * c);
+                l *= __builtin_amdgcn_exp2f(m - most);
+                m = most;
+#pragma unroll
+                for (int i = 0; i < E; ++i) l += __builtin_amdgcn_exp2f(fmaf(f[i], c, -m));
+            }
+            const float most = wave_max(m);
+            l *= __builtin_amdgcn_exp2f(m - most);
+            m = most;
+        }
+        l = wave_sum(l);
+        if (tid % kWave == 0) {
+            part[0][wave] = m;
+            part[1][wave] = l;
+        }
+        __syncthreads();
+        m = part[0][0];
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) m = fmaxf(m, part[0][i]);
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) l = fmaf(part[1][i], __builtin_amdgcn_exp2f(part[0][i] - m), l);
+        const float lse2 = m + __builtin_amdgcn_logf(l), lse = lse2 * kLn2;
+        const bool some = teacher.some;
+        if (tid == 0) {
+            a.lse[row] = lse;
+            a.loss[row] = some ? a.tau * a.tau * (teacher.cross + lse) : 0.f;
+        }
+        if (a.dlogits) {
+            T* out = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
+            const float scale = some ? a.tau * a.dloss[row] : 0.f;
+            const auto write = [&](int v, u4 w, int left) {
+                float f[E];
+                Words<T>::unpack(w, f);
+#pragma unroll
+                for (int i = 0; i < E; ++i) f[i] = some ? scale * __builtin_amdgcn_exp2f(fmaf(f[i], c, -lse2)) : 0.f;
+                Words<T>::store(out + v, left, f);
+            };
+            if (NV > 0) {
+                keep_packed(held);
+                asm volatile("" : "+v"(t));
+#pragma unroll
+                for (int j = 0; j < NV; ++j) {
+                    const int v = (j * THREADS + t) * E;
+                    if (v < a.vocab) write(min(v, a.vocab - E), held[j], E);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                for (int v = tid * E; v < a.vocab; v += THREADS * E) write(v, Words<T>::load(z + v, a.vocab - v), a.vocab - v);
+            }
+            __syncthreads();
+            if (some) fix_entries(teacher, a, out, 0, a.vocab, lse2, scale);
+        }
+        __syncthreads();        // (the teacher's part is free again)
+    }
+}
+
+// One segment of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, int segments) {
+    constexpr int E = Words<T>::kElems, kAtOnce = 4;
+    __shared__ Teacher teacher;
+    const float c = kLog2e / a.tau;
+    for (int64_t b = blockIdx.x; b < a.tokens * segments; b += gridDim.x) {
+        const int64_t row = b / segments;
+        const int v0 = int(b % segments) * a.segment, v1 = min(v0 + a.segment, a.vocab);
+        const T* z = static_cast<const T*>(a.logits) + row * a.logits_stride;
+        T* out = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
+        if (threadIdx.x < kWave) work_teacher(teacher, a, row, z, v0, v1, false);
+        const float lse2 = a.lse_in[row] * kLog2e;
+        __syncthreads();
+        const bool some = teacher.some;
+        const float scale = some ? a.tau * a.dloss[row] : 0.f;
+        for (int v = v0 + int(threadIdx.x) * E; v < v1; v += 256 * E * kAtOnce) {
+            u4 w[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) w[j] = Words<T>::load(z + v + j * 256 * E, v1 - v - j * 256 * E);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                float f[E];
+                Words<T>::unpack(w[j], f);
+#pragma unroll
+                for (int i = 0; i < E; ++i) f[i] = some ? scale * __builtin_amdgcn_exp2f(fmaf(f[i], c, -lse2)) : 0.f;
+                if (v + j * 256 * E < v1) Words<T>::store(out + v + j * 256 * E, v1 - v - j * 256 * E, f);
+            }
+        }
+        __syncthreads();
+        if (some) fix_entries(teacher, a, out, v0, v1, lse2, scale);
+        __syncthreads();
+    }
+}
+
+constexpr int64_t kMostBlocks = int64_t(1) << 20;
+
+template <typename T>
+void launch_forward(const DistillArgs& a, hipStream_t st) {
+    const int64_t words = (a.vocab + Words<T>::kElems - 1) / Words<T>::kElems;
+    const dim3 grid(uint32_t(std::min(a.tokens, kMostBlocks)));
+#define BNS_DISTILL(THREADS, NV)                                                                          \
+    if (words <= int64_t(THREADS) * NV) {                                                                 \
+        BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV>), grid, dim3(THREADS), 0, st, a);              \
+        return;                                                                                           \
+    }
+    if (a.vocab >= Words<T>::kElems) {
+    BNS_DISTILL(256, 2)
+    BNS_DISTILL(256, 4)
+    BNS_DISTILL(512, 4)
+    BNS_DISTILL(1024, 4)
+    BNS_DISTILL(1024, 8)
+    BNS_DISTILL(1024, 12)
+    BNS_DISTILL(1024, 16)
+    }
+#undef BNS_DISTILL
+    BNS_LAUNCH((distill_forward_kernel<T, 1024, 0>), grid, dim3(1024), 0, st, a);
+}
+
+template <typename T>
+void launch_backward(DistillArgs a, hipStream_t st) {
+    // Segments of a whole row where the rows alone fill the device, else shorter ones; a block takes 256 x 4 words at a time.
+    const int64_t least = 256 * 4 * Words<T>::kElems, want = std::max<int64_t>(1, 2048 / std::max<int64_t>(a.tokens, 1));
+    const int64_t segments = std::max<int64_t>(1, std::min<int64_t>(want, (a.vocab + least - 1) / least));
+    a.segment = int32_t(round_up((a.vocab + segments - 1) / segments, 8));
+    const int count = int((a.vocab + a.segment - 1) / a.segment);
+    BNS_LAUNCH((distill_backward_kernel<T>), dim3(uint32_t(std::min(a.tokens * count, kMostBlocks))), dim3(256), 0, st, a, count);
+}
+
+bns_status check_tensors(const bns_distill* distill, const DistillDims& d, const void* logits, const void* ids, const void* teacher, const void* dlogits) {
+    if (!logits || !ids || !teacher) return BNS_EINVAL;
+    for (const void* p : {logits, ids, teacher, dlogits})
+        if (!aligned16(p)) return BNS_EINVAL;
+    const size_t e = dtype_bytes(distill->dtype), row = size_t(d.vocab) * e;
+    const Matrix out = matrix(dlogits, d.tokens, d.vocab, d.dlogits_stride, e), in = matrix(logits, d.tokens, d.vocab, d.logits_stride, e);
+    if (collide(out, in, true, row, row) || collide(out, matrix(ids, d.tokens, d.k, d.k, 8), false, row, size_t(d.k) * 8) ||
+        collide(out, matrix(teacher, d.tokens, d.k, d.k, 4), false, row, size_t(d.k) * 4))
+        return BNS_EINVAL;
+    return BNS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+bns_status bns_distill_forward(const bns_distill* distill, const void* logits, const int64_t* ids, const float* teacher, const float* dloss,
+                               float* loss, float* lse, void* dlogits, void* stream) {
+    DistillDims d;
+    bns_status s = check_distill(distill, &d);
+    if (s != BNS_OK) return s;
+    if (d.tokens == 0) return BNS_OK;
+    if (!loss || !lse || (dlogits && !dloss)) return BNS_EINVAL;
+    if ((s = check_tensors(distill, d, logits, ids, teacher, dlogits)) != BNS_OK) return s;
+    const DistillArgs a = {logits, ids, teacher, dloss, nullptr, loss, lse, dlogits, d.tokens, d.logits_stride, d.dlogits_stride,
+                           d.vocab, d.k, 0, distill->temperature};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (distill->dtype == BNS_F32) launch_forward<float>(a, st);
+    else launch_forward<bf16_t>(a, st);
+    return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
+}
+
+bns_status bns_distill_backward(const bns_distill* distill, const void* logits, const int64_t* ids, const float* teacher, const float* lse,
+                                const float* dloss, void* dlogits, void* stream) {
+    DistillDims d;
+    bns_status s = check_distill(distill, &d);
+    if (s != BNS_OK) return s;
+    if (d.tokens == 0) return BNS_OK;
+    if (!lse || !dloss || !dlogits) return BNS_EINVAL;
+    if ((s = check_tensors(distill, d, logits, ids, teacher, dlogits)) != BNS_OK) return s;
+    const DistillArgs a = {logits, ids, teacher, dloss, lse, nullptr, nullptr, dlogits, d.tokens, d.logits_stride, d.dlogits_stride,
+                           d.vocab, d.k, 0, distill->temperature};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (distill->dtype == BNS_F32) launch_backward<float>(a, st);
+    else launch_backward<bf16_t>(a, st);
+    return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
+}
+
+}  // extern "C"

@@ -1,0 +1,394 @@
+// Root-mean-square norm of the residual stream: forward with the residual's addition and an output in 8 bits, and backward.
+// See include/bns.h for the equations.
+//
+// Both passes read every element once and write once, so HBM bounds them; a row stays in registers between its sum of squares and its
+// output.  A row belongs to TPR threads (a wave, 256, 512 or 1024), each of which holds VPT vectors of eight neighbouring elements.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "bns_internal.hpp"
+#include "bns_lm_device.hpp"
+#include "bns_lm_validate.hpp"
+
+using namespace bns;
+
+namespace {
+
+struct RmsArgs {
+    const void *x, *residual, *weight;
+    void *sum, *y;
+    float *scales, *rstd;
+    int64_t rows, x_stride, residual_stride, sum_stride, y_stride;
+    int32_t width, groups, group;
+    int32_t weight_bf16, e4m3, pow2;
+    float eps, inv_width;
+};
+
+struct RmsBackwardArgs {
+    const void *x, *weight, *dy, *dsum;
+    const float* rstd;
+    void* dx;
+    float* partial;     // [row groups][width]
+    int64_t rows, x_stride, dsum_stride, dx_stride, dy_stride;
+    int32_t width, weight_bf16;
+    float inv_width;
+};
+
+__device__ __forceinline__ void load_weight(const void* w, int bf16, int col, int left, float (&f)[8]) {
+    if (bf16) Row8<bf16_t>::load(static_cast<const bf16_t*>(w) + col, left, f);
+    else Row8<float>::load(static_cast<const float*>(w) + col, left, f);
+}
+
+// Sum / maximum over the TPR threads of a row; `lds` holds a float for every wave.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* lds) {
+    v = wave_sum(v);
+    if (TPR == kWave) return v;
+    __syncthreads();                    // (the values of the last use have been read)
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < TPR / kWave; ++i) s += lds[i];
+    return s;
+}
+template <int TPR>
+__device__ __forceinline__ float row_max(float v, float* lds) {
+    v = wave_max(v);
+    if (TPR == kWave) return v;
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    float s = lds[0];
+#pragma unroll
+    for (int i = 1; i < TPR / kWave; ++i) s = fmaxf(s, lds[i]);
+    return s;
+}
+
+// The scale of values whose largest magnitude is `most`: see include/bns.h.
+__device__ __forceinline__ float e4m3_scale(float most, int pow2) {
+    const float s = fmaxf(most * (1.f / 448.f), 0x1p-126f);
+    if (!pow2) return s;
+    const uint32_t bits = __float_as_uint(s);
+    return __uint_as_float((bits + 0x7fffffu) & 0x7f800000u);
+}
+
+template <int TPR>
+constexpr int block_of() { return TPR == kWave ? 256 : TPR; }
+
+template <typename T, int TPR, int VPT>
+__global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a) {
+    constexpr int kRows = block_of<TPR>() / TPR;
+    __shared__ float lds[block_of<TPR>() / kWave];
+    const int t = threadIdx.x % TPR;
+    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR; row < a.rows; row += int64_t(gridDim.x) * kRows) {
+        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+        float s[VPT][8];
+        float square = 0.f;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8, left = a.width - col;
+            if (left > 0) {
+                Row8<T>::load(x + col, left, s[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[j][i] = 0.f;
+            }
+        }
+        if (a.residual) {
+            const T* r = static_cast<const T*>(a.residual) + row * a.residual_stride;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const int col = (j * TPR + t) * 8, left = a.width - col;
+                if (left > 0) {
+                    float f[8];
+                    Row8<T>::load(r + col, left, f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[j][i] += f[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < VPT; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) square = fmaf(s[j][i], s[j][i], square);
+        const float rstd = __frsqrt_rn(fmaf(row_sum<TPR>(square, lds), a.inv_width, a.eps));
+        if (a.rstd && t == 0) a.rstd[row] = rstd;
+        if (a.sum) {
+            T* out = static_cast<T*>(a.sum) + row * a.sum_stride;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const int col = (j * TPR + t) * 8, left = a.width - col;
+                if (left > 0) Row8<T>::store(out + col, left, s[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8, left = a.width - col;
+            if (left > 0) {
+                float w[8];
+                load_weight(a.weight, a.weight_bf16, col, left, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[j][i] = s[j][i] * rstd * w[i];
+            }
+        }
+        if (!a.e4m3) {
+            T* y = static_cast<T*>(a.y) + row * a.y_stride;
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const int col = (j * TPR + t) * 8, left = a.width - col;
+                if (left > 0) Row8<T>::store(y + col, left, s[j]);
+            }
+            continue;
+        }
+        float most[VPT], whole = 0.f;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            most[j] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most[j] = fmaxf(most[j], fabsf(s[j][i]));
+            whole = fmaxf(whole, most[j]);
+        }
+        if (a.group == 0) {
+            whole = row_max<TPR>(whole, lds);
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) most[j] = whole;
+        } else {
+            // the vectors of a group lie in 4, 8 or 16 neighbouring lanes
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                most[j] = fmaxf(most[j], __shfl_xor(most[j], 1));
+                most[j] = fmaxf(most[j], __shfl_xor(most[j], 2));
+                if (a.group > 32) most[j] = fmaxf(most[j], __shfl_xor(most[j], 4));
+                if (a.group > 64) most[j] = fmaxf(most[j], __shfl_xor(most[j], 8));
+            }
+        }
+        uint8_t* y = static_cast<uint8_t*>(a.y) + row * a.y_stride;
+        float* scales = a.scales + row * a.groups;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8, left = a.width - col;
+            if (left <= 0) continue;
+            const float scale = e4m3_scale(most[j], a.pow2), inv = 1.f / scale;
+            if (a.group == 0 ? col == 0 : col % a.group == 0) scales[a.group == 0 ? 0 : col / a.group] = scale;
+            uint32_t q[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                int v = __builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * h] * inv, s[j][4 * h + 1] * inv, 0, false);
+                q[h] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * h + 2] * inv, s[j][4 * h + 3] * inv, v, true));
+            }
+            if (left >= 8) {
+                typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+                typedef u2 u2e __attribute__((aligned(1)));
+                *reinterpret_cast<u2e*>(y + col) = u2{q[0], q[1]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < left) y[col + i] = uint8_t(q[i / 4] >> (8 * (i % 4)));
+            }
+        }
+    }
+}
+
+// dx of every row, and dweight as one partial sum for each of the gridDim.x * kRows row groups: a thread meets the same columns in every row,
+// so their sums stay in its registers.
+template <typename T, int TPR, int VPT>
+__global__ void __launch_bounds__(block_of<TPR>()) rms_backward_kernel(RmsBackwardArgs a) {
+    constexpr int kRows = block_of<TPR>() / TPR;
+    __shared__ float lds[block_of<TPR>() / kWave];
+    const int t = threadIdx.x % TPR;
+    const int64_t first = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR, step = int64_t(gridDim.x) * kRows;
+    float dw[VPT][8];
+#pragma unroll
+    for (int j = 0; j < VPT; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[j][i] = 0.f;
+    for (int64_t row = first; row < a.rows; row += step) {
+        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+        const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
+        const float rstd = a.rstd[row];
+        float xh[VPT][8], g[VPT][8];
+        float dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8, left = a.width - col;
+            if (left > 0) {
+                Row8<T>::load(x + col, left, xh[j]);
+                Row8<T>::load(dy + col, left, g[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) xh[j][i] = g[j][i] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8, left = a.width - col;
+            if (left > 0) {
+                float w[8];
+                load_weight(a.weight, a.weight_bf16, col, left, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    xh[j][i] *= rstd;
+                    dw[j][i] = fmaf(g[j][i], xh[j][i], dw[j][i]);
+                    g[j][i] *= w[i];
+                    dot = fmaf(g[j][i], xh[j][i], dot);
+                }
+            }
+        }
+        const float mean = row_sum<TPR>(dot, lds) * a.inv_width;
+        T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
+        const T* dsum = a.dsum ? static_cast<const T*>(a.dsum) + row * a.dsum_stride : nullptr;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8, left = a.width - col;
+            if (left <= 0) continue;
+            float f[8];
+            if (dsum) {
+                Row8<T>::load(dsum + col, left, f);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = fmaf(rstd, fmaf(-xh[j][i], mean, g[j][i]), f[i]);
+            Row8<T>::store(dx + col, left, f);
+        }
+    }
+    if (first < step) {     // every row group has a place, whether it met a row or not
+        float* out = a.partial + first * a.width;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8, left = a.width - col;
+            if (left > 0) Row8<float>::store(out + col, left, dw[j]);
+        }
+    }
+}
+
+// Adds the partial sums of a column in a fixed order: 16 threads take every 16th of them, then one adds the 16.
+constexpr int kSumColumns = 64, kSumLanes = 16;
+__global__ void __launch_bounds__(kSumColumns * kSumLanes) column_sum_kernel(const float* partial, int count, int width, float* out) {
+    __shared__ float lds[kSumLanes][kSumColumns];
+    const int c = threadIdx.x % kSumColumns, l = threadIdx.x / kSumColumns, col = blockIdx.x * kSumColumns + c;
+    float s = 0.f;
+    if (col < width)
+        for (int i = l; i < count; i += kSumLanes) s += partial[int64_t(i) * width + col];
+    lds[l][c] = s;
+    __syncthreads();
+    if (l == 0 && col < width) {
+        for (int i = 1; i < kSumLanes; ++i) s += lds[i][c];
+        out[col] = s;
+    }
+}
+
+// Threads per row and vectors per thread.
+struct RmsPlan {
+    int tpr, vpt;
+};
+RmsPlan rms_plan(int64_t rows, int width) {
+    const int vectors = (width + 7) / 8;
+    // Few rows leave compute units idle: as many threads as the row has vectors.  Many rows: a wave each as far as its registers go, which
+    // needs no exchange through LDS.
+    const bool few = rows < 1024;
+    const int tpr = vectors <= (few ? 64 : 256) ? 64 : vectors <= (few ? 256 : 1024) ? 256 : few && vectors <= 1024 ? 1024 : 512;
+    int vpt = (vectors + tpr - 1) / tpr;
+    if (tpr == 64 && vpt == 3) vpt = 4;
+    if (tpr == 512) vpt = 4;
+    return {tpr, vpt};
+}
+
+// Row groups of the backward pass: enough to fill the device, each of which leaves a row of partial sums behind.
+constexpr int kMostGroups = 512;
+int64_t backward_groups(const RmsPlan& p, int64_t rows) {
+    const int per_block = p.tpr == kWave ? 4 : 1;
+    return round_up(std::min<int64_t>(std::max<int64_t>(rows, 1), p.tpr == kWave ? 2 * kMostGroups : kMostGroups), per_block);
+}
+
+#define BNS_RMS_DISPATCH(T, KERNEL)                                              \
+    switch (p.tpr * 10 + p.vpt) {                                                \
+        case 641: BNS_LAUNCH((KERNEL<T, 64, 1>), grid, dim3(256), 0, st, a); break;     \
+        case 642: BNS_LAUNCH((KERNEL<T, 64, 2>), grid, dim3(256), 0, st, a); break;     \
+        case 644: BNS_LAUNCH((KERNEL<T, 64, 4>), grid, dim3(256), 0, st, a); break;     \
+        case 2561: BNS_LAUNCH((KERNEL<T, 256, 1>), grid, dim3(256), 0, st, a); break;   \
+        case 2562: BNS_LAUNCH((KERNEL<T, 256, 2>), grid, dim3(256), 0, st, a); break;   \
+        case 2563: BNS_LAUNCH((KERNEL<T, 256, 3>), grid, dim3(256), 0, st, a); break;   \
+        case 2564: BNS_LAUNCH((KERNEL<T, 256, 4>), grid, dim3(256), 0, st, a); break;   \
+        case 10241: BNS_LAUNCH((KERNEL<T, 1024, 1>), grid, dim3(1024), 0, st, a); break; \
+        default: BNS_LAUNCH((KERNEL<T, 512, 4>), grid, dim3(512), 0, st, a); break;     \
+    }
+
+constexpr int64_t kMostBlocks = int64_t(1) << 20;      // (a launch holds fewer than 2^32 threads; rows beyond are taken in turn)
+
+}  // namespace
+
+extern "C" {
+
+bns_status bns_rms_forward(const bns_rms* rms, const void* x, const void* residual, const void* weight, void* sum, void* y, float* scales,
+                           float* rstd, void* stream) {
+    RmsDims d;
+    const bns_status s = check_rms(rms, &d);
+    if (s != BNS_OK) return s;
+    const bool e4m3 = rms->out == BNS_OUT_E4M3;
+    if (sum && !residual) return BNS_EINVAL;
+    if (!e4m3 && scales) return BNS_EINVAL;
+    if (d.rows == 0) return BNS_OK;
+    if (!x || !weight || !y || (e4m3 && !scales)) return BNS_EINVAL;
+    for (const void* p : {x, residual, weight, static_cast<const void*>(sum), static_cast<const void*>(y)})
+        if (!aligned16(p)) return BNS_EINVAL;
+    const size_t e = dtype_bytes(rms->dtype), ye = e4m3 ? 1 : e, row = size_t(d.width) * e, yrow = size_t(d.width) * ye;
+    const Matrix mx = matrix(x, d.rows, d.width, d.x_stride, e), mr = matrix(residual, d.rows, d.width, d.residual_stride, e),
+                 ms = matrix(sum, d.rows, d.width, d.sum_stride, e), my = matrix(y, d.rows, d.width, d.y_stride, ye);
+    if (collide(ms, mx, true, row, row) || collide(ms, mr, true, row, row) || collide(my, mx, !e4m3, yrow, row) || collide(my, mr, false, yrow, row) ||
+        collide(my, ms, false, yrow, row))
+        return BNS_EINVAL;
+    const RmsArgs a = {x, residual, weight, sum, y, scales, rstd, d.rows, d.x_stride, d.residual_stride, d.sum_stride, d.y_stride,
+                       d.width, d.groups, rms->group, rms->weight_dtype == BNS_BF16, e4m3, rms->pow2_scales, rms->eps, 1.f / float(d.width)};
+    const RmsPlan p = rms_plan(d.rows, d.width);
+    const int per_block = p.tpr == kWave ? 4 : 1;
+    const dim3 grid(uint32_t(std::min<int64_t>((d.rows + per_block - 1) / per_block, kMostBlocks)));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rms->dtype == BNS_F32) {
+        BNS_RMS_DISPATCH(float, rms_forward_kernel)
+    } else {
+        BNS_RMS_DISPATCH(bf16_t, rms_forward_kernel)
+    }
+    return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
+}
+
+size_t bns_rms_workspace_bytes(const bns_rms* rms) {
+    RmsDims d;
+    if (check_rms(rms, &d) != BNS_OK) return 0;
+    return size_t(round_up(backward_groups(rms_plan(d.rows, d.width), d.rows) * d.width * 4, 256));
+}
+
+bns_status bns_rms_backward(const bns_rms* rms, const void* x, const void* weight, const float* rstd, const void* dy, const void* dsum, void* dx,
+                            float* dweight, void* workspace, size_t workspace_bytes, void* stream) {
+    RmsDims d;
+    const bns_status s = check_rms(rms, &d);
+    if (s != BNS_OK) return s;
+    if (!weight || !dweight || !workspace || (d.rows > 0 && (!x || !rstd || !dy || !dx))) return BNS_EINVAL;
+    for (const void* p : {x, weight, dy, dsum, static_cast<const void*>(dx), static_cast<const void*>(workspace)})
+        if (!aligned16(p)) return BNS_EINVAL;
+    const size_t e = dtype_bytes(rms->dtype), row = size_t(d.width) * e;
+    const Matrix mx = matrix(x, d.rows, d.width, d.x_stride, e), mdy = matrix(dy, d.rows, d.width, d.y_stride, e),
+                 mds = matrix(dsum, d.rows, d.width, d.residual_stride, e), mdx = matrix(dx, d.rows, d.width, d.sum_stride, e);
+    if (collide(mdx, mx, false, row, row) || collide(mdx, mdy, true, row, row) || collide(mdx, mds, true, row, row)) return BNS_EINVAL;
+    if (workspace_bytes < bns_rms_workspace_bytes(rms)) return BNS_EWORKSPACE;
+    const RmsBackwardArgs a = {x, weight, dy, dsum, rstd, dx, static_cast<float*>(workspace), d.rows, d.x_stride, d.residual_stride, d.sum_stride,
+                               d.y_stride, d.width, rms->weight_dtype == BNS_BF16, 1.f / float(d.width)};
+    const RmsPlan p = rms_plan(d.rows, d.width);
+    const int64_t groups = backward_groups(p, d.rows);
+    const dim3 grid(uint32_t(groups / (p.tpr == kWave ? 4 : 1)));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (rms->dtype == BNS_F32) {
+        BNS_RMS_DISPATCH(float, rms_backward_kernel)
+    } else {
+        BNS_RMS_DISPATCH(bf16_t, rms_backward_kernel)
+    }
+    if (hipGetLastError() != hipSuccess) return BNS_EDEVICE;
+    BNS_LAUNCH(column_sum_kernel, dim3((d.width + kSumColumns - 1) / kSumColumns), dim3(kSumColumns * kSumLanes), 0, st,
+               static_cast<const float*>(workspace), int(groups), d.width, dweight);
+    return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
+}
+
+}  // extern "C"
