@@ -71,6 +71,7 @@ _lib = _call = None
 _P = C.c_void_p
 _SHP, _SPC = C.POINTER(bns_shape), C.POINTER(bns_spec)
 _RMS, _HEAD, _DISTILL = C.POINTER(bns_rms), C.POINTER(bns_head), C.POINTER(bns_distill)
+_STRUCTURES = (_SHP, _SPC, _RMS, _HEAD, _DISTILL)
 _PROTOS = {
     "bns_status_string": (C.c_char_p, [C.c_int]),
     "bns_sample_index": (C.c_int, [_SHP, _SPC, C.c_uint64, C.POINTER(bns_box)]),
@@ -108,13 +109,14 @@ _PROTOS = {
 
 
 _EVERY_STEP = ("forward", "backward", "forward_mixed", "backward_mixed", "inference")
+_EVERY_STEP_LM = ("rms_forward", "rms_backward", "head_forward", "head_backward", "distill_forward", "distill_backward")
 
 
 class _NoExtension:
     """What _bnscall is to an interpreter that has none: every call is left to ctypes."""
 
 
-for _name in _EVERY_STEP:
+for _name in _EVERY_STEP + _EVERY_STEP_LM:
     setattr(_NoExtension, _name, staticmethod(lambda *args: None))
 
 
@@ -143,6 +145,7 @@ def load(reload: bool = False):
         call = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(call)
         call.bind(bns_shape, bns_spec, *(C.cast(getattr(lib, "bns_" + name), C.c_void_p).value for name in _EVERY_STEP))
+        call.bind_lm(bns_rms, bns_head, bns_distill, *(C.cast(getattr(lib, "bns_" + name), C.c_void_p).value for name in _EVERY_STEP_LM))
     # The current stream of a device as an integer: torch's own accessor where it has one, a tenth of the time of
     # building a Stream object (1.2 us of a call whose kernels take 4).
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -246,7 +249,7 @@ def _calls():
 def _by_ctypes(name, *args):
     """A call of every step whose arguments the extension left alone: structures, tensors and a stream as in _PROTOS."""
     types = _PROTOS[name][1]
-    plain = [C.byref(a) if t in (_SHP, _SPC) else _ptr(a) if t is _P else a for a, t in zip(args[:-1], types)]
+    plain = [C.byref(a) if t in _STRUCTURES else _ptr(a) if t is _P else a for a, t in zip(args[:-1], types)]
     return getattr(load(), name)(*plain, args[-1])
 
 
@@ -395,8 +398,10 @@ def make_distill(tokens, vocab, k, dtype="bf16", *, temperature=1.0, logits_stri
 
 
 def bns_rms_forward(rms, x, residual, weight, sum, y, scales, rstd):
-    _check(load().bns_rms_forward(C.byref(rms), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum), _ptr(y), _ptr(scales), _ptr(rstd), _stream(x)),
-           "bns_rms_forward")
+    status = _calls().rms_forward(rms, x, residual, weight, sum, y, scales, rstd, _stream(x))
+    if status is None:
+        status = _by_ctypes("bns_rms_forward", rms, x, residual, weight, sum, y, scales, rstd, _stream(x))
+    _check(status, "bns_rms_forward")
 
 
 def bns_rms_workspace_bytes(rms) -> int:
@@ -404,8 +409,10 @@ def bns_rms_workspace_bytes(rms) -> int:
 
 
 def bns_rms_backward(rms, x, weight, rstd, dy, dsum, dx, dweight, workspace):
-    _check(load().bns_rms_backward(C.byref(rms), _ptr(x), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dsum), _ptr(dx), _ptr(dweight), _ptr(workspace),
-                                   workspace.nbytes, _stream(x)), "bns_rms_backward")
+    status = _calls().rms_backward(rms, x, weight, rstd, dy, dsum, dx, dweight, workspace, workspace.nbytes, _stream(weight))
+    if status is None:
+        status = _by_ctypes("bns_rms_backward", rms, x, weight, rstd, dy, dsum, dx, dweight, workspace, workspace.nbytes, _stream(weight))
+    _check(status, "bns_rms_backward")
 
 
 def bns_head_workspace_bytes(head) -> int:
@@ -413,23 +420,31 @@ def bns_head_workspace_bytes(head) -> int:
 
 
 def bns_head_forward(head, hidden, weight, targets, loss, lse, workspace):
-    _check(load().bns_head_forward(C.byref(head), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(workspace),
-                                   workspace.nbytes, _stream(hidden)), "bns_head_forward")
+    status = _calls().head_forward(head, hidden, weight, targets, loss, lse, workspace, workspace.nbytes, _stream(weight))
+    if status is None:
+        status = _by_ctypes("bns_head_forward", head, hidden, weight, targets, loss, lse, workspace, workspace.nbytes, _stream(weight))
+    _check(status, "bns_head_forward")
 
 
 def bns_head_backward(head, hidden, weight, targets, lse, dloss, dhidden, dweight, workspace):
-    _check(load().bns_head_backward(C.byref(head), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(lse), _ptr(dloss), _ptr(dhidden), _ptr(dweight),
-                                    _ptr(workspace), workspace.nbytes, _stream(hidden)), "bns_head_backward")
+    status = _calls().head_backward(head, hidden, weight, targets, lse, dloss, dhidden, dweight, workspace, workspace.nbytes, _stream(weight))
+    if status is None:
+        status = _by_ctypes("bns_head_backward", head, hidden, weight, targets, lse, dloss, dhidden, dweight, workspace, workspace.nbytes, _stream(weight))
+    _check(status, "bns_head_backward")
 
 
 def bns_distill_forward(distill, logits, ids, teacher, dloss, loss, lse, dlogits):
-    _check(load().bns_distill_forward(C.byref(distill), _ptr(logits), _ptr(ids), _ptr(teacher), _ptr(dloss), _ptr(loss), _ptr(lse), _ptr(dlogits),
-                                      _stream(logits)), "bns_distill_forward")
+    status = _calls().distill_forward(distill, logits, ids, teacher, dloss, loss, lse, dlogits, _stream(logits))
+    if status is None:
+        status = _by_ctypes("bns_distill_forward", distill, logits, ids, teacher, dloss, loss, lse, dlogits, _stream(logits))
+    _check(status, "bns_distill_forward")
 
 
 def bns_distill_backward(distill, logits, ids, teacher, lse, dloss, dlogits):
-    _check(load().bns_distill_backward(C.byref(distill), _ptr(logits), _ptr(ids), _ptr(teacher), _ptr(lse), _ptr(dloss), _ptr(dlogits),
-                                       _stream(logits)), "bns_distill_backward")
+    status = _calls().distill_backward(distill, logits, ids, teacher, lse, dloss, dlogits, _stream(logits))
+    if status is None:
+        status = _by_ctypes("bns_distill_backward", distill, logits, ids, teacher, lse, dloss, dlogits, _stream(logits))
+    _check(status, "bns_distill_backward")
 
 
 # --------------------------------------------------------------------------------------

@@ -21,14 +21,21 @@ decltype(&bns_backward) g_backward;
 decltype(&bns_forward_mixed) g_forward_mixed;
 decltype(&bns_backward_mixed) g_backward_mixed;
 decltype(&bns_inference) g_inference;
+decltype(&bns_rms_forward) g_rms_forward;
+decltype(&bns_rms_backward) g_rms_backward;
+decltype(&bns_head_forward) g_head_forward;
+decltype(&bns_head_backward) g_head_backward;
+decltype(&bns_distill_forward) g_distill_forward;
+decltype(&bns_distill_backward) g_distill_backward;
 PyObject *g_shape_type, *g_spec_type, *g_data_ptr;
+PyObject *g_rms_type, *g_head_type, *g_distill_type;
 
 // Reads positional arguments one after the other; after one that is left to ctypes nothing more is read.  No exception stays set.
 struct Reader {
     PyObject* const* at;
     bool ok;
 
-    Reader(PyObject* const* args, Py_ssize_t given, Py_ssize_t wanted) : at(args), ok(g_shape_type && given == wanted) {}
+    Reader(PyObject* const* args, Py_ssize_t given, Py_ssize_t wanted, PyObject* bound = g_shape_type) : at(args), ok(bound && given == wanted) {}
 
     void leave() {
         PyErr_Clear();
@@ -180,6 +187,78 @@ PyObject* inference(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return finish(r, [&] { return g_inference(&shape, x, gamma, beta, mean, var, eps, y, stream); });
 }
 
+PyObject* rms_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 9, g_rms_type);
+    const bns_rms rms = r.structure<bns_rms>(g_rms_type);
+    const void *x = r.pointer(), *residual = r.pointer(), *weight = r.pointer();
+    void *sum = r.pointer(), *y = r.pointer();
+    float *scales = r.vector(), *rstd = r.vector();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_rms_forward(&rms, x, residual, weight, sum, y, scales, rstd, stream); });
+}
+
+PyObject* rms_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 11, g_rms_type);
+    const bns_rms rms = r.structure<bns_rms>(g_rms_type);
+    const void *x = r.pointer(), *weight = r.pointer();
+    const float* rstd = r.vector();
+    const void *dy = r.pointer(), *dsum = r.pointer();
+    void* dx = r.pointer();
+    float* dweight = r.vector();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_rms_backward(&rms, x, weight, rstd, dy, dsum, dx, dweight, workspace, bytes, stream); });
+}
+
+PyObject* head_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 9, g_rms_type);
+    const bns_head head = r.structure<bns_head>(g_head_type);
+    const void *hidden = r.pointer(), *weight = r.pointer();
+    const int64_t* targets = static_cast<const int64_t*>(r.pointer());
+    float *loss = r.vector(), *lse = r.vector();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_head_forward(&head, hidden, weight, targets, loss, lse, workspace, bytes, stream); });
+}
+
+PyObject* head_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 11, g_rms_type);
+    const bns_head head = r.structure<bns_head>(g_head_type);
+    const void *hidden = r.pointer(), *weight = r.pointer();
+    const int64_t* targets = static_cast<const int64_t*>(r.pointer());
+    const float *lse = r.vector(), *dloss = r.vector();
+    void *dhidden = r.pointer(), *dweight = r.pointer();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_head_backward(&head, hidden, weight, targets, lse, dloss, dhidden, dweight, workspace, bytes, stream); });
+}
+
+PyObject* distill_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 9, g_rms_type);
+    const bns_distill distill = r.structure<bns_distill>(g_distill_type);
+    const void* logits = r.pointer();
+    const int64_t* ids = static_cast<const int64_t*>(r.pointer());
+    const float *teacher = r.vector(), *dloss = r.vector();
+    float *loss = r.vector(), *lse = r.vector();
+    void* dlogits = r.pointer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_distill_forward(&distill, logits, ids, teacher, dloss, loss, lse, dlogits, stream); });
+}
+
+PyObject* distill_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 8, g_rms_type);
+    const bns_distill distill = r.structure<bns_distill>(g_distill_type);
+    const void* logits = r.pointer();
+    const int64_t* ids = static_cast<const int64_t*>(r.pointer());
+    const float *teacher = r.vector(), *lse = r.vector(), *dloss = r.vector();
+    void* dlogits = r.pointer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_distill_backward(&distill, logits, ids, teacher, lse, dloss, dlogits, stream); });
+}
+
 // bind(type of bns_shape, type of bns_spec, addresses of the five functions)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *shape, *spec;
@@ -197,9 +276,32 @@ PyObject* bind(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
+// bind_lm(types of bns_rms, bns_head, bns_distill, addresses of their functions)
+PyObject* bind_lm(PyObject*, PyObject* args) {
+    PyObject *rms, *head, *distill;
+    unsigned long long f[6];
+    if (!PyArg_ParseTuple(args, "O!O!O!KKKKKK", &PyType_Type, &rms, &PyType_Type, &head, &PyType_Type, &distill, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5]))
+        return nullptr;
+    g_rms_forward = reinterpret_cast<decltype(g_rms_forward)>(f[0]);
+    g_rms_backward = reinterpret_cast<decltype(g_rms_backward)>(f[1]);
+    g_head_forward = reinterpret_cast<decltype(g_head_forward)>(f[2]);
+    g_head_backward = reinterpret_cast<decltype(g_head_backward)>(f[3]);
+    g_distill_forward = reinterpret_cast<decltype(g_distill_forward)>(f[4]);
+    g_distill_backward = reinterpret_cast<decltype(g_distill_backward)>(f[5]);
+    Py_INCREF(rms);
+    Py_INCREF(head);
+    Py_INCREF(distill);
+    Py_XSETREF(g_rms_type, rms);
+    Py_XSETREF(g_head_type, head);
+    Py_XSETREF(g_distill_type, distill);
+    Py_RETURN_NONE;
+}
+
 #define BNS_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {{"bind", &bind, METH_VARARGS, nullptr}, BNS_FAST(forward), BNS_FAST(backward), BNS_FAST(forward_mixed),
-                           BNS_FAST(backward_mixed),               BNS_FAST(inference), {nullptr, nullptr, 0, nullptr}};
+                           BNS_FAST(backward_mixed),               BNS_FAST(inference),
+                           {"bind_lm", &bind_lm, METH_VARARGS, nullptr}, BNS_FAST(rms_forward), BNS_FAST(rms_backward), BNS_FAST(head_forward),
+                           BNS_FAST(head_backward),                BNS_FAST(distill_forward), BNS_FAST(distill_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_bnscall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

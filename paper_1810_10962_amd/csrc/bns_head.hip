@@ -10,33 +10,15 @@
 #include <algorithm>
 
 #include "bns_internal.hpp"
-#include "bns_lm_device.hpp"
+#include "bns_head_device.hpp"
+#include "bns_head_direct.hpp"
 #include "bns_lm_validate.hpp"
 
 using namespace bns;
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kDepth = 64;      // elements of k in a staged tile: 128 bytes a row
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-
-// ---- parts of an fp32 value ---------------------------------------------------------------------------------------
-// x = hi + mid + lo exactly, each of them the bf16 nearest to what is left (cut off instead where that would overflow).  Infinities and NaN are
-// hi alone.  A product of two values needs the six pairs of parts whose exponents reach into an fp32 result: what is dropped is
-// at most 2^-24 of it.
-__device__ __forceinline__ void split3(float x, uint32_t (&part)[3]) {
-    part[0] = f32_to_bf16(x);
-    if (fabsf(x) > 0x1.fep127f) part[0] = __float_as_uint(x) >> 16;
-    float r = x - bf16_to_f32(part[0]);
-    if (!(fabsf(r) < __builtin_inff())) r = 0.f;
-    part[1] = f32_to_bf16(r);
-    part[2] = f32_to_bf16(r - bf16_to_f32(part[1]));
-}
 
 // ---- laying operands out ------------------------------------------------------------------------------------------
 struct PackArgs {
@@ -48,9 +30,6 @@ struct PackArgs {
     int32_t depth;              // elements of k in a plane of dst, padded with zeros; a row of dst holds its planes one behind the other
     int32_t vocab;
 };
-
-template <typename T>
-constexpr int planes_of() { return sizeof(T) == 4 ? 3 : 1; }
 
 // Row r of src becomes row r of dst (k = the column).
 template <typename T>
@@ -129,32 +108,7 @@ __global__ void __launch_bounds__(256) pack_columns_kernel(PackArgs a) {
 }
 
 // ---- the product --------------------------------------------------------------------------------------------------
-enum Epilogue { kStatistics, kGradient, kAccumulate, kStore };
-
-struct GemmArgs {
-    const void *a, *b;
-    int64_t lda, ldb;           // elements from row to row
-    int32_t rows_a, rows_b;     // rows that exist; those beyond in a tile are read as the last one and their results left out
-    int32_t depth;              // elements of k in a plane, a multiple of kDepth
-    int32_t splits;             // k is divided between so many blocks (kAccumulate)
-    int32_t tiles_a, tiles_b;
-    // logits: m = row of the piece, n = token
-    const int64_t* targets;
-    const float *lse, *dloss;
-    float2* partial;            // [tile of the whole vocabulary][token]: maximum and sum of a tile's logits, in powers of two
-    float* at_target;           // [token]
-    uint16_t *g, *gt;           // [token][planes][g_depth], [row of the piece][planes][gt_depth]
-    int32_t v0, vocab, g_depth, gt_depth;
-    // gradients: m = column, n = token / row of the piece
-    void* out;
-    int64_t ldo, split_stride;  // of out, in elements
-    int32_t fresh;              // kAccumulate: out holds nothing yet
-};
-
-// Which pairs of planes an fp32 product takes, smallest first.
-__device__ __forceinline__ int plane_a(int segment) { return (0x010120 >> (4 * segment)) & 3; }      // 0 2 1 0 1 0
-__device__ __forceinline__ int plane_b(int segment) { return (0x001102 >> (4 * segment)) & 3; }      // 2 0 1 1 0 0
-
+// Operands that are k-contiguous bf16 in memory (in three planes, where they are the parts of fp32 values): a row beyond the last is read as the last.
 template <int BM, int BN, int WM, int WN>
 struct Tile {
     static constexpr int kThreads = WM * WN * kWave, kPerIssue = kThreads / 8;       // rows that all threads bring in at once
@@ -162,16 +116,6 @@ struct Tile {
     static constexpr int kBytes = (BM + BN) * kDepth * 2;
     static_assert(BM % kPerIssue == 0 && BN % kPerIssue == 0, "whole issues");
 };
-
-// Block -> tile.  Blocks go round robin over the eight dies, each with an L2 of its own: a die gets a contiguous range of tiles, walked in groups of
-// four rows of tiles, so that the tiles in flight share their operands.
-__device__ __forceinline__ void place(int block, int total, int tiles_a, int tiles_b, int& ta, int& tb) {
-    const int die = block % 8, q = total / 8, r = total % 8;
-    const int i = die * q + min(die, r) + block / 8;
-    const int group = i / (4 * tiles_b), in = i - group * 4 * tiles_b, high = min(4, tiles_a - 4 * group);
-    tb = in / high;
-    ta = 4 * group + in - tb * high;
-}
 
 template <typename T, int BM, int BN, int WM, int WN, int EPILOGUE>
 __global__ void __launch_bounds__(WM* WN* kWave) gemm_kernel(GemmArgs a) {
@@ -243,129 +187,23 @@ __global__ void __launch_bounds__(WM* WN* kWave) gemm_kernel(GemmArgs a) {
         }
     }
 
-    // acc[i][j][e] is C[m][n] of m = m_base + 16 i + e, n = n_base + 16 j
-    const int m_base = m0 + wm * S::kM + quarter * 4, n_base = n0 + wn * S::kN + r16;
-    if constexpr (EPILOGUE == kStatistics) {
-        __syncthreads();
-        float2* const stat = reinterpret_cast<float2*>(lds);        // [WM][BN]
-#pragma unroll
-        for (int j = 0; j < S::NI; ++j) {
-            const int n = n_base + 16 * j;
-            const int64_t target = n < a.rows_b ? a.targets[n] : -1;
-            const int aim = target >= 0 && target < a.vocab ? int(target) - a.v0 - m_base : -1;
-            float m = -__builtin_inff(), l = 0.f;
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (aim == 16 * i + e) a.at_target[n] = acc[i][j][e];
-                    acc[i][j][e] = m_base + 16 * i + e < a.rows_a ? acc[i][j][e] * kLog2e : -__builtin_inff();
-                    m = fmaxf(m, acc[i][j][e]);
-                }
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), -3e38f);        // (a finite number where the wave has no row)
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(acc[i][j][e] - m);
-            l += __shfl_xor(l, 16);
-            l += __shfl_xor(l, 32);
-            if (quarter == 0) stat[wm * BN + wn * S::kN + 16 * j + r16] = float2{m, l};
-        }
-        __syncthreads();
-        for (int c = threadIdx.x; c < BN; c += S::kThreads) {
-            if (n0 + c >= a.rows_b) continue;
-            float m = stat[c].x, l = 0.f;
-#pragma unroll
-            for (int w = 1; w < WM; ++w) m = fmaxf(m, stat[w * BN + c].x);
-#pragma unroll
-            for (int w = 0; w < WM; ++w) l = fmaf(stat[w * BN + c].y, __builtin_amdgcn_exp2f(stat[w * BN + c].x - m), l);
-            a.partial[int64_t(a.v0 / BM + ta) * a.rows_b + n0 + c] = float2{m, l};
-        }
-    }
-    if constexpr (EPILOGUE == kGradient) {
-#pragma unroll
-        for (int j = 0; j < S::NI; ++j) {
-            const int n = n_base + 16 * j;
-            int64_t target = -1;
-            float lse = 0.f, scale = 0.f;
-            if (n < a.rows_b) {
-                target = a.targets[n];
-                lse = a.lse[n];
-                scale = a.dloss[n];
-            }
-            const bool valid = target >= 0 && target < a.vocab;
-            const int aim = valid ? int(target) - a.v0 - m_base : -1;
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i) {
-                const int m = m_base + 16 * i;
-                uint32_t part[4][3];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float f = __builtin_amdgcn_exp2f((acc[i][j][e] - lse) * kLog2e);
-                    if (aim == 16 * i + e) f -= 1.f;
-                    f = valid && m + e < a.rows_a ? f * scale : 0.f;
-                    if (P == 1) part[e][0] = f32_to_bf16(f);
-                    else split3(f, part[e]);
-                }
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    if (n < a.gt_depth && m < a.g_depth) {
-                        if (n < a.rows_b)
-                            *reinterpret_cast<u2*>(a.g + int64_t(n) * a.g_depth * P + int64_t(p) * a.g_depth + m) =
-                                u2{part[0][p] | part[1][p] << 16, part[2][p] | part[3][p] << 16};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (m + e < a.rows_a) a.gt[int64_t(m + e) * a.gt_depth * P + int64_t(p) * a.gt_depth + n] = uint16_t(part[e][p]);
-                    }
-                }
-            }
-        }
-    }
-    if constexpr (EPILOGUE == kAccumulate) {
-        float* const out = static_cast<float*>(a.out) + split * a.split_stride;
-#pragma unroll
-        for (int j = 0; j < S::NI; ++j) {
-            const int n = n_base + 16 * j;
-            if (n >= a.rows_b) continue;
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i) {
-                if (m_base + 16 * i >= a.rows_a) continue;
-                f32x4* const p = reinterpret_cast<f32x4*>(out + n * a.ldo + m_base + 16 * i);
-                *p = a.fresh ? acc[i][j] : *p + acc[i][j];
-            }
-        }
-    }
-    if constexpr (EPILOGUE == kStore) {
-        T* const out = static_cast<T*>(a.out);
-#pragma unroll
-        for (int j = 0; j < S::NI; ++j) {
-            const int n = n_base + 16 * j;
-            if (n >= a.rows_b) continue;
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i) {
-                const int m = m_base + 16 * i;
-                T* const p = out + n * a.ldo + m;
-                if (m + 4 <= a.rows_a) {
-                    if constexpr (P == 1) {
-                        typedef u2 u2e __attribute__((aligned(2)));
-                        *reinterpret_cast<u2e*>(p) = u2{pack_bf16x2(acc[i][j][0], acc[i][j][1]), pack_bf16x2(acc[i][j][2], acc[i][j][3])};
-                    } else {
-                        typedef f32x4 f32x4e __attribute__((aligned(4)));
-                        *reinterpret_cast<f32x4e*>(p) = acc[i][j];
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (m + e < a.rows_a) {
-                            if constexpr (P == 1) p[e].bits = uint16_t(f32_to_bf16(acc[i][j][e]));
-                            else p[e] = acc[i][j][e];
-                        }
-                }
-            }
-        }
-    }
+    finish<T, EPILOGUE, BM, BN, WM, WN>(a, acc, ta, tb, split, reinterpret_cast<float2*>(lds));
 #endif
+}
+
+template <typename T, int BM, int BN, int WM, int WN, int EPILOGUE>
+__global__ void __launch_bounds__(WM* WN* kWave) direct_logits_kernel(GemmArgs a) {
+    __shared__ __attribute__((aligned(16))) char lds[DirectTile<T, BM, BN, WM, WN>::kBytes];
+    direct_tile<T, BM, BN, WM, WN, true, true, EPILOGUE>(a, int(blockIdx.x), lds);
+}
+
+// Both gradients from g in one launch: the first blocks take dhidden, whose k is the vocabulary, the others dweight, whose k is the tokens.
+template <typename T, int BM, int BN, int WM, int WN, int BW, int EPILOGUE>
+__global__ void __launch_bounds__(256) direct_gradients_kernel(GemmArgs h, GemmArgs w, int blocks_h) {
+    constexpr int kH = DirectTile<T, BM, BN, WM, WN>::kBytes, kW = DirectTile<T, BW, BW, 2, 2>::kBytes;
+    __shared__ __attribute__((aligned(16))) char lds[kH > kW ? kH : kW];
+    if (int(blockIdx.x) < blocks_h) direct_tile<T, BM, BN, WM, WN, false, true, EPILOGUE>(h, int(blockIdx.x), lds);
+    else direct_tile<T, BW, BW, 2, 2, false, false, kStore>(w, int(blockIdx.x) - blocks_h, lds);
 }
 
 // ---- what follows the products --------------------------------------------------------------------------------------
@@ -422,17 +260,54 @@ __global__ void __launch_bounds__(256) fill_zero_kernel(uint16_t* p, int64_t n) 
 constexpr int kTileM = 256;
 
 struct HeadPlan {
+    bool direct;                            // operands are read as they lie in memory
+    int tile;                               // direct: tokens of a tile, 16, 32, 64 or 128
+    int64_t piece;                          // rows of a piece of the vocabulary
+    int splits;                             // of dhidden
+    // laid out:
     int planes;
-    int64_t depth_d, depth_t, piece;        // padded width, tokens, rows of a piece
+    int64_t depth_d, depth_t;               // padded width, tokens
     bool direct_h, direct_w;                // read where they are, without a copy
     bool narrow;                            // few tokens: tiles of 64 of them
-    int splits;                             // of dhidden
     // offsets into the workspace
     size_t hidden, weight, partial, at_target, weight_t, hidden_t, g, gt, sums, forward_bytes, backward_bytes;
 };
 
-HeadPlan head_plan(const HeadDims& d) {
-    HeadPlan p;
+struct Offsets {
+    size_t at = 0;
+    size_t take(size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 1023) & ~size_t(1023);
+        return here;
+    }
+};
+
+HeadPlan direct_plan(const HeadDims& d) {
+    HeadPlan p = {};
+    const size_t e = dtype_bytes(d.dtype), T = size_t(d.tokens);
+    p.direct = true;
+    p.tile = d.tokens <= 16 ? 16 : d.tokens <= 32 ? 32 : 64;
+    if (g_tuning.head_tile == 128) p.tile = 128;
+    p.depth_d = round_up(d.width, 8);
+    // g of a piece takes 64 MB at most
+    const int64_t piece = d.piece ? d.piece : std::max<int64_t>(1024, (int64_t(64) << 20) / int64_t(std::max<size_t>(T * e, 1)));
+    p.piece = std::min(round_up(std::min<int64_t>(piece, 1 << 19), kTileM), round_up(d.vocab, kTileM));
+    const int m = p.tile == 128 ? 128 : 64;
+    const int64_t tiles = ((d.width + m - 1) / m) * ((d.tokens + p.tile - 1) / p.tile), steps = std::min<int64_t>(p.piece, d.vocab) / (d.dtype == BNS_F32 ? 32 : 64);
+    p.splits = int(std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(tiles, 1), steps / 4)));
+    Offsets o;
+    p.partial = o.take(size_t((d.vocab + m - 1) / m) * T * sizeof(float2));
+    p.at_target = o.take(T * 4);
+    p.forward_bytes = o.at;
+    o.at = 0;
+    p.g = o.take(T * p.piece * e);
+    p.sums = o.take(size_t(p.splits) * T * p.depth_d * 4);
+    p.backward_bytes = o.at;
+    return p;
+}
+
+HeadPlan laid_out_plan(const HeadDims& d) {
+    HeadPlan p = {};
     p.planes = d.dtype == BNS_F32 ? 3 : 1;
     p.depth_d = round_up(d.width, kDepth);
     p.depth_t = round_up(std::max<int64_t>(d.tokens, 1), kDepth);
@@ -440,32 +315,36 @@ HeadPlan head_plan(const HeadDims& d) {
     p.direct_h = fits && d.hidden_stride % 8 == 0 && d.hidden_stride < (1 << 21);
     p.direct_w = fits && d.weight_stride % 8 == 0 && d.weight_stride < (1 << 21);
     p.narrow = d.tokens <= 64;
-    int64_t piece = d.piece ? d.piece : 16384;
+    const int64_t piece = d.piece ? d.piece : 16384;
     p.piece = std::min(round_up(std::min<int64_t>(piece, 1 << 18), kTileM), round_up(d.vocab, kTileM));
     const int64_t tiles = ((d.width + kTileM - 1) / kTileM) * ((d.tokens + (p.narrow ? 63 : 255)) / (p.narrow ? 64 : 256));
     p.splits = int(std::max<int64_t>(1, std::min<int64_t>(256 / std::max<int64_t>(tiles, 1), p.piece / 512)));
-    size_t at = 0;
-    const auto take = [&](size_t bytes) {
-        const size_t here = at;
-        at += (bytes + 1023) & ~size_t(1023);
-        return here;
-    };
     const size_t P = size_t(p.planes) * 2, T = size_t(d.tokens), rows = size_t(p.piece);
-    p.hidden = take(p.direct_h ? 0 : T * p.depth_d * P);
-    p.weight = take(p.direct_w ? 0 : rows * p.depth_d * P);
-    const size_t both = at;
-    p.partial = take(size_t((d.vocab + kTileM - 1) / kTileM) * T * sizeof(float2));
-    p.at_target = take(T * 4);
-    p.forward_bytes = at;
-    at = both;
-    p.weight_t = take(size_t(d.width) * rows * P);
-    p.hidden_t = take(size_t(d.width) * p.depth_t * P);
-    p.g = take(T * rows * P);
-    p.gt = take(rows * p.depth_t * P);
-    p.sums = take(size_t(p.splits) * T * p.depth_d * 4);
-    p.backward_bytes = at;
+    Offsets o;
+    p.hidden = o.take(p.direct_h ? 0 : T * p.depth_d * P);
+    p.weight = o.take(p.direct_w ? 0 : rows * p.depth_d * P);
+    const size_t both = o.at;
+    p.partial = o.take(size_t((d.vocab + kTileM - 1) / kTileM) * T * sizeof(float2));
+    p.at_target = o.take(T * 4);
+    p.forward_bytes = o.at;
+    o.at = both;
+    p.weight_t = o.take(size_t(d.width) * rows * P);
+    p.hidden_t = o.take(size_t(d.width) * p.depth_t * P);
+    p.g = o.take(T * rows * P);
+    p.gt = o.take(rows * p.depth_t * P);
+    p.sums = o.take(size_t(p.splits) * T * p.depth_d * 4);
+    p.backward_bytes = o.at;
     return p;
 }
+
+HeadPlan head_plan(const HeadDims& d) {
+    const int path = g_tuning.head_path;
+    const bool direct = path ? path == 1 : d.tokens <= 64;
+    return direct ? direct_plan(d) : laid_out_plan(d);
+}
+
+// (never 0, which stands for an invalid description)
+inline size_t need(const HeadPlan& p) { return std::max<size_t>(std::max(p.forward_bytes, p.backward_bytes), 1024); }
 
 inline bool failed() { return hipGetLastError() != hipSuccess; }
 
@@ -491,6 +370,20 @@ bool gemm(GemmArgs a, bool narrow, hipStream_t st) {
     const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b * a.splits);
     if (narrow) BNS_LAUNCH((gemm_kernel<T, 256, 64, 4, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
     else BNS_LAUNCH((gemm_kernel<T, 256, 256, 2, 4, EPILOGUE>), grid, dim3(512), 0, st, a);
+    return !failed();
+}
+
+bool join_statistics(const HeadDims& d, const HeadPlan& p, int tile, const int64_t* targets, float* loss, float* lse, char* ws, hipStream_t st) {
+    BNS_LAUNCH(join_statistics_kernel, dim3(uint32_t((d.tokens + 15) / 16)), dim3(256), 0, st, reinterpret_cast<const float2*>(ws + p.partial),
+               reinterpret_cast<const float*>(ws + p.at_target), targets, (d.vocab + tile - 1) / tile, int(d.tokens), d.vocab, loss, lse);
+    return !failed();
+}
+
+template <typename T>
+bool join_splits(const HeadDims& d, const HeadPlan& p, void* dhidden, char* ws, hipStream_t st) {
+    const int64_t blocks = (d.tokens * ((d.width + 7) / 8) + 255) / 256;
+    BNS_LAUNCH((join_splits_kernel<T>), dim3(uint32_t(std::min<int64_t>(blocks, 1 << 16))), dim3(256), 0, st, reinterpret_cast<const float*>(ws + p.sums),
+               d.tokens * p.depth_d, p.splits, int(d.tokens), d.width, int(p.depth_d), static_cast<T*>(dhidden));
     return !failed();
 }
 
@@ -525,19 +418,13 @@ bool forward(const HeadDims& d, const HeadPlan& p, const void* hidden, const voi
         a.at_target = reinterpret_cast<float*>(ws + p.at_target);
         if (!gemm<T, kStatistics>(a, p.narrow, st)) return false;
     }
-    BNS_LAUNCH(join_statistics_kernel, dim3(uint32_t((d.tokens + 15) / 16)), dim3(256), 0, st, reinterpret_cast<const float2*>(ws + p.partial),
-               reinterpret_cast<const float*>(ws + p.at_target), targets, int((d.vocab + kTileM - 1) / kTileM), int(d.tokens), d.vocab, loss, lse);
-    return !failed();
+    return join_statistics(d, p, kTileM, targets, loss, lse, ws, st);
 }
 
 template <typename T>
 bool backward(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, const float* lse, const float* dloss,
               void* dhidden, void* dweight, char* ws, hipStream_t st) {
     const int planes = p.planes;
-    if (d.tokens == 0) {
-        BNS_LAUNCH(fill_zero_kernel, dim3(4096), dim3(256), 0, st, static_cast<uint16_t*>(dweight), int64_t(d.vocab) * d.width * int64_t(sizeof(T) / 2));
-        return !failed();
-    }
     if (!p.direct_h && !pack_rows<T>(hidden, d.hidden_stride, d.tokens, d.width, p.depth_d, ws + p.hidden, st)) return false;
     if (!pack_columns<T>(hidden, d.hidden_stride, d.tokens, d.width, p.depth_t, targets, d.vocab, ws + p.hidden_t, st)) return false;
     for (int64_t v0 = 0; v0 < d.vocab; v0 += p.piece) {
@@ -552,7 +439,7 @@ bool backward(const HeadDims& d, const HeadPlan& p, const void* hidden, const vo
         a.gt = reinterpret_cast<uint16_t*>(ws + p.gt);
         a.g_depth = int32_t(depth_v);
         a.gt_depth = int32_t(p.depth_t);
-        if (!gemm<T, kGradient>(a, p.narrow, st)) return false;
+        if (!gemm<T, kGradientParts>(a, p.narrow, st)) return false;
         const void* piece = static_cast<const T*>(weight) + v0 * d.weight_stride;
         if (!pack_columns<T>(piece, d.weight_stride, rows, d.width, depth_v, nullptr, 0, ws + p.weight_t, st)) return false;
         // dhidden[n][m] += sum over the piece of g[n] weight[m]
@@ -582,10 +469,109 @@ bool backward(const HeadDims& d, const HeadPlan& p, const void* hidden, const vo
         w.ldo = d.width;
         if (!gemm<T, kStore>(w, false, st)) return false;
     }
-    const int64_t blocks = (d.tokens * ((d.width + 7) / 8) + 255) / 256;
-    BNS_LAUNCH((join_splits_kernel<T>), dim3(uint32_t(std::min<int64_t>(blocks, 1 << 16))), dim3(256), 0, st, reinterpret_cast<const float*>(ws + p.sums),
-               d.tokens * p.depth_d, p.splits, int(d.tokens), d.width, int(p.depth_d), static_cast<T*>(dhidden));
+    return join_splits<T>(d, p, dhidden, ws, st);
+}
+
+// ---- the same, operands as they lie in memory -------------------------------------------------------------------------
+template <typename T, int EPILOGUE>
+bool direct_logits(GemmArgs a, int tile, hipStream_t st) {
+    const int m = tile == 128 ? 128 : 64;
+    a.tiles_a = (a.rows_a + m - 1) / m;
+    a.tiles_b = (a.rows_b + tile - 1) / tile;
+    const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b);
+    if (tile == 16) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (tile == 32) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (tile == 64) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else BNS_LAUNCH((direct_logits_kernel<T, 128, 128, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
     return !failed();
+}
+
+template <typename T, int EPILOGUE>
+bool direct_gradients(GemmArgs h, GemmArgs w, int tile, hipStream_t st) {
+    const int m = tile == 128 ? 128 : 64;
+    h.tiles_a = w.tiles_a = (h.rows_a + m - 1) / m;
+    h.tiles_b = (h.rows_b + tile - 1) / tile;
+    w.tiles_b = (w.rows_b + m - 1) / m;
+    const int blocks_h = h.tiles_a * h.tiles_b * h.splits;
+    const dim3 grid(uint32_t(blocks_h) + uint32_t(w.tiles_a) * w.tiles_b);
+    if (tile == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else if (tile == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else if (tile == 64) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else BNS_LAUNCH((direct_gradients_kernel<T, 128, 128, 2, 2, 128, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    return !failed();
+}
+
+GemmArgs direct_operands(const HeadDims& d, const void* hidden, const void* weight, const int64_t* targets, int64_t v0, int rows) {
+    GemmArgs a = {};
+    a.a = static_cast<const char*>(weight) + v0 * d.weight_stride * int64_t(dtype_bytes(d.dtype));
+    a.b = hidden;
+    a.lda = d.weight_stride;
+    a.ldb = d.hidden_stride;
+    a.rows_a = rows;
+    a.rows_b = int32_t(d.tokens);
+    a.depth = d.width;
+    a.splits = 1;
+    a.targets = targets;
+    a.v0 = int32_t(v0);
+    a.vocab = d.vocab;
+    return a;
+}
+
+template <typename T>
+bool forward_direct(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, float* loss, float* lse, char* ws,
+                    hipStream_t st) {
+    const int m = p.tile == 128 ? 128 : 64;
+    const int64_t most = std::max<int64_t>(1, (1 << 22) / ((d.tokens + p.tile - 1) / p.tile)) * m;
+    for (int64_t v0 = 0; v0 < d.vocab; v0 += most) {
+        GemmArgs a = direct_operands(d, hidden, weight, targets, v0, int(std::min<int64_t>(most, d.vocab - v0)));
+        a.partial = reinterpret_cast<float2*>(ws + p.partial);
+        a.at_target = reinterpret_cast<float*>(ws + p.at_target);
+        if (!direct_logits<T, kStatistics>(a, p.tile, st)) return false;
+    }
+    return join_statistics(d, p, m, targets, loss, lse, ws, st);
+}
+
+template <typename T>
+bool backward_direct(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, const float* lse, const float* dloss,
+                     void* dhidden, void* dweight, char* ws, hipStream_t st) {
+    const bool whole = p.splits == 1 && p.piece >= d.vocab;     // dhidden needs no sums beside it
+    for (int64_t v0 = 0; v0 < d.vocab; v0 += p.piece) {
+        const int rows = int(std::min<int64_t>(p.piece, d.vocab - v0));
+        GemmArgs a = direct_operands(d, hidden, weight, targets, v0, rows);
+        a.lse = lse;
+        a.dloss = dloss;
+        a.out = ws + p.g;
+        a.ldo = p.piece;
+        if (!direct_logits<T, kGradient>(a, p.tile, st)) return false;
+        GemmArgs h = {};
+        h.a = a.a;
+        h.lda = a.lda;
+        h.b = ws + p.g;
+        h.ldb = p.piece;
+        h.rows_a = d.width;
+        h.rows_b = int32_t(d.tokens);
+        h.depth = rows;
+        h.splits = p.splits;
+        h.out = whole ? dhidden : ws + p.sums;
+        h.ldo = whole ? d.width : p.depth_d;
+        h.split_stride = d.tokens * p.depth_d;
+        h.fresh = v0 == 0;
+        GemmArgs w = {};
+        w.a = hidden;
+        w.lda = d.hidden_stride;
+        w.b = ws + p.g;
+        w.ldb = p.piece;
+        w.rows_a = d.width;
+        w.rows_b = rows;
+        w.depth = int32_t(d.tokens);
+        w.splits = 1;
+        w.targets = targets;
+        w.vocab = d.vocab;
+        w.out = static_cast<T*>(dweight) + v0 * d.width;
+        w.ldo = d.width;
+        if (whole ? !direct_gradients<T, kStore>(h, w, p.tile, st) : !direct_gradients<T, kAccumulate>(h, w, p.tile, st)) return false;
+    }
+    return whole || join_splits<T>(d, p, dhidden, ws, st);
 }
 
 }  // namespace
@@ -596,7 +582,7 @@ size_t bns_head_workspace_bytes(const bns_head* head) {
     HeadDims d;
     if (check_head(head, &d) != BNS_OK) return 0;
     const HeadPlan p = head_plan(d);
-    return std::max(p.forward_bytes, p.backward_bytes);
+    return need(p);
 }
 
 bns_status bns_head_forward(const bns_head* head, const void* hidden, const void* weight, const int64_t* targets, float* loss, float* lse,
@@ -608,11 +594,11 @@ bns_status bns_head_forward(const bns_head* head, const void* hidden, const void
     if (!hidden || !weight || !targets || !loss || !lse || !workspace) return BNS_EINVAL;
     if (!aligned16(hidden) || !aligned16(weight) || !aligned16(workspace)) return BNS_EINVAL;
     const HeadPlan p = head_plan(d);
-    if (workspace_bytes < std::max(p.forward_bytes, p.backward_bytes)) return BNS_EWORKSPACE;
+    if (workspace_bytes < need(p)) return BNS_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
-    const bool ok = d.dtype == BNS_F32 ? forward<float>(d, p, hidden, weight, targets, loss, lse, ws, st)
-                                       : forward<bf16_t>(d, p, hidden, weight, targets, loss, lse, ws, st);
+    const auto call = d.dtype == BNS_F32 ? (p.direct ? forward_direct<float> : forward<float>) : p.direct ? forward_direct<bf16_t> : forward<bf16_t>;
+    const bool ok = call(d, p, hidden, weight, targets, loss, lse, ws, st);
     return ok ? BNS_OK : BNS_EDEVICE;
 }
 
@@ -632,11 +618,15 @@ bns_status bns_head_backward(const bns_head* head, const void* hidden, const voi
             if (collide(out, in, false, row, row)) return BNS_EINVAL;
     if (collide(mdh, mdw, false, row, row)) return BNS_EINVAL;
     const HeadPlan p = head_plan(d);
-    if (workspace_bytes < std::max(p.forward_bytes, p.backward_bytes)) return BNS_EWORKSPACE;
+    if (workspace_bytes < need(p)) return BNS_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
-    const bool ok = d.dtype == BNS_F32 ? backward<float>(d, p, hidden, weight, targets, lse, dloss, dhidden, dweight, ws, st)
-                                       : backward<bf16_t>(d, p, hidden, weight, targets, lse, dloss, dhidden, dweight, ws, st);
+    if (d.tokens == 0) {
+        BNS_LAUNCH(fill_zero_kernel, dim3(4096), dim3(256), 0, st, static_cast<uint16_t*>(dweight), int64_t(d.vocab) * d.width * int64_t(e / 2));
+        return failed() ? BNS_EDEVICE : BNS_OK;
+    }
+    const auto call = d.dtype == BNS_F32 ? (p.direct ? backward_direct<float> : backward<float>) : p.direct ? backward_direct<bf16_t> : backward<bf16_t>;
+    const bool ok = call(d, p, hidden, weight, targets, lse, dloss, dhidden, dweight, ws, st);
     return ok ? BNS_OK : BNS_EDEVICE;
 }
 

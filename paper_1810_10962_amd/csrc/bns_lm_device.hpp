@@ -62,6 +62,48 @@ struct Row8<bf16_t> {
     }
 };
 
+// The same eight elements as they are stored, so that a row that is asked for ahead of its turn takes no more registers than memory.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    typedef u4 u4e __attribute__((aligned(4)));
+    u4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = *reinterpret_cast<const u4e*>(p);
+        b = *reinterpret_cast<const u4e*>(p + 4);
+    }
+    __device__ __forceinline__ void load_left(const float* p, int left) {       // the first `left` elements, zeros behind them
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = i < left ? __float_as_uint(p[i]) : 0u;
+            b[i] = 4 + i < left ? __float_as_uint(p[4 + i]) : 0u;
+        }
+    }
+    __device__ __forceinline__ void clear() { a = b = u4{0, 0, 0, 0}; }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(a[i]), f[4 + i] = __uint_as_float(b[i]);
+    }
+};
+template <>
+struct Raw8<bf16_t> {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    typedef u4 u4e __attribute__((aligned(2)));
+    u4 a;
+    __device__ __forceinline__ void load(const bf16_t* p) { a = *reinterpret_cast<const u4e*>(p); }
+    __device__ __forceinline__ void load_left(const bf16_t* p, int left) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = uint32_t(2 * i < left ? p[2 * i].bits : 0) | uint32_t(2 * i + 1 < left ? p[2 * i + 1].bits : 0) << 16;
+    }
+    __device__ __forceinline__ void clear() { a = u4{0, 0, 0, 0}; }
+    __device__ __forceinline__ void unpack(float (&f)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(a[i] << 16), f[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+    }
+};
+
 // Maximum over the 64 lanes of a wave, as a wave-uniform value; as wave_sum, NaN counting for nothing.
 __device__ __forceinline__ float wave_max(float v) {
 #define BNS_MAX_STEP(ctrl, rows) \

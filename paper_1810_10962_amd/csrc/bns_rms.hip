@@ -29,7 +29,7 @@ struct RmsBackwardArgs {
     const void *x, *weight, *dy, *dsum;
     const float* rstd;
     void* dx;
-    float* partial;     // [row groups][width]
+    float* partial;     // [blocks][width]
     int64_t rows, x_stride, dsum_stride, dx_stride, dy_stride;
     int32_t width, weight_bf16;
     float inv_width;
@@ -40,12 +40,11 @@ __device__ __forceinline__ void load_weight(const void* w, int bf16, int col, in
     else Row8<float>::load(static_cast<const float*>(w) + col, left, f);
 }
 
-// Sum / maximum over the TPR threads of a row; `lds` holds a float for every wave.
+// Sum / maximum over the TPR threads of a row; `lds` holds a float for every wave, and two calls in a row are given two different ones.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* lds) {
     v = wave_sum(v);
     if (TPR == kWave) return v;
-    __syncthreads();                    // (the values of the last use have been read)
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
     __syncthreads();
     float s = 0.f;
@@ -57,7 +56,6 @@ template <int TPR>
 __device__ __forceinline__ float row_max(float v, float* lds) {
     v = wave_max(v);
     if (TPR == kWave) return v;
-    __syncthreads();
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
     __syncthreads();
     float s = lds[0];
@@ -65,6 +63,43 @@ __device__ __forceinline__ float row_max(float v, float* lds) {
     for (int i = 1; i < TPR / kWave; ++i) s = fmaxf(s, lds[i]);
     return s;
 }
+
+// The vectors of a row that a thread holds.  RAGGED: the width is no multiple of eight, so the last vector goes element by element.  Otherwise
+// a vector lies in the row or behind it, and what lies behind is read from the row's last vector and cleared: the loads stand in no branch,
+// so that all of them are on their way at once.
+template <typename T, int TPR, int VPT, bool RAGGED>
+struct RowOf {
+    Raw8<T> raw[RAGGED ? 1 : VPT];
+    float f[RAGGED ? VPT : 1][8];
+
+    __device__ __forceinline__ void load(const T* p, int t, int width) {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int col = (j * TPR + t) * 8;
+            if constexpr (RAGGED) {
+                if (col < width) {
+                    Row8<T>::load(p + col, width - col, f[j]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[j][i] = 0.f;
+                }
+            } else {
+                raw[j].load(p + min(col, width - 8));
+            }
+        }
+    }
+    __device__ __forceinline__ void get(int j, int t, int width, float (&out)[8]) const {
+        if constexpr (RAGGED) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = f[j][i];
+        } else {
+            const bool in = (j * TPR + t) * 8 < width;
+            raw[j].unpack(out);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = in ? out[i] : 0.f;
+        }
+    }
+};
 
 // The scale of values whose largest magnitude is `most`: see include/bns.h.
 __device__ __forceinline__ float e4m3_scale(float most, int pow2) {
@@ -77,58 +112,45 @@ __device__ __forceinline__ float e4m3_scale(float most, int pow2) {
 template <int TPR>
 constexpr int block_of() { return TPR == kWave ? 256 : TPR; }
 
-template <typename T, int TPR, int VPT>
+template <typename T, int TPR, int VPT, bool RAGGED>
 __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a) {
     constexpr int kRows = block_of<TPR>() / TPR;
-    __shared__ float lds[block_of<TPR>() / kWave];
+    __shared__ float lds[2][block_of<TPR>() / kWave];
     const int t = threadIdx.x % TPR;
     for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR; row < a.rows; row += int64_t(gridDim.x) * kRows) {
-        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+        RowOf<T, TPR, VPT, RAGGED> x, r;
+        x.load(static_cast<const T*>(a.x) + row * a.x_stride, t, a.width);
+        if (a.residual) r.load(static_cast<const T*>(a.residual) + row * a.residual_stride, t, a.width);
         float s[VPT][8];
         float square = 0.f;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int col = (j * TPR + t) * 8, left = a.width - col;
-            if (left > 0) {
-                Row8<T>::load(x + col, left, s[j]);
-            } else {
+            x.get(j, t, a.width, s[j]);
+            if (a.residual) {
+                float f[8];
+                r.get(j, t, a.width, f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[j][i] = 0.f;
+                for (int i = 0; i < 8; ++i) s[j][i] += f[i];
             }
-        }
-        if (a.residual) {
-            const T* r = static_cast<const T*>(a.residual) + row * a.residual_stride;
-#pragma unroll
-            for (int j = 0; j < VPT; ++j) {
-                const int col = (j * TPR + t) * 8, left = a.width - col;
-                if (left > 0) {
-                    float f[8];
-                    Row8<T>::load(r + col, left, f);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) s[j][i] += f[i];
-                }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < VPT; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) square = fmaf(s[j][i], s[j][i], square);
-        const float rstd = __frsqrt_rn(fmaf(row_sum<TPR>(square, lds), a.inv_width, a.eps));
+        }
+        const float rstd = __frsqrt_rn(fmaf(row_sum<TPR>(square, lds[0]), a.inv_width, a.eps));
         if (a.rstd && t == 0) a.rstd[row] = rstd;
         if (a.sum) {
             T* out = static_cast<T*>(a.sum) + row * a.sum_stride;
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
-                const int col = (j * TPR + t) * 8, left = a.width - col;
-                if (left > 0) Row8<T>::store(out + col, left, s[j]);
+                const int col = (j * TPR + t) * 8;
+                if (col < a.width) Row8<T>::store(out + col, RAGGED ? a.width - col : 8, s[j]);
             }
         }
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int col = (j * TPR + t) * 8, left = a.width - col;
-            if (left > 0) {
+            const int col = (j * TPR + t) * 8;
+            if (col < a.width) {
                 float w[8];
-                load_weight(a.weight, a.weight_bf16, col, left, w);
+                load_weight(a.weight, a.weight_bf16, col, RAGGED ? a.width - col : 8, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s[j][i] = s[j][i] * rstd * w[i];
             }
@@ -137,9 +159,10 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
             T* y = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
-                const int col = (j * TPR + t) * 8, left = a.width - col;
-                if (left > 0) Row8<T>::store(y + col, left, s[j]);
+                const int col = (j * TPR + t) * 8;
+                if (col < a.width) Row8<T>::store(y + col, RAGGED ? a.width - col : 8, s[j]);
             }
+            if (TPR > kWave) __syncthreads();       // (the sums have been read)
             continue;
         }
         float most[VPT], whole = 0.f;
@@ -151,7 +174,7 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
             whole = fmaxf(whole, most[j]);
         }
         if (a.group == 0) {
-            whole = row_max<TPR>(whole, lds);
+            whole = row_max<TPR>(whole, lds[1]);
 #pragma unroll
             for (int j = 0; j < VPT; ++j) most[j] = whole;
         } else {
@@ -168,8 +191,8 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
         float* scales = a.scales + row * a.groups;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int col = (j * TPR + t) * 8, left = a.width - col;
-            if (left <= 0) continue;
+            const int col = (j * TPR + t) * 8, left = RAGGED ? a.width - col : 8;
+            if (col >= a.width) continue;
             const float scale = e4m3_scale(most[j], a.pow2), inv = 1.f / scale;
             if (a.group == 0 ? col == 0 : col % a.group == 0) scales[a.group == 0 ? 0 : col / a.group] = scale;
             uint32_t q[2];
@@ -188,15 +211,17 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
                     if (i < left) y[col + i] = uint8_t(q[i / 4] >> (8 * (i % 4)));
             }
         }
+        if (TPR > kWave) __syncthreads();
     }
 }
 
-// dx of every row, and dweight as one partial sum for each of the gridDim.x * kRows row groups: a thread meets the same columns in every row,
-// so their sums stay in its registers.
-template <typename T, int TPR, int VPT>
+// dx of every row, and dweight as one partial sum for each block: a thread meets the same columns in every row,
+// so their sums stay in its registers.  The next row is asked for before the present one is worked on, where the registers hold both.
+template <typename T, int TPR, int VPT, bool RAGGED>
 __global__ void __launch_bounds__(block_of<TPR>()) rms_backward_kernel(RmsBackwardArgs a) {
     constexpr int kRows = block_of<TPR>() / TPR;
-    __shared__ float lds[block_of<TPR>() / kWave];
+    constexpr bool kAhead = TPR < 1024;
+    __shared__ float lds[2][block_of<TPR>() / kWave];
     const int t = threadIdx.x % TPR;
     const int64_t first = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR, step = int64_t(gridDim.x) * kRows;
     float dw[VPT][8];
@@ -204,75 +229,96 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_backward_kernel(RmsBackwa
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[j][i] = 0.f;
-    for (int64_t row = first; row < a.rows; row += step) {
-        const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-        const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
-        const float rstd = a.rstd[row];
+    RowOf<T, TPR, VPT, RAGGED> next_x, next_dy, next_ds;
+    float next_rstd = 0.f;
+    const auto ask = [&](int64_t row) {
+        next_rstd = a.rstd[row];
+        next_x.load(static_cast<const T*>(a.x) + row * a.x_stride, t, a.width);
+        next_dy.load(static_cast<const T*>(a.dy) + row * a.dy_stride, t, a.width);
+        if (a.dsum) next_ds.load(static_cast<const T*>(a.dsum) + row * a.dsum_stride, t, a.width);
+    };
+    if (kAhead && first < a.rows) ask(first);
+    int turn = 0;
+    for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
+        if (!kAhead) ask(row);
+        const RowOf<T, TPR, VPT, RAGGED> x = next_x, dy = next_dy, ds = next_ds;
+        const float rstd = next_rstd;
+        if (kAhead && row + step < a.rows) ask(row + step);
         float xh[VPT][8], g[VPT][8];
         float dot = 0.f;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int col = (j * TPR + t) * 8, left = a.width - col;
-            if (left > 0) {
-                Row8<T>::load(x + col, left, xh[j]);
-                Row8<T>::load(dy + col, left, g[j]);
-            } else {
+            const int col = (j * TPR + t) * 8;
+            x.get(j, t, a.width, xh[j]);
+            dy.get(j, t, a.width, g[j]);
+            float w[8];
+            if (RAGGED) {
+                if (col < a.width) {
+                    load_weight(a.weight, a.weight_bf16, col, a.width - col, w);
+                } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) xh[j][i] = g[j][i] = 0.f;
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int col = (j * TPR + t) * 8, left = a.width - col;
-            if (left > 0) {
-                float w[8];
-                load_weight(a.weight, a.weight_bf16, col, left, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    xh[j][i] *= rstd;
-                    dw[j][i] = fmaf(g[j][i], xh[j][i], dw[j][i]);
-                    g[j][i] *= w[i];
-                    dot = fmaf(g[j][i], xh[j][i], dot);
+                    for (int i = 0; i < 8; ++i) w[i] = 0.f;
                 }
+            } else {
+                load_weight(a.weight, a.weight_bf16, min(col, a.width - 8), 8, w);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                xh[j][i] *= rstd;
+                dw[j][i] = fmaf(g[j][i], xh[j][i], dw[j][i]);
+                g[j][i] *= w[i];
+                dot = fmaf(g[j][i], xh[j][i], dot);
             }
         }
-        const float mean = row_sum<TPR>(dot, lds) * a.inv_width;
+        const float mean = row_sum<TPR>(dot, lds[turn]) * a.inv_width;
         T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
-        const T* dsum = a.dsum ? static_cast<const T*>(a.dsum) + row * a.dsum_stride : nullptr;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int col = (j * TPR + t) * 8, left = a.width - col;
-            if (left <= 0) continue;
-            float f[8];
-            if (dsum) {
-                Row8<T>::load(dsum + col, left, f);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = 0.f;
-            }
+            const int col = (j * TPR + t) * 8;
+            if (col >= a.width) continue;
+            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (a.dsum) ds.get(j, t, a.width, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = fmaf(rstd, fmaf(-xh[j][i], mean, g[j][i]), f[i]);
-            Row8<T>::store(dx + col, left, f);
+            Row8<T>::store(dx + col, RAGGED ? a.width - col : 8, f);
         }
     }
-    if (first < step) {     // every row group has a place, whether it met a row or not
-        float* out = a.partial + first * a.width;
+    if constexpr (kRows > 1) {                      // the waves of a block add theirs up first
+        __shared__ float sums[kRows - 1][VPT * 8][TPR];
+        const int group = threadIdx.x / TPR;
+        if (group > 0) {
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int col = (j * TPR + t) * 8, left = a.width - col;
-            if (left > 0) Row8<float>::store(out + col, left, dw[j]);
+            for (int j = 0; j < VPT; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sums[group - 1][j * 8 + i][t] = dw[j][i];
         }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int k = 0; k < kRows - 1; ++k)
+#pragma unroll
+            for (int j = 0; j < VPT; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dw[j][i] += sums[k][j * 8 + i][t];
+    }
+    float* out = a.partial + int64_t(blockIdx.x) * a.width;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        const int col = (j * TPR + t) * 8;
+        if (col < a.width) Row8<float>::store(out + col, RAGGED ? a.width - col : 8, dw[j]);
     }
 }
 
-// Adds the partial sums of a column in a fixed order: 16 threads take every 16th of them, then one adds the 16.
-constexpr int kSumColumns = 64, kSumLanes = 16;
+// Adds the partial sums of a column in a fixed order: 32 threads take every 32nd of them, then one adds the 32.
+constexpr int kSumColumns = 32, kSumLanes = 32;
 __global__ void __launch_bounds__(kSumColumns * kSumLanes) column_sum_kernel(const float* partial, int count, int width, float* out) {
     __shared__ float lds[kSumLanes][kSumColumns];
     const int c = threadIdx.x % kSumColumns, l = threadIdx.x / kSumColumns, col = blockIdx.x * kSumColumns + c;
     float s = 0.f;
-    if (col < width)
+    if (col < width) {
+#pragma unroll 8
         for (int i = l; i < count; i += kSumLanes) s += partial[int64_t(i) * width + col];
+    }
     lds[l][c] = s;
     __syncthreads();
     if (l == 0 && col < width) {
@@ -285,7 +331,7 @@ __global__ void __launch_bounds__(kSumColumns * kSumLanes) column_sum_kernel(con
 struct RmsPlan {
     int tpr, vpt;
 };
-RmsPlan rms_plan(int64_t rows, int width) {
+RmsPlan forward_plan(int64_t rows, int width) {
     const int vectors = (width + 7) / 8;
     // Few rows leave compute units idle: as many threads as the row has vectors.  Many rows: a wave each as far as its registers go, which
     // needs no exchange through LDS.
@@ -297,24 +343,43 @@ RmsPlan rms_plan(int64_t rows, int width) {
     return {tpr, vpt};
 }
 
-// Row groups of the backward pass: enough to fill the device, each of which leaves a row of partial sums behind.
-constexpr int kMostGroups = 512;
-int64_t backward_groups(const RmsPlan& p, int64_t rows) {
-    const int per_block = p.tpr == kWave ? 4 : 1;
-    return round_up(std::min<int64_t>(std::max<int64_t>(rows, 1), p.tpr == kWave ? 2 * kMostGroups : kMostGroups), per_block);
+// The backward pass holds five values of an element where the forward pass holds two: two vectors per thread at most.
+RmsPlan backward_plan(int width) {
+    const int vectors = (width + 7) / 8;
+    const int tpr = vectors <= 128 ? 64 : vectors <= 512 ? 256 : vectors <= 1024 ? 512 : 1024;
+    return {tpr, tpr > 256 ? 2 : (vectors + tpr - 1) / tpr};
 }
 
-#define BNS_RMS_DISPATCH(T, KERNEL)                                              \
-    switch (p.tpr * 10 + p.vpt) {                                                \
-        case 641: BNS_LAUNCH((KERNEL<T, 64, 1>), grid, dim3(256), 0, st, a); break;     \
-        case 642: BNS_LAUNCH((KERNEL<T, 64, 2>), grid, dim3(256), 0, st, a); break;     \
-        case 644: BNS_LAUNCH((KERNEL<T, 64, 4>), grid, dim3(256), 0, st, a); break;     \
-        case 2561: BNS_LAUNCH((KERNEL<T, 256, 1>), grid, dim3(256), 0, st, a); break;   \
-        case 2562: BNS_LAUNCH((KERNEL<T, 256, 2>), grid, dim3(256), 0, st, a); break;   \
-        case 2563: BNS_LAUNCH((KERNEL<T, 256, 3>), grid, dim3(256), 0, st, a); break;   \
-        case 2564: BNS_LAUNCH((KERNEL<T, 256, 4>), grid, dim3(256), 0, st, a); break;   \
-        case 10241: BNS_LAUNCH((KERNEL<T, 1024, 1>), grid, dim3(1024), 0, st, a); break; \
-        default: BNS_LAUNCH((KERNEL<T, 512, 4>), grid, dim3(512), 0, st, a); break;     \
+// Blocks of the backward pass: enough to fill the device, each of which leaves a row of partial sums behind.
+int64_t backward_blocks(const RmsPlan& p, int64_t rows) {
+    const int per_block = p.tpr == kWave ? 4 : 1;
+    return std::min<int64_t>(std::max<int64_t>((rows + per_block - 1) / per_block, 1), 512);
+}
+
+#define BNS_RMS_CASE(T, KERNEL, TPR, VPT, THREADS)                                                                    \
+    if (a.width % 8) BNS_LAUNCH((KERNEL<T, TPR, VPT, true>), grid, dim3(THREADS), 0, st, a);                          \
+    else BNS_LAUNCH((KERNEL<T, TPR, VPT, false>), grid, dim3(THREADS), 0, st, a);                                     \
+    break;
+#define BNS_RMS_FORWARD(T)                                              \
+    switch (p.tpr * 10 + p.vpt) {                                       \
+        case 641: BNS_RMS_CASE(T, rms_forward_kernel, 64, 1, 256)       \
+        case 642: BNS_RMS_CASE(T, rms_forward_kernel, 64, 2, 256)       \
+        case 644: BNS_RMS_CASE(T, rms_forward_kernel, 64, 4, 256)       \
+        case 2561: BNS_RMS_CASE(T, rms_forward_kernel, 256, 1, 256)     \
+        case 2562: BNS_RMS_CASE(T, rms_forward_kernel, 256, 2, 256)     \
+        case 2563: BNS_RMS_CASE(T, rms_forward_kernel, 256, 3, 256)     \
+        case 2564: BNS_RMS_CASE(T, rms_forward_kernel, 256, 4, 256)     \
+        case 10241: BNS_RMS_CASE(T, rms_forward_kernel, 1024, 1, 1024)  \
+        default: BNS_RMS_CASE(T, rms_forward_kernel, 512, 4, 512)       \
+    }
+#define BNS_RMS_BACKWARD(T)                                             \
+    switch (p.tpr * 10 + p.vpt) {                                       \
+        case 641: BNS_RMS_CASE(T, rms_backward_kernel, 64, 1, 256)      \
+        case 642: BNS_RMS_CASE(T, rms_backward_kernel, 64, 2, 256)      \
+        case 2561: BNS_RMS_CASE(T, rms_backward_kernel, 256, 1, 256)    \
+        case 2562: BNS_RMS_CASE(T, rms_backward_kernel, 256, 2, 256)    \
+        case 5122: BNS_RMS_CASE(T, rms_backward_kernel, 512, 2, 512)    \
+        default: BNS_RMS_CASE(T, rms_backward_kernel, 1024, 2, 1024)    \
     }
 
 constexpr int64_t kMostBlocks = int64_t(1) << 20;      // (a launch holds fewer than 2^32 threads; rows beyond are taken in turn)
@@ -343,14 +408,14 @@ bns_status bns_rms_forward(const bns_rms* rms, const void* x, const void* residu
         return BNS_EINVAL;
     const RmsArgs a = {x, residual, weight, sum, y, scales, rstd, d.rows, d.x_stride, d.residual_stride, d.sum_stride, d.y_stride,
                        d.width, d.groups, rms->group, rms->weight_dtype == BNS_BF16, e4m3, rms->pow2_scales, rms->eps, 1.f / float(d.width)};
-    const RmsPlan p = rms_plan(d.rows, d.width);
+    const RmsPlan p = forward_plan(d.rows, d.width);
     const int per_block = p.tpr == kWave ? 4 : 1;
     const dim3 grid(uint32_t(std::min<int64_t>((d.rows + per_block - 1) / per_block, kMostBlocks)));
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (rms->dtype == BNS_F32) {
-        BNS_RMS_DISPATCH(float, rms_forward_kernel)
+        BNS_RMS_FORWARD(float)
     } else {
-        BNS_RMS_DISPATCH(bf16_t, rms_forward_kernel)
+        BNS_RMS_FORWARD(bf16_t)
     }
     return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
 }
@@ -358,7 +423,7 @@ bns_status bns_rms_forward(const bns_rms* rms, const void* x, const void* residu
 size_t bns_rms_workspace_bytes(const bns_rms* rms) {
     RmsDims d;
     if (check_rms(rms, &d) != BNS_OK) return 0;
-    return size_t(round_up(backward_groups(rms_plan(d.rows, d.width), d.rows) * d.width * 4, 256));
+    return size_t(round_up(backward_blocks(backward_plan(d.width), d.rows) * d.width * 4, 256));
 }
 
 bns_status bns_rms_backward(const bns_rms* rms, const void* x, const void* weight, const float* rstd, const void* dy, const void* dsum, void* dx,
@@ -376,18 +441,18 @@ bns_status bns_rms_backward(const bns_rms* rms, const void* x, const void* weigh
     if (workspace_bytes < bns_rms_workspace_bytes(rms)) return BNS_EWORKSPACE;
     const RmsBackwardArgs a = {x, weight, dy, dsum, rstd, dx, static_cast<float*>(workspace), d.rows, d.x_stride, d.residual_stride, d.sum_stride,
                                d.y_stride, d.width, rms->weight_dtype == BNS_BF16, 1.f / float(d.width)};
-    const RmsPlan p = rms_plan(d.rows, d.width);
-    const int64_t groups = backward_groups(p, d.rows);
-    const dim3 grid(uint32_t(groups / (p.tpr == kWave ? 4 : 1)));
+    const RmsPlan p = backward_plan(d.width);
+    const int64_t blocks = backward_blocks(p, d.rows);
+    const dim3 grid{uint32_t(blocks)};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (rms->dtype == BNS_F32) {
-        BNS_RMS_DISPATCH(float, rms_backward_kernel)
+        BNS_RMS_BACKWARD(float)
     } else {
-        BNS_RMS_DISPATCH(bf16_t, rms_backward_kernel)
+        BNS_RMS_BACKWARD(bf16_t)
     }
     if (hipGetLastError() != hipSuccess) return BNS_EDEVICE;
     BNS_LAUNCH(column_sum_kernel, dim3((d.width + kSumColumns - 1) / kSumColumns), dim3(kSumColumns * kSumLanes), 0, st,
-               static_cast<const float*>(workspace), int(groups), d.width, dweight);
+               static_cast<const float*>(workspace), int(blocks), d.width, dweight);
     return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
 }
 

@@ -14,6 +14,19 @@ from paper_1810_10962_amd import bns
 pytestmark = pytest.mark.gpu
 
 
+# How the operands are read: as they lie in memory (tiles by size, or of 128), or laid out first; see "head_path" and "head_tile".
+PATHS = {"direct": (1, 0), "direct128": (1, 128), "laid_out": (2, 0), "auto": (0, 0)}
+
+
+@pytest.fixture(params=PATHS)
+def path(request):
+    for name, value in zip(("head_path", "head_tile"), PATHS[request.param]):
+        bns.bns_set_option(name, value)
+    yield request.param
+    bns.bns_set_option("head_path", 0)
+    bns.bns_set_option("head_tile", 0)
+
+
 def make(tokens, width, vocab, dtype, seed=0, ignored=0.2):
     g = torch.Generator().manual_seed(seed * 7919 + tokens * 31 + width * 7 + vocab)
     rnd = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
@@ -74,14 +87,14 @@ def run(hidden, weight, targets, dloss, dtype, pad=0, piece=0):
 
 
 SHAPES = [(1, 1, 1), (1, 64, 2), (3, 8, 257), (5, 100, 1000), (16, 128, 300), (64, 192, 513), (65, 64, 256), (130, 200, 255), (257, 320, 1030), (300, 77, 700), (40, 1000, 5003),
-          (511, 512, 2049)]
+          (511, 512, 2049), (30, 72, 1500)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("tokens,width,vocab", SHAPES)
-def test_loss_and_gradients(tokens, width, vocab, dtype):
+def test_loss_and_gradients(tokens, width, vocab, dtype, path):
     for pad, piece in [(0, 0), (3, 256), (8, 512)]:
-        print(f"[gpu-case] head {tokens}x{width}x{vocab} {dtype} pad={pad} piece={piece}", flush=True)
+        print(f"[gpu-case] head {tokens}x{width}x{vocab} {dtype} {path} pad={pad} piece={piece}", flush=True)
         hidden, weight, targets, dloss = make(tokens, width, vocab, dtype)
         loss, lse, dh, dw = run(hidden, weight, targets, dloss, dtype, pad, piece)
         check_forward(loss, lse, hidden, weight, targets, dtype)
@@ -90,7 +103,7 @@ def test_loss_and_gradients(tokens, width, vocab, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("tokens", [7, 100])
-def test_tokens_that_are_left_out_may_hold_anything(tokens, dtype):
+def test_tokens_that_are_left_out_may_hold_anything(tokens, dtype, path):
     hidden, weight, targets, dloss = make(tokens, 128, 600, dtype, seed=1, ignored=0.4)
     out = (targets < 0) | (targets >= 600)
     assert bool(out.any()) and not bool(out.all())
@@ -106,7 +119,7 @@ def test_tokens_that_are_left_out_may_hold_anything(tokens, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_no_token_is_kept_or_there(dtype):
+def test_no_token_is_kept_or_there(dtype, path):
     print(f"[gpu-case] head without tokens {dtype}", flush=True)
     hidden, weight, targets, dloss = make(9, 64, 300, dtype, ignored=1.1)
     loss, lse, dh, dw = run(hidden, weight, targets, dloss, dtype)
@@ -121,7 +134,7 @@ def test_no_token_is_kept_or_there(dtype):
     assert bool((dw.check() == 0).all())
 
 
-def test_large_logits_and_a_sure_model():
+def test_large_logits_and_a_sure_model(path):
     """Logits of a few hundred, all probability on the target: a loss of zero, not of NaN, and gradients that vanish."""
     tokens, width, vocab = 64, 64, 700
     weight = torch.zeros(vocab, width)
@@ -137,7 +150,7 @@ def test_large_logits_and_a_sure_model():
         assert float(dh.float().abs().max()) < 1e-3 and float(dw.float().abs().max()) < 1e-3
 
 
-def test_same_bits_from_run_to_run_and_in_a_graph():
+def test_same_bits_from_run_to_run_and_in_a_graph(path):
     hidden, weight, targets, dloss = make(200, 256, 3000, "bf16", seed=5)
     head = bns.make_head(200, 256, 3000, "bf16", piece=1024)
     h, w, t, d = hidden.cuda(), weight.cuda(), targets.cuda(), dloss.cuda()
