@@ -91,8 +91,9 @@ const TuningEntry kTuningTable[] = {
     {"nhwc_split_ordered", &Tuning::nhwc_split_ordered, 2, 0, false},
     {"nhwc_split_dx", &Tuning::nhwc_split_dx, 2, 0, false},
     {"cache_reuse", &Tuning::cache_reuse, 2, 0, false},
-    {"head_path", &Tuning::head_path, 2, 0, false},
-    {"head_tile", &Tuning::head_tile, 128, 0, false},
+    {"head_logits", &Tuning::head_logits, 5, 0, false},
+    {"head_logits_backward", &Tuning::head_logits_backward, 5, 0, false},
+    {"head_gradients", &Tuning::head_gradients, 5, 0, false},
 };
 
 int stats_splits(const Dims& d, const IndexParams& ip, int cg) {

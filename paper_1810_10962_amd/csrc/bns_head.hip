@@ -1,195 +1,22 @@
 // Softmax cross entropy from hidden states and the vocabulary's matrix, without keeping the logits, and its gradients.  See include/bns.h.
 //
 // Three matrix products: the logits (weight hidden^T, computed in the forward pass and again in the backward pass), dhidden = g weight and
-// dweight = g^T hidden.  All of them are one kernel: C[m][n] = sum over k of A[m][k] B[n][k] with both operands k-contiguous bf16, tiles
-// staged through LDS, fp32 sums on the matrix units, and an epilogue that turns a tile of logits into softmax statistics or into g.  What is not
-// k-contiguous bf16 (fp32 operands, which become three bf16 parts; widths and strides that are no multiple of the tile; the
-// transposes that the gradients need) is laid out in the workspace first, piece by piece of the vocabulary.
+// dweight = g^T hidden.  C[m][n] = sum over k of A[m][k] B[n][k] on the matrix units, bf16 operands (fp32 values as three bf16 parts) and fp32
+// sums, with an epilogue that turns a tile of logits into softmax statistics or into g.  Three families of kernels, see the plan below:
+// few tokens (bns_head_stream.hpp), operands as they lie in memory (bns_head_direct.hpp), operands laid out first (bns_head_laid_out.hpp).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 
-#include "bns_internal.hpp"
-#include "bns_head_device.hpp"
 #include "bns_head_direct.hpp"
+#include "bns_head_laid_out.hpp"
+#include "bns_head_stream.hpp"
+#include "bns_internal.hpp"
 #include "bns_lm_validate.hpp"
 
 using namespace bns;
 
 namespace {
-
-constexpr int kDepth = 64;      // elements of k in a staged tile: 128 bytes a row
-
-// ---- laying operands out ------------------------------------------------------------------------------------------
-struct PackArgs {
-    const void* src;
-    uint16_t* dst;
-    const int64_t* targets;     // rows whose target lies outside [0, vocab) count as zeros; NULL: none do
-    int64_t src_stride;
-    int32_t rows, cols;         // of src
-    int32_t depth;              // elements of k in a plane of dst, padded with zeros; a row of dst holds its planes one behind the other
-    int32_t vocab;
-};
-
-// Row r of src becomes row r of dst (k = the column).
-template <typename T>
-__global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) {
-    constexpr int P = planes_of<T>();
-    const int per_row = a.depth / 8;
-    const int64_t total = int64_t(a.rows) * per_row;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-        const int64_t row = i / per_row;
-        const int col = int(i - row * per_row) * 8, left = a.cols - col;
-        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (left > 0) Row8<T>::load(static_cast<const T*>(a.src) + row * a.src_stride + col, left, f);
-        uint16_t* out = a.dst + row * a.depth * P + col;
-        if (P == 1) {
-            *reinterpret_cast<u4*>(out) = u4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-        } else {
-            u4 w[3];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t lo[3], hi[3];
-                split3(f[2 * j], lo);
-                split3(f[2 * j + 1], hi);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) w[p][j] = lo[p] | hi[p] << 16;
-            }
-#pragma unroll
-            for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(out + int64_t(p) * a.depth) = w[p];
-        }
-    }
-}
-
-// Column c of src becomes row c of dst (k = the row), in tiles of 64 x 64 through LDS.
-template <typename T>
-__global__ void __launch_bounds__(256) pack_columns_kernel(PackArgs a) {
-    constexpr int P = planes_of<T>();
-    __shared__ float tile[64][65];
-    const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int r = int(threadIdx.x) / 8 + 32 * j, c = int(threadIdx.x) % 8 * 8, row = r0 + r, left = a.cols - (c0 + c);
-        float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        bool in = row < a.rows && left > 0;
-        if (in && a.targets) {
-            const int64_t target = a.targets[row];
-            in = target >= 0 && target < a.vocab;
-        }
-        if (in) Row8<T>::load(static_cast<const T*>(a.src) + int64_t(row) * a.src_stride + c0 + c, left, f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) tile[r][c + i] = f[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = int(threadIdx.x) / 8 + 32 * j, r = int(threadIdx.x) % 8 * 8;
-        if (c0 + c >= a.cols) continue;
-        uint16_t* out = a.dst + int64_t(c0 + c) * a.depth * P + r0 + r;
-        if (P == 1) {
-            u4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(tile[r + 2 * i][c], tile[r + 2 * i + 1][c]);
-            *reinterpret_cast<u4*>(out) = w;
-        } else {
-            u4 w[3];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t lo[3], hi[3];
-                split3(tile[r + 2 * i][c], lo);
-                split3(tile[r + 2 * i + 1][c], hi);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) w[p][i] = lo[p] | hi[p] << 16;
-            }
-#pragma unroll
-            for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(out + int64_t(p) * a.depth) = w[p];
-        }
-    }
-}
-
-// ---- the product --------------------------------------------------------------------------------------------------
-// Operands that are k-contiguous bf16 in memory (in three planes, where they are the parts of fp32 values): a row beyond the last is read as the last.
-template <int BM, int BN, int WM, int WN>
-struct Tile {
-    static constexpr int kThreads = WM * WN * kWave, kPerIssue = kThreads / 8;       // rows that all threads bring in at once
-    static constexpr int kM = BM / WM, kN = BN / WN, MI = kM / 16, NI = kN / 16;
-    static constexpr int kBytes = (BM + BN) * kDepth * 2;
-    static_assert(BM % kPerIssue == 0 && BN % kPerIssue == 0, "whole issues");
-};
-
-template <typename T, int BM, int BN, int WM, int WN, int EPILOGUE>
-__global__ void __launch_bounds__(WM* WN* kWave) gemm_kernel(GemmArgs a) {
-#ifdef __HIP_DEVICE_COMPILE__   // (the host compiler has no buffer resources)
-    using S = Tile<BM, BN, WM, WN>;
-    constexpr int P = planes_of<T>(), kSegments = P == 1 ? 1 : 6;
-    __shared__ __attribute__((aligned(1024))) char lds[2][S::kBytes];
-    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave), lane = threadIdx.x % kWave;
-    const int tiles = a.tiles_a * a.tiles_b, split = int(blockIdx.x) / tiles;
-    int ta, tb;
-    place(int(blockIdx.x) - split * tiles, tiles, a.tiles_a, a.tiles_b, ta, tb);
-    const int m0 = ta * BM, n0 = tb * BN;
-
-    // Staging: a wave brings in eight rows of 128 bytes with one instruction, which puts lane after lane into LDS; the 16-byte chunks of row r
-    // are swapped by r on their way (chunk c lies at c ^ (r % 8)), so that the reads of 16 rows at one chunk spread over the banks.
-    const int last_a = a.rows_a - 1 - m0, last_b = a.rows_b - 1 - n0;
-    const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(a.a) + int64_t(m0) * a.lda * 2), 0, -1, 0x00027000);
-    const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(a.b) + int64_t(n0) * a.ldb * 2), 0, -1, 0x00027000);
-    uint32_t at_a[BM / S::kPerIssue], at_b[BN / S::kPerIssue];
-    const int in_row = lane / 8, chunk = (lane % 8) ^ in_row;
-#pragma unroll
-    for (int i = 0; i < BM / S::kPerIssue; ++i) at_a[i] = uint32_t(min(i * S::kPerIssue + wave * 8 + in_row, last_a)) * uint32_t(a.lda) * 2 + chunk * 16;
-#pragma unroll
-    for (int i = 0; i < BN / S::kPerIssue; ++i) at_b[i] = uint32_t(min(i * S::kPerIssue + wave * 8 + in_row, last_b)) * uint32_t(a.ldb) * 2 + chunk * 16;
-
-    const int per_plane = a.depth / kDepth, steps = per_plane * kSegments;
-    const int first = int(int64_t(steps) * split / a.splits), end = int(int64_t(steps) * (split + 1) / a.splits);
-    typedef __attribute__((address_space(3))) void lds_t;
-    const auto stage = [&](int step, char* to) {
-        int ka = step, kb = step;
-        if (kSegments > 1) {
-            const int segment = step / per_plane, k = step - segment * per_plane;
-            ka = plane_a(segment) * per_plane + k;
-            kb = plane_b(segment) * per_plane + k;
-        }
-#pragma unroll
-        for (int i = 0; i < BM / S::kPerIssue; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_t*)(to + (i * S::kPerIssue + wave * 8) * 128), 16, at_a[i], ka * 128, 0, 0);
-#pragma unroll
-        for (int i = 0; i < BN / S::kPerIssue; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_t*)(to + (BM + i * S::kPerIssue + wave * 8) * 128), 16, at_b[i], kb * 128, 0, 0);
-    };
-
-    const int wm = wave / WN, wn = wave % WN, r16 = lane % 16, quarter = lane / 16;
-    f32x4 acc[S::MI][S::NI];
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-        for (int j = 0; j < S::NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    if (first < end) stage(first, lds[0]);
-    for (int step = first; step < end; ++step) {
-        // the tile of this step has landed, and every wave is done with the one before
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        char* const now = lds[(step - first) & 1];
-        if (step + 1 < end) stage(step + 1, lds[(step + 1 - first) & 1]);
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            bf16x8 fa[S::MI], fb[S::NI];
-            const int at = ((kk * 4 + quarter) ^ (r16 % 8)) * 16;
-#pragma unroll
-            for (int j = 0; j < S::NI; ++j) fb[j] = *reinterpret_cast<const bf16x8*>(now + (BM + wn * S::kN + j * 16 + r16) * 128 + at);
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i) fa[i] = *reinterpret_cast<const bf16x8*>(now + (wm * S::kM + i * 16 + r16) * 128 + at);
-#pragma unroll
-            for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-                for (int j = 0; j < S::NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        }
-    }
-
-    finish<T, EPILOGUE, BM, BN, WM, WN>(a, acc, ta, tb, split, reinterpret_cast<float2*>(lds));
-#endif
-}
 
 template <typename T, int BM, int BN, int WM, int WN, int EPILOGUE>
 __global__ void __launch_bounds__(WM* WN* kWave) direct_logits_kernel(GemmArgs a) {
@@ -207,14 +34,17 @@ __global__ void __launch_bounds__(256) direct_gradients_kernel(GemmArgs h, GemmA
 }
 
 // ---- what follows the products --------------------------------------------------------------------------------------
-// loss and lse from the statistics of the tiles: 16 tokens a block, 16 threads each.
+// loss and lse from the statistics of the tiles: TOKENS tokens a block, 256 / TOKENS threads each (few tokens have many tiles each and need them all).
+template <int TOKENS>
 __global__ void __launch_bounds__(256) join_statistics_kernel(const float2* partial, const float* at_target, const int64_t* targets, int tiles, int tokens, int vocab,
                                                                float* loss, float* lse) {
-    __shared__ float2 part[16][17];
-    const int c = threadIdx.x % 16, lane = threadIdx.x / 16, token = blockIdx.x * 16 + c;
+    constexpr int kLanes = 256 / TOKENS;
+    __shared__ float2 part[kLanes][TOKENS];
+    const int c = threadIdx.x % TOKENS, lane = threadIdx.x / TOKENS, token = blockIdx.x * TOKENS + c;
     float m = -3e38f, l = 0.f;
     if (token < tokens) {
-        for (int i = lane; i < tiles; i += 16) {
+#pragma unroll 4
+        for (int i = lane; i < tiles; i += kLanes) {
             const float2 p = partial[int64_t(i) * tokens + token];
             const float most = fmaxf(m, p.x);
             l = l * __builtin_amdgcn_exp2f(m - most) + p.y * __builtin_amdgcn_exp2f(p.x - most);
@@ -222,33 +52,55 @@ __global__ void __launch_bounds__(256) join_statistics_kernel(const float2* part
         }
     }
     part[lane][c] = float2{m, l};
-    __syncthreads();
+    for (int half = kLanes / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (lane >= half) continue;
+        const float2 p = part[lane + half][c];
+        const float most = fmaxf(m, p.x);
+        l = l * __builtin_amdgcn_exp2f(m - most) + p.y * __builtin_amdgcn_exp2f(p.x - most);
+        m = most;
+        part[lane][c] = float2{m, l};
+    }
     if (lane != 0 || token >= tokens) return;
-    for (int i = 1; i < 16; ++i) m = fmaxf(m, part[i][c].x);
-    l = 0.f;
-    for (int i = 0; i < 16; ++i) l = fmaf(part[i][c].y, __builtin_amdgcn_exp2f(part[i][c].x - m), l);
     const float all = (m + __builtin_amdgcn_logf(l)) * kLn2;
     const int64_t target = targets[token];
     lse[token] = all;
     loss[token] = target >= 0 && target < vocab ? all - at_target[token] : 0.f;
 }
 
-// dhidden from the sums that the splits left behind.
-template <typename T>
-__global__ void __launch_bounds__(256) join_splits_kernel(const float* part, int64_t split_stride, int splits, int tokens, int width, int ld, T* out) {
-    const int per_row = (width + 7) / 8;
-    const int64_t total = int64_t(tokens) * per_row;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-        const int64_t row = i / per_row;
-        const int col = int(i - row * per_row) * 8;
-        float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < splits; ++k) {
-            const f32x4* p = reinterpret_cast<const f32x4*>(part + k * split_stride + row * ld + col);
-            const f32x4 x = p[0], y = p[1];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] += x[e], s[4 + e] += y[e];
+// dhidden from the sums that the splits left behind: 8 columns x 32 a block and row, LANES threads each take every LANES-th split.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(32 * LANES) join_splits_kernel(const float* part, int64_t split_stride, int splits, int tokens, int width, int64_t ld, T* out) {
+    __shared__ f32x4 sums[LANES > 1 ? LANES - 1 : 1][2][32];
+    const int c = threadIdx.x % 32, lane = threadIdx.x / 32, per_row = (width + 255) / 256;
+    for (int64_t b = blockIdx.x; b < int64_t(tokens) * per_row; b += gridDim.x) {
+        const int64_t row = b / per_row;
+        const int col = (int(b - row * per_row) * 32 + c) * 8;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+        if (col < width) {
+#pragma unroll 4
+            for (int k = lane; k < splits; k += LANES) {
+                const f32x4* p = reinterpret_cast<const f32x4*>(part + k * split_stride + row * ld + col);
+                x += p[0];
+                y += p[1];
+            }
         }
-        Row8<T>::store(out + row * width + col, width - col, s);
+        if constexpr (LANES > 1) {
+            __syncthreads();
+            if (lane > 0) {
+                sums[lane - 1][0][c] = x;
+                sums[lane - 1][1][c] = y;
+            }
+            __syncthreads();
+            if (lane > 0) continue;
+#pragma unroll
+            for (int k = 0; k < LANES - 1; ++k) {
+                x += sums[k][0][c];
+                y += sums[k][1][c];
+            }
+        }
+        const float f[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        if (col < width) Row8<T>::store(out + row * width + col, width - col, f);
     }
 }
 
@@ -257,97 +109,138 @@ __global__ void __launch_bounds__(256) fill_zero_kernel(uint16_t* p, int64_t n) 
 }
 
 // ---- the plan -------------------------------------------------------------------------------------------------------
-constexpr int kTileM = 256;
+// Kernels of a product.
+enum Kind { kStream = 1, kDirect64, kDirect128, kGemm256, kGemm128 };
+
+inline int rows_of(Kind kind, const HeadDims& d) {      // rows of the vocabulary in a tile of logits
+    switch (kind) {
+        case kStream: return d.vocab < 16384 ? 16 : 32;  // (a small vocabulary needs the blocks)
+        case kDirect64: return 64;
+        case kGemm256: return 256;
+        default: return 128;
+    }
+}
 
 struct HeadPlan {
-    bool direct;                            // operands are read as they lie in memory
-    int tile;                               // direct: tokens of a tile, 16, 32, 64 or 128
-    int64_t piece;                          // rows of a piece of the vocabulary
-    int splits;                             // of dhidden
-    // laid out:
+    Kind kind;                              // of the logits
+    Kind gradients;
     int planes;
+    int64_t piece;                          // rows of a piece of the vocabulary
     int64_t depth_d, depth_t;               // padded width, tokens
-    bool direct_h, direct_w;                // read where they are, without a copy
-    bool narrow;                            // few tokens: tiles of 64 of them
+    int splits, splits_w;                   // of dhidden; of dweight's rows (kStream)
+    bool copy_h, copy_w;                    // the laid-out logits need copies of hidden, weight
     // offsets into the workspace
-    size_t hidden, weight, partial, at_target, weight_t, hidden_t, g, gt, sums, forward_bytes, backward_bytes;
+    size_t hidden, weight, partial, at_target, weight_t, hidden_t, g, gt, sums, bytes;
+
+    bool parts() const { return gradients == kStream || gradients >= kGemm256; }     // g as kGradientParts
 };
 
-struct Offsets {
+inline int tiles_of(int64_t rows, int tile) { return int((rows + tile - 1) / tile); }
+
+// Whether the laid-out kernels read an operand where it is.
+inline bool lies_well(const HeadDims& d, int64_t stride) { return d.dtype == BNS_BF16 && d.width % kDepth == 0 && stride % 8 == 0 && stride < (1 << 21); }
+
+// Times below: tokens x width x vocabulary, forward pass in us (best alternative behind "against").
+inline Kind logits_kind(const HeadDims& d, bool backward) {
+    const int chosen = backward ? g_tuning.head_logits_backward : g_tuning.head_logits;
+    if (chosen) return Kind(chosen);
+    const bool f32 = d.dtype == BNS_F32;
+    const auto tiles = [&](int tile) { return int64_t(tiles_of(d.tokens, tile)) * tiles_of(d.vocab, tile); };
+    // Fewer tiles of 64 than compute units: what counts is how long a block takes along the width, which kStream divides between its waves (fp32
+    // 9x1792x1071 18 against 53, 226x1728x1148 46 against 66; bf16 11 against 16, but 26 against 20).
+    if (tiles(64) < 128 && d.width >= 512 && (f32 || d.tokens <= 64)) return kStream;
+    const bool well = lies_well(d, d.hidden_stride) && lies_well(d, d.weight_stride);
+    // Tiles of 256 need two rounds of blocks (bf16 4096x4096x16384 411 against 472, 1021x1000x32003 95 against 108; fp32 364 against 418), tokens that fill
+    // them, and copies tokens that read them often (fp32 256x4096x32000 1447 against 438).
+    if (tiles(256) >= 400 && d.tokens > (well ? 192 : 1000)) return kGemm256;
+    // Without copies the laid-out kernels win as soon as they have the blocks (1024x1024x8192 25 against 30; 226x1728x1148 23 against 20).
+    if (well && d.tokens > 32 && tiles(128) >= 128) return kGemm128;
+    // fp32 256x512x32000 60 against 89, 1663x128x1920 19 against 18
+    return d.tokens > 64 && tiles(128) >= 256 ? kDirect128 : kDirect64;
+}
+
+// Times: whole backward pass, in us.
+inline Kind gradients_kind(const HeadDims& d) {
+    const int chosen = g_tuning.head_gradients;
+    const bool f32 = d.dtype == BNS_F32;
+    const bool few = d.tokens <= (f32 ? 32 : 64);        // what kStream holds in registers
+    if (chosen && (chosen != kStream || few)) return Kind(chosen);
+    const int64_t matrix = int64_t(d.width) * d.vocab;
+    // bf16 16x2048x50257 135 against 178, 2x384x85765 48 against 64, 40x1024x4096 29 against 24; fp32 1x3520x87977 999 against 1085, 16x2048x50257 400 against 393
+    if (few && matrix >= (int64_t(1) << (f32 ? 27 : 23))) return kStream;
+    const double work = double(matrix) * double(d.tokens);
+    // Laying operands out pays where each of them is read many times: bf16 512x2048x8192 99 against 120, 256x4096x32000 492 against 397; fp32
+    // 1021x1000x32003 1243 against 1444, 1024x1024x8192 344 against 341.
+    if (d.tokens >= 512 && work >= (f32 ? 3e10 : 5e9)) return d.tokens >= (f32 ? 1000 : 2048) && d.width >= (f32 ? 1000 : 2048) ? kGemm256 : kGemm128;
+    // bf16 256x4096x32000 397 against 446, 256x512x32000 86 against 77; fp32 40x1024x4096 41 against 51, 9x1792x1071 35 against 30, 1663x128x1920 152 against 130
+    if (f32 ? d.width >= 192 && matrix >= (int64_t(1) << 21) : work >= 1.5e10) return kDirect128;
+    return kDirect64;
+}
+
+HeadPlan head_plan(const HeadDims& d, bool backward) {
+    HeadPlan p = {};
+    const size_t e = dtype_bytes(d.dtype), T = size_t(d.tokens);
+    const bool f32 = d.dtype == BNS_F32;
+    p.kind = logits_kind(d, backward);
+    p.gradients = gradients_kind(d);
+    // (the laid-out kernels leave g in parts only, which is not what the direct ones read)
+    if (backward && !p.parts() && p.kind >= kGemm256) p.kind = kDirect128;
+    p.planes = f32 ? 3 : 1;
+    p.depth_d = round_up(d.width, kDepth);
+    p.depth_t = p.gradients == kStream && d.tokens <= 32 ? 32 : round_up(std::max<int64_t>(d.tokens, 1), kDepth);
+    const size_t P = size_t(p.planes) * 2;
+    if (p.kind >= kGemm256) {
+        p.copy_h = !lies_well(d, d.hidden_stride);
+        p.copy_w = !lies_well(d, d.weight_stride);
+    }
+    // The larger the piece, the fewer passes over dhidden's sums; 16384 rows where operands are laid out, else what keeps g at 64 MB.
+    int64_t piece = d.piece;
+    if (!piece) piece = p.gradients >= kGemm256 || p.copy_w ? 16384 : std::max<int64_t>(1024, (int64_t(64) << 20) / int64_t(std::max<size_t>(T * e, 1)));
+    p.piece = std::min(round_up(std::min<int64_t>(piece, 1 << 18), 256), round_up(d.vocab, 256));
+    const int64_t rows = std::min<int64_t>(p.piece, d.vocab);
     size_t at = 0;
-    size_t take(size_t bytes) {
+    const auto take = [&](size_t bytes) {
         const size_t here = at;
         at += (bytes + 1023) & ~size_t(1023);
         return here;
+    };
+    p.hidden = take(p.copy_h ? T * p.depth_d * P : 0);
+    p.weight = take(p.copy_w ? size_t(p.piece) * p.depth_d * P : 0);
+    if (!backward) {
+        const int m = rows_of(p.kind, d);
+        p.partial = take(size_t((d.vocab + m - 1) / m) * T * sizeof(float2));
+        p.at_target = take(T * 4);
+    } else {
+        p.splits = p.splits_w = 1;
+        if (p.gradients == kStream) {
+            // blocks for half of the device's waves, each with eight steps for its waves at least
+            const int64_t groups = (d.width + kStreamColumns - 1) / kStreamColumns;
+            p.splits = int(std::max<int64_t>(1, std::min<int64_t>(1024 / groups, rows / 256)));
+            p.splits_w = int(std::max<int64_t>(1, std::min<int64_t>(1024 / groups, rows / 128)));
+        } else if (p.gradients <= kDirect128) {
+            const int m = p.gradients == kDirect128 ? 128 : 64;
+            const int64_t tiles = ((d.width + m - 1) / m) * ((d.tokens + m - 1) / m), steps = rows / (f32 ? 32 : 64);
+            p.splits = int(std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(tiles, 1), steps / 4)));
+        } else {
+            const int m = p.gradients == kGemm128 ? 128 : 256;
+            const int64_t tiles = ((d.width + m - 1) / m) * ((d.tokens + m - 1) / m);
+            p.splits = int(std::max<int64_t>(1, std::min<int64_t>((m == 128 ? 512 : 256) / std::max<int64_t>(tiles, 1), rows / 512)));
+        }
+        if (p.gradients >= kGemm256) {
+            p.weight_t = take(size_t(d.width) * p.piece * P);
+            p.hidden_t = take(size_t(d.width) * p.depth_t * P);
+        }
+        p.g = take(T * p.piece * (p.parts() ? P : e));
+        if (p.parts()) p.gt = take(size_t(p.piece) * p.depth_t * P);
+        p.sums = take(size_t(p.splits) * T * p.depth_d * 4);
     }
-};
-
-HeadPlan direct_plan(const HeadDims& d) {
-    HeadPlan p = {};
-    const size_t e = dtype_bytes(d.dtype), T = size_t(d.tokens);
-    p.direct = true;
-    p.tile = d.tokens <= 16 ? 16 : d.tokens <= 32 ? 32 : 64;
-    if (g_tuning.head_tile == 128) p.tile = 128;
-    p.depth_d = round_up(d.width, 8);
-    // g of a piece takes 64 MB at most
-    const int64_t piece = d.piece ? d.piece : std::max<int64_t>(1024, (int64_t(64) << 20) / int64_t(std::max<size_t>(T * e, 1)));
-    p.piece = std::min(round_up(std::min<int64_t>(piece, 1 << 19), kTileM), round_up(d.vocab, kTileM));
-    const int m = p.tile == 128 ? 128 : 64;
-    const int64_t tiles = ((d.width + m - 1) / m) * ((d.tokens + p.tile - 1) / p.tile), steps = std::min<int64_t>(p.piece, d.vocab) / (d.dtype == BNS_F32 ? 32 : 64);
-    p.splits = int(std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(tiles, 1), steps / 4)));
-    Offsets o;
-    p.partial = o.take(size_t((d.vocab + m - 1) / m) * T * sizeof(float2));
-    p.at_target = o.take(T * 4);
-    p.forward_bytes = o.at;
-    o.at = 0;
-    p.g = o.take(T * p.piece * e);
-    p.sums = o.take(size_t(p.splits) * T * p.depth_d * 4);
-    p.backward_bytes = o.at;
+    p.bytes = std::max<size_t>(at, 1024);       // (never 0, which stands for an invalid description)
     return p;
 }
-
-HeadPlan laid_out_plan(const HeadDims& d) {
-    HeadPlan p = {};
-    p.planes = d.dtype == BNS_F32 ? 3 : 1;
-    p.depth_d = round_up(d.width, kDepth);
-    p.depth_t = round_up(std::max<int64_t>(d.tokens, 1), kDepth);
-    const bool fits = d.dtype == BNS_BF16 && d.width % kDepth == 0;
-    p.direct_h = fits && d.hidden_stride % 8 == 0 && d.hidden_stride < (1 << 21);
-    p.direct_w = fits && d.weight_stride % 8 == 0 && d.weight_stride < (1 << 21);
-    p.narrow = d.tokens <= 64;
-    const int64_t piece = d.piece ? d.piece : 16384;
-    p.piece = std::min(round_up(std::min<int64_t>(piece, 1 << 18), kTileM), round_up(d.vocab, kTileM));
-    const int64_t tiles = ((d.width + kTileM - 1) / kTileM) * ((d.tokens + (p.narrow ? 63 : 255)) / (p.narrow ? 64 : 256));
-    p.splits = int(std::max<int64_t>(1, std::min<int64_t>(256 / std::max<int64_t>(tiles, 1), p.piece / 512)));
-    const size_t P = size_t(p.planes) * 2, T = size_t(d.tokens), rows = size_t(p.piece);
-    Offsets o;
-    p.hidden = o.take(p.direct_h ? 0 : T * p.depth_d * P);
-    p.weight = o.take(p.direct_w ? 0 : rows * p.depth_d * P);
-    const size_t both = o.at;
-    p.partial = o.take(size_t((d.vocab + kTileM - 1) / kTileM) * T * sizeof(float2));
-    p.at_target = o.take(T * 4);
-    p.forward_bytes = o.at;
-    o.at = both;
-    p.weight_t = o.take(size_t(d.width) * rows * P);
-    p.hidden_t = o.take(size_t(d.width) * p.depth_t * P);
-    p.g = o.take(T * rows * P);
-    p.gt = o.take(rows * p.depth_t * P);
-    p.sums = o.take(size_t(p.splits) * T * p.depth_d * 4);
-    p.backward_bytes = o.at;
-    return p;
-}
-
-HeadPlan head_plan(const HeadDims& d) {
-    const int path = g_tuning.head_path;
-    const bool direct = path ? path == 1 : d.tokens <= 64;
-    return direct ? direct_plan(d) : laid_out_plan(d);
-}
-
-// (never 0, which stands for an invalid description)
-inline size_t need(const HeadPlan& p) { return std::max<size_t>(std::max(p.forward_bytes, p.backward_bytes), 1024); }
 
 inline bool failed() { return hipGetLastError() != hipSuccess; }
 
+// ---- launches -------------------------------------------------------------------------------------------------------
 template <typename T>
 bool pack_rows(const void* src, int64_t stride, int64_t rows, int width, int64_t depth, void* dst, hipStream_t st) {
     const PackArgs a = {src, static_cast<uint16_t*>(dst), nullptr, stride, int32_t(rows), width, int32_t(depth), 0};
@@ -364,212 +257,185 @@ bool pack_columns(const void* src, int64_t stride, int64_t rows, int width, int6
 }
 
 template <typename T, int EPILOGUE>
-bool gemm(GemmArgs a, bool narrow, hipStream_t st) {
-    a.tiles_a = (a.rows_a + kTileM - 1) / kTileM;
-    a.tiles_b = narrow ? (a.rows_b + 63) / 64 : (a.rows_b + 255) / 256;
+bool gemm(GemmArgs a, Kind kind, hipStream_t st) {
+    const int m = kind == kGemm128 ? 128 : 256;
+    a.tiles_a = tiles_of(a.rows_a, m);
+    a.tiles_b = tiles_of(a.rows_b, m);
     const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b * a.splits);
-    if (narrow) BNS_LAUNCH((gemm_kernel<T, 256, 64, 4, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
+    if (m == 128) BNS_LAUNCH((gemm_kernel<T, 128, 128, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
     else BNS_LAUNCH((gemm_kernel<T, 256, 256, 2, 4, EPILOGUE>), grid, dim3(512), 0, st, a);
     return !failed();
 }
 
-bool join_statistics(const HeadDims& d, const HeadPlan& p, int tile, const int64_t* targets, float* loss, float* lse, char* ws, hipStream_t st) {
-    BNS_LAUNCH(join_statistics_kernel, dim3(uint32_t((d.tokens + 15) / 16)), dim3(256), 0, st, reinterpret_cast<const float2*>(ws + p.partial),
-               reinterpret_cast<const float*>(ws + p.at_target), targets, (d.vocab + tile - 1) / tile, int(d.tokens), d.vocab, loss, lse);
+// Tokens of a tile in the kernels that have several sizes.
+inline int token_tile(int tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : 64; }
+
+template <typename T, int EPILOGUE>
+bool logits(const HeadDims& d, const HeadPlan& p, GemmArgs a, hipStream_t st) {
+    // (gt is written up to its depth, a multiple of 64 or 32)
+    const int m = rows_of(p.kind, d), n = p.kind == kDirect128 ? 128 : EPILOGUE == kGradientParts ? std::min(a.gt_depth, 64) : token_tile(a.rows_b);
+    if (p.kind >= kGemm256) {
+        if constexpr (EPILOGUE != kGradient) return gemm<T, EPILOGUE>(a, p.kind, st);
+        return false;       // (not planned)
+    }
+    a.tiles_a = tiles_of(std::max(a.rows_a, a.g_depth), m);
+    a.tiles_b = tiles_of(a.rows_b, n);
+    const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b);
+    if (p.kind == kDirect128) BNS_LAUNCH((direct_logits_kernel<T, 128, 128, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (p.kind == kDirect64 && n == 16) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (p.kind == kDirect64 && n == 32) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (p.kind == kDirect64) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (m == 16 && n == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (m == 16 && n == 32) BNS_LAUNCH((stream_logits_kernel<T, 1, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (m == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 4, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (n == 16) BNS_LAUNCH((stream_logits_kernel<T, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (n == 32) BNS_LAUNCH((stream_logits_kernel<T, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else BNS_LAUNCH((stream_logits_kernel<T, 2, 4, EPILOGUE>), grid, dim3(256), 0, st, a);
+    return !failed();
+}
+
+// The operands of the logits of rows [v0, v0 + rows) of the vocabulary; copies a piece that has to be.
+template <typename T>
+bool logits_operands(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, char* ws, int64_t v0, int rows,
+                     hipStream_t st, GemmArgs* a) {
+    const void* piece = static_cast<const T*>(weight) + v0 * d.weight_stride;
+    const int64_t packed = p.depth_d * p.planes;
+    a->a = p.copy_w ? ws + p.weight : piece;
+    a->lda = p.copy_w ? packed : d.weight_stride;
+    a->b = p.copy_h ? ws + p.hidden : hidden;
+    a->ldb = p.copy_h ? packed : d.hidden_stride;
+    a->rows_a = rows;
+    a->rows_b = int32_t(d.tokens);
+    a->depth = p.kind >= kGemm256 ? int32_t(p.depth_d) : d.width;
+    a->splits = 1;
+    a->targets = targets;
+    a->v0 = int32_t(v0);
+    a->vocab = d.vocab;
+    if (v0 == 0 && p.copy_h && !pack_rows<T>(hidden, d.hidden_stride, d.tokens, d.width, p.depth_d, ws + p.hidden, st)) return false;
+    return !p.copy_w || pack_rows<T>(piece, d.weight_stride, rows, d.width, p.depth_d, ws + p.weight, st);
+}
+
+bool join_statistics(const HeadDims& d, const HeadPlan& p, const int64_t* targets, float* loss, float* lse, char* ws, hipStream_t st) {
+    const auto* partial = reinterpret_cast<const float2*>(ws + p.partial);
+    const auto* at_target = reinterpret_cast<const float*>(ws + p.at_target);
+    const int tiles = tiles_of(d.vocab, rows_of(p.kind, d)), tokens = int(d.tokens);
+    if (tokens <= 1024) BNS_LAUNCH((join_statistics_kernel<1>), dim3(tokens), dim3(256), 0, st, partial, at_target, targets, tiles, tokens, d.vocab, loss, lse);
+    else BNS_LAUNCH((join_statistics_kernel<16>), dim3((tokens + 15) / 16), dim3(256), 0, st, partial, at_target, targets, tiles, tokens, d.vocab, loss, lse);
     return !failed();
 }
 
 template <typename T>
 bool join_splits(const HeadDims& d, const HeadPlan& p, void* dhidden, char* ws, hipStream_t st) {
-    const int64_t blocks = (d.tokens * ((d.width + 7) / 8) + 255) / 256;
-    BNS_LAUNCH((join_splits_kernel<T>), dim3(uint32_t(std::min<int64_t>(blocks, 1 << 16))), dim3(256), 0, st, reinterpret_cast<const float*>(ws + p.sums),
-               d.tokens * p.depth_d, p.splits, int(d.tokens), d.width, int(p.depth_d), static_cast<T*>(dhidden));
+    const dim3 grid(uint32_t(std::min<int64_t>(d.tokens * ((d.width + 255) / 256), 1 << 20)));
+    const float* sums = reinterpret_cast<const float*>(ws + p.sums);
+    const int64_t stride = d.tokens * p.depth_d;
+    T* const out = static_cast<T*>(dhidden);
+    if (p.splits > 4) BNS_LAUNCH((join_splits_kernel<T, 8>), grid, dim3(256), 0, st, sums, stride, p.splits, int(d.tokens), d.width, p.depth_d, out);
+    else BNS_LAUNCH((join_splits_kernel<T, 1>), grid, dim3(32), 0, st, sums, stride, p.splits, int(d.tokens), d.width, p.depth_d, out);
     return !failed();
 }
 
-// The operands of the logits of rows [v0, v0 + rows) of the vocabulary; packs what has to be packed.
+template <typename T, int EPILOGUE>
+bool direct_gradients(GemmArgs h, GemmArgs w, Kind kind, hipStream_t st) {
+    const int m = kind == kDirect128 ? 128 : 64, n = kind == kDirect128 ? 128 : token_tile(h.rows_b);
+    h.tiles_a = w.tiles_a = tiles_of(h.rows_a, m);
+    h.tiles_b = tiles_of(h.rows_b, n);
+    w.tiles_b = tiles_of(w.rows_b, m);
+    const int blocks_h = h.tiles_a * h.tiles_b * h.splits;
+    const dim3 grid(uint32_t(blocks_h) + uint32_t(w.tiles_a) * w.tiles_b);
+    if (n == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else if (n == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else if (n == 64) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else BNS_LAUNCH((direct_gradients_kernel<T, 128, 128, 2, 2, 128, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    return !failed();
+}
+
 template <typename T>
-bool logits_operands(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, char* ws, int v0, int rows, hipStream_t st, GemmArgs* a) {
-    const int64_t packed = p.depth_d * p.planes;
-    a->b = p.direct_h ? hidden : ws + p.hidden;
-    a->ldb = p.direct_h ? d.hidden_stride : packed;
-    const void* piece = static_cast<const T*>(weight) + int64_t(v0) * d.weight_stride;
-    a->a = p.direct_w ? piece : ws + p.weight;
-    a->lda = p.direct_w ? d.weight_stride : packed;
-    a->rows_a = rows;
-    a->rows_b = int32_t(d.tokens);
-    a->depth = int32_t(p.depth_d);
-    a->splits = 1;
-    a->v0 = v0;
-    a->vocab = d.vocab;
-    return p.direct_w || pack_rows<T>(piece, d.weight_stride, rows, d.width, p.depth_d, ws + p.weight, st);
+bool stream_gradients(GemmArgs h, GemmArgs w, hipStream_t st) {
+    const int groups = (h.rows_a + kStreamColumns - 1) / kStreamColumns, n = token_tile(h.rows_b);
+    const dim3 grid(uint32_t(groups) * uint32_t(h.splits + w.splits));
+    if (n == 16) BNS_LAUNCH((stream_gradients_kernel<T, 1, 1>), grid, dim3(256), 0, st, h, w, groups);
+    else if (n == 32) BNS_LAUNCH((stream_gradients_kernel<T, 2, 1>), grid, dim3(256), 0, st, h, w, groups);
+    else if constexpr (sizeof(T) == 2) BNS_LAUNCH((stream_gradients_kernel<T, 4, 2>), grid, dim3(256), 0, st, h, w, groups);
+    else return false;      // (not planned)
+    return !failed();
 }
 
 template <typename T>
 bool forward(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, float* loss, float* lse, char* ws, hipStream_t st) {
-    if (!p.direct_h && !pack_rows<T>(hidden, d.hidden_stride, d.tokens, d.width, p.depth_d, ws + p.hidden, st)) return false;
     // (without copies the whole vocabulary is one piece, as far as a launch goes: 2^22 blocks)
-    const int64_t most = std::max<int64_t>(1, (1 << 22) / ((d.tokens + 63) / 64)) * kTileM, step = p.direct_w ? std::min<int64_t>(d.vocab, most) : p.piece;
+    const int64_t most = std::max<int64_t>(1, (1 << 22) / ((d.tokens + 15) / 16)) * 256, step = p.copy_w ? p.piece : std::min<int64_t>(d.vocab, most);
     for (int64_t v0 = 0; v0 < d.vocab; v0 += step) {
         GemmArgs a = {};
-        if (!logits_operands<T>(d, p, hidden, weight, ws, int(v0), int(std::min<int64_t>(step, d.vocab - v0)), st, &a)) return false;
-        a.targets = targets;
+        if (!logits_operands<T>(d, p, hidden, weight, targets, ws, v0, int(std::min<int64_t>(step, d.vocab - v0)), st, &a)) return false;
         a.partial = reinterpret_cast<float2*>(ws + p.partial);
         a.at_target = reinterpret_cast<float*>(ws + p.at_target);
-        if (!gemm<T, kStatistics>(a, p.narrow, st)) return false;
+        if (!logits<T, kStatistics>(d, p, a, st)) return false;
     }
-    return join_statistics(d, p, kTileM, targets, loss, lse, ws, st);
+    return join_statistics(d, p, targets, loss, lse, ws, st);
 }
 
 template <typename T>
 bool backward(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, const float* lse, const float* dloss,
               void* dhidden, void* dweight, char* ws, hipStream_t st) {
-    const int planes = p.planes;
-    if (!p.direct_h && !pack_rows<T>(hidden, d.hidden_stride, d.tokens, d.width, p.depth_d, ws + p.hidden, st)) return false;
-    if (!pack_columns<T>(hidden, d.hidden_stride, d.tokens, d.width, p.depth_t, targets, d.vocab, ws + p.hidden_t, st)) return false;
+    const bool laid_out = p.gradients >= kGemm256;
+    const bool whole = p.gradients <= kDirect128 && p.gradients != kStream && p.splits == 1 && p.piece >= d.vocab;     // dhidden needs no sums beside it
+    if (laid_out && !pack_columns<T>(hidden, d.hidden_stride, d.tokens, d.width, p.depth_t, targets, d.vocab, ws + p.hidden_t, st)) return false;
     for (int64_t v0 = 0; v0 < d.vocab; v0 += p.piece) {
         const int rows = int(std::min<int64_t>(p.piece, d.vocab - v0));
         const int64_t depth_v = round_up(rows, kDepth);
         GemmArgs a = {};
-        if (!logits_operands<T>(d, p, hidden, weight, ws, int(v0), rows, st, &a)) return false;
-        a.targets = targets;
+        if (!logits_operands<T>(d, p, hidden, weight, targets, ws, v0, rows, st, &a)) return false;
         a.lse = lse;
         a.dloss = dloss;
-        a.g = reinterpret_cast<uint16_t*>(ws + p.g);
-        a.gt = reinterpret_cast<uint16_t*>(ws + p.gt);
-        a.g_depth = int32_t(depth_v);
-        a.gt_depth = int32_t(p.depth_t);
-        if (!gemm<T, kGradientParts>(a, p.narrow, st)) return false;
+        if (p.parts()) {
+            a.g = reinterpret_cast<uint16_t*>(ws + p.g);
+            a.gt = reinterpret_cast<uint16_t*>(ws + p.gt);
+            a.g_depth = int32_t(depth_v);
+            a.gt_depth = int32_t(p.depth_t);
+            if (!logits<T, kGradientParts>(d, p, a, st)) return false;
+        } else {
+            a.out = ws + p.g;
+            a.ldo = p.piece;
+            if (!logits<T, kGradient>(d, p, a, st)) return false;
+        }
         const void* piece = static_cast<const T*>(weight) + v0 * d.weight_stride;
-        if (!pack_columns<T>(piece, d.weight_stride, rows, d.width, depth_v, nullptr, 0, ws + p.weight_t, st)) return false;
+        if (laid_out && !pack_columns<T>(piece, d.weight_stride, rows, d.width, depth_v, nullptr, 0, ws + p.weight_t, st)) return false;
         // dhidden[n][m] += sum over the piece of g[n] weight[m]
         GemmArgs h = {};
-        h.a = ws + p.weight_t;
+        h.a = laid_out ? ws + p.weight_t : piece;
+        h.lda = laid_out ? depth_v * p.planes : d.weight_stride;
         h.b = ws + p.g;
-        h.lda = h.ldb = depth_v * planes;
+        h.ldb = p.parts() ? depth_v * p.planes : p.piece;
         h.rows_a = d.width;
         h.rows_b = int32_t(d.tokens);
-        h.depth = int32_t(depth_v);
-        h.splits = p.splits;
-        h.out = ws + p.sums;
-        h.ldo = p.depth_d;
-        h.split_stride = d.tokens * p.depth_d;
-        h.fresh = v0 == 0;
-        if (!gemm<T, kAccumulate>(h, p.narrow, st)) return false;
-        // dweight[n][m] = sum over the tokens of g[n] hidden[m]
-        GemmArgs w = {};
-        w.a = ws + p.hidden_t;
-        w.b = ws + p.gt;
-        w.lda = w.ldb = p.depth_t * planes;
-        w.rows_a = d.width;
-        w.rows_b = rows;
-        w.depth = int32_t(p.depth_t);
-        w.splits = 1;
-        w.out = static_cast<T*>(dweight) + v0 * d.width;
-        w.ldo = d.width;
-        if (!gemm<T, kStore>(w, false, st)) return false;
-    }
-    return join_splits<T>(d, p, dhidden, ws, st);
-}
-
-// ---- the same, operands as they lie in memory -------------------------------------------------------------------------
-template <typename T, int EPILOGUE>
-bool direct_logits(GemmArgs a, int tile, hipStream_t st) {
-    const int m = tile == 128 ? 128 : 64;
-    a.tiles_a = (a.rows_a + m - 1) / m;
-    a.tiles_b = (a.rows_b + tile - 1) / tile;
-    const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b);
-    if (tile == 16) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (tile == 32) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (tile == 64) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else BNS_LAUNCH((direct_logits_kernel<T, 128, 128, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
-    return !failed();
-}
-
-template <typename T, int EPILOGUE>
-bool direct_gradients(GemmArgs h, GemmArgs w, int tile, hipStream_t st) {
-    const int m = tile == 128 ? 128 : 64;
-    h.tiles_a = w.tiles_a = (h.rows_a + m - 1) / m;
-    h.tiles_b = (h.rows_b + tile - 1) / tile;
-    w.tiles_b = (w.rows_b + m - 1) / m;
-    const int blocks_h = h.tiles_a * h.tiles_b * h.splits;
-    const dim3 grid(uint32_t(blocks_h) + uint32_t(w.tiles_a) * w.tiles_b);
-    if (tile == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else if (tile == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else if (tile == 64) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else BNS_LAUNCH((direct_gradients_kernel<T, 128, 128, 2, 2, 128, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    return !failed();
-}
-
-GemmArgs direct_operands(const HeadDims& d, const void* hidden, const void* weight, const int64_t* targets, int64_t v0, int rows) {
-    GemmArgs a = {};
-    a.a = static_cast<const char*>(weight) + v0 * d.weight_stride * int64_t(dtype_bytes(d.dtype));
-    a.b = hidden;
-    a.lda = d.weight_stride;
-    a.ldb = d.hidden_stride;
-    a.rows_a = rows;
-    a.rows_b = int32_t(d.tokens);
-    a.depth = d.width;
-    a.splits = 1;
-    a.targets = targets;
-    a.v0 = int32_t(v0);
-    a.vocab = d.vocab;
-    return a;
-}
-
-template <typename T>
-bool forward_direct(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, float* loss, float* lse, char* ws,
-                    hipStream_t st) {
-    const int m = p.tile == 128 ? 128 : 64;
-    const int64_t most = std::max<int64_t>(1, (1 << 22) / ((d.tokens + p.tile - 1) / p.tile)) * m;
-    for (int64_t v0 = 0; v0 < d.vocab; v0 += most) {
-        GemmArgs a = direct_operands(d, hidden, weight, targets, v0, int(std::min<int64_t>(most, d.vocab - v0)));
-        a.partial = reinterpret_cast<float2*>(ws + p.partial);
-        a.at_target = reinterpret_cast<float*>(ws + p.at_target);
-        if (!direct_logits<T, kStatistics>(a, p.tile, st)) return false;
-    }
-    return join_statistics(d, p, m, targets, loss, lse, ws, st);
-}
-
-template <typename T>
-bool backward_direct(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, const float* lse, const float* dloss,
-                     void* dhidden, void* dweight, char* ws, hipStream_t st) {
-    const bool whole = p.splits == 1 && p.piece >= d.vocab;     // dhidden needs no sums beside it
-    for (int64_t v0 = 0; v0 < d.vocab; v0 += p.piece) {
-        const int rows = int(std::min<int64_t>(p.piece, d.vocab - v0));
-        GemmArgs a = direct_operands(d, hidden, weight, targets, v0, rows);
-        a.lse = lse;
-        a.dloss = dloss;
-        a.out = ws + p.g;
-        a.ldo = p.piece;
-        if (!direct_logits<T, kGradient>(a, p.tile, st)) return false;
-        GemmArgs h = {};
-        h.a = a.a;
-        h.lda = a.lda;
-        h.b = ws + p.g;
-        h.ldb = p.piece;
-        h.rows_a = d.width;
-        h.rows_b = int32_t(d.tokens);
-        h.depth = rows;
+        h.depth = laid_out ? int32_t(depth_v) : rows;
+        h.g_depth = int32_t(depth_v);
         h.splits = p.splits;
         h.out = whole ? dhidden : ws + p.sums;
         h.ldo = whole ? d.width : p.depth_d;
         h.split_stride = d.tokens * p.depth_d;
         h.fresh = v0 == 0;
+        // dweight[n][m] = sum over the tokens of g[n] hidden[m]
         GemmArgs w = {};
-        w.a = hidden;
-        w.lda = d.hidden_stride;
-        w.b = ws + p.g;
-        w.ldb = p.piece;
+        w.a = laid_out ? ws + p.hidden_t : hidden;
+        w.lda = laid_out ? p.depth_t * p.planes : d.hidden_stride;
+        w.b = ws + (p.parts() ? p.gt : p.g);
+        w.ldb = p.parts() ? p.depth_t * p.planes : p.piece;
         w.rows_a = d.width;
         w.rows_b = rows;
-        w.depth = int32_t(d.tokens);
-        w.splits = 1;
+        w.depth = laid_out ? int32_t(p.depth_t) : int32_t(d.tokens);
+        w.gt_depth = int32_t(p.depth_t);
+        w.splits = p.splits_w;
         w.targets = targets;
         w.vocab = d.vocab;
         w.out = static_cast<T*>(dweight) + v0 * d.width;
         w.ldo = d.width;
-        if (whole ? !direct_gradients<T, kStore>(h, w, p.tile, st) : !direct_gradients<T, kAccumulate>(h, w, p.tile, st)) return false;
+        const bool ok = laid_out               ? gemm<T, kAccumulate>(h, p.gradients, st) && gemm<T, kStore>(w, p.gradients, st)
+                        : p.gradients == kStream ? stream_gradients<T>(h, w, st)
+                        : whole                  ? direct_gradients<T, kStore>(h, w, p.gradients, st)
+                                                 : direct_gradients<T, kAccumulate>(h, w, p.gradients, st);
+        if (!ok) return false;
     }
     return whole || join_splits<T>(d, p, dhidden, ws, st);
 }
@@ -581,8 +447,7 @@ extern "C" {
 size_t bns_head_workspace_bytes(const bns_head* head) {
     HeadDims d;
     if (check_head(head, &d) != BNS_OK) return 0;
-    const HeadPlan p = head_plan(d);
-    return need(p);
+    return std::max(head_plan(d, false).bytes, head_plan(d, true).bytes);
 }
 
 bns_status bns_head_forward(const bns_head* head, const void* hidden, const void* weight, const int64_t* targets, float* loss, float* lse,
@@ -593,11 +458,11 @@ bns_status bns_head_forward(const bns_head* head, const void* hidden, const void
     if (d.tokens == 0) return BNS_OK;
     if (!hidden || !weight || !targets || !loss || !lse || !workspace) return BNS_EINVAL;
     if (!aligned16(hidden) || !aligned16(weight) || !aligned16(workspace)) return BNS_EINVAL;
-    const HeadPlan p = head_plan(d);
-    if (workspace_bytes < need(p)) return BNS_EWORKSPACE;
+    const HeadPlan p = head_plan(d, false);
+    if (workspace_bytes < bns_head_workspace_bytes(head)) return BNS_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
-    const auto call = d.dtype == BNS_F32 ? (p.direct ? forward_direct<float> : forward<float>) : p.direct ? forward_direct<bf16_t> : forward<bf16_t>;
+    const auto call = d.dtype == BNS_F32 ? forward<float> : forward<bf16_t>;
     const bool ok = call(d, p, hidden, weight, targets, loss, lse, ws, st);
     return ok ? BNS_OK : BNS_EDEVICE;
 }
@@ -617,15 +482,15 @@ bns_status bns_head_backward(const bns_head* head, const void* hidden, const voi
         for (const Matrix& in : {mh, mw})
             if (collide(out, in, false, row, row)) return BNS_EINVAL;
     if (collide(mdh, mdw, false, row, row)) return BNS_EINVAL;
-    const HeadPlan p = head_plan(d);
-    if (workspace_bytes < need(p)) return BNS_EWORKSPACE;
+    const HeadPlan p = head_plan(d, true);
+    if (workspace_bytes < bns_head_workspace_bytes(head)) return BNS_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     if (d.tokens == 0) {
         BNS_LAUNCH(fill_zero_kernel, dim3(4096), dim3(256), 0, st, static_cast<uint16_t*>(dweight), int64_t(d.vocab) * d.width * int64_t(e / 2));
         return failed() ? BNS_EDEVICE : BNS_OK;
     }
-    const auto call = d.dtype == BNS_F32 ? (p.direct ? backward_direct<float> : backward<float>) : p.direct ? backward_direct<bf16_t> : backward<bf16_t>;
+    const auto call = d.dtype == BNS_F32 ? backward<float> : backward<bf16_t>;
     const bool ok = call(d, p, hidden, weight, targets, lse, dloss, dhidden, dweight, ws, st);
     return ok ? BNS_OK : BNS_EDEVICE;
 }

@@ -66,28 +66,92 @@ __device__ __forceinline__ void place(int block, int total, int tiles_a, int til
 // other tiles of k add to; a result.
 enum Epilogue { kStatistics, kGradient, kGradientParts, kAccumulate, kStore };
 
-// acc[i][j][e] is C[m][n] of m = m0 + 16 i + 4 (lane / 16) + e, n = n0 + 16 j + lane % 16, where m0, n0 are the wave's; ta: number of the tile
-// along m; `stat`: LDS for WM * BN pairs, free for use.
+// Which rows of a wave's part of a tile meet in a fragment of sixteen is free, as long as operands and results agree.  They are dealt out so that what a
+// lane holds along m comes in runs of eight that continue from one quarter of the wave to the next (16 bytes of bf16 a lane, 64 a row of results), and
+// what it holds along n is contiguous: acc[i][j][e] is C[m][n] of
+//   m = m0 + 32 (i / 2) + 8 (lane / 16) + 4 (i % 2) + e  (MI even; else m0 + 16 i + 4 (lane / 16) + e)          n = n0 + NI (lane % 16) + j.
+// row_m, row_n: the row that is number r (16 i + lane % 16, 16 j + lane % 16) among the fragments' rows; slot_m, slot_n: the other way round.
+template <int MI>
+__device__ __forceinline__ int row_m(int r) { return MI % 2 ? r : r / 32 * 32 + r % 16 / 4 * 8 + r % 32 / 16 * 4 + r % 4; }
+template <int MI>
+__device__ __forceinline__ int slot_m(int m) { return MI % 2 ? m : m / 32 * 32 + m % 8 / 4 * 16 + m % 32 / 8 * 4 + m % 4; }
+template <int NI>
+__device__ __forceinline__ int row_n(int r) { return r / (16 * NI) * (16 * NI) + r % 16 * NI + r % (16 * NI) / 16; }
+template <int NI>
+__device__ __forceinline__ int slot_n(int n) { return n / (16 * NI) * (16 * NI) + n % NI * 16 + n % (16 * NI) / NI; }
+
+// COUNT neighbouring elements of a row that may begin anywhere; `left` of them exist.
+template <typename T, int COUNT>
+__device__ __forceinline__ void store_run(T* p, int left, const float (&f)[COUNT]) {
+    if (left >= COUNT) {
+        if constexpr (sizeof(T) == 2 && COUNT % 8 == 0) {
+            typedef u4 u4e __attribute__((aligned(2)));
+#pragma unroll
+            for (int k = 0; k < COUNT; k += 8)
+                *reinterpret_cast<u4e*>(p + k) = u4{pack_bf16x2(f[k], f[k + 1]), pack_bf16x2(f[k + 2], f[k + 3]), pack_bf16x2(f[k + 4], f[k + 5]), pack_bf16x2(f[k + 6], f[k + 7])};
+        } else if constexpr (sizeof(T) == 2) {
+            typedef u2 u2e __attribute__((aligned(2)));
+#pragma unroll
+            for (int k = 0; k < COUNT; k += 4) *reinterpret_cast<u2e*>(p + k) = u2{pack_bf16x2(f[k], f[k + 1]), pack_bf16x2(f[k + 2], f[k + 3])};
+        } else {
+            typedef f32x4 f32x4e __attribute__((aligned(4)));
+#pragma unroll
+            for (int k = 0; k < COUNT; k += 4) *reinterpret_cast<f32x4e*>(p + k) = f32x4{f[k], f[k + 1], f[k + 2], f[k + 3]};
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k)
+            if (k < left) {
+                if constexpr (sizeof(T) == 2) p[k].bits = uint16_t(f32_to_bf16(f[k]));
+                else p[k] = f[k];
+            }
+    }
+}
+
+// COUNT neighbouring parts at an address that is a multiple of their size.
+template <int COUNT>
+__device__ __forceinline__ void store_parts(uint16_t* p, const uint32_t (&v)[COUNT]) {
+    if constexpr (COUNT % 8 == 0) {
+#pragma unroll
+        for (int k = 0; k < COUNT; k += 8)
+            *reinterpret_cast<u4*>(p + k) = u4{v[k] | v[k + 1] << 16, v[k + 2] | v[k + 3] << 16, v[k + 4] | v[k + 5] << 16, v[k + 6] | v[k + 7] << 16};
+    } else if constexpr (COUNT % 4 == 0) {
+#pragma unroll
+        for (int k = 0; k < COUNT; k += 4) *reinterpret_cast<u2*>(p + k) = u2{v[k] | v[k + 1] << 16, v[k + 2] | v[k + 3] << 16};
+    } else if constexpr (COUNT == 2) {
+        *reinterpret_cast<uint32_t*>(p) = v[0] | v[1] << 16;
+    } else {
+        static_assert(COUNT == 1, "one, two, or a multiple of four");
+        *p = uint16_t(v[0]);
+    }
+}
+
+// ta, tb: numbers of the tile along m and n; `stat`: LDS for WM * BN pairs, free for use once every wave has come here (WM = 1: none).
 template <typename T, int EPILOGUE, int BM, int BN, int WM, int WN>
 __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM / 16][BN / WN / 16], int ta, int tb, int split, float2* stat) {
     constexpr int P = planes_of<T>(), kM = BM / WM, kN = BN / WN, MI = kM / 16, NI = kN / 16;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, wm = wave / WN, wn = wave % WN, r16 = lane % 16, quarter = lane / 16;
-    const int n0 = tb * BN, m_base = ta * BM + wm * kM + quarter * 4, n_base = n0 + wn * kN + r16;
+    constexpr int kRun = MI % 2 ? 4 : 8, kRuns = 4 * MI / kRun, kStride = 4 * kRun;     // a lane has kRuns runs of kRun, kStride apart
+    const int wave = WM * WN == 1 ? 0 : int(threadIdx.x) / kWave, lane = threadIdx.x % kWave, wm = wave / WN, wn = wave % WN, r16 = lane % 16;
+    const int m_base = ta * BM + wm * kM + lane / 16 * kRun, n_base = tb * BN + wn * kN + r16 * NI, left = a.rows_a - m_base;
+    // element x of run r
+    const auto at = [&](int r, int j, int x) { return acc[r * (kRun / 4) + x / 4][j][x % 4]; };
+    const auto put = [&](int r, int j, int x, float f) { acc[r * (kRun / 4) + x / 4][j][x % 4] = f; };
     if constexpr (EPILOGUE == kStatistics) {
-        __syncthreads();
+        if constexpr (WM > 1) __syncthreads();
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            const int n = n_base + 16 * j;
+            const int n = n_base + j;
             const int64_t target = n < a.rows_b ? a.targets[n] : -1;
             const int aim = target >= 0 && target < a.vocab ? int(target) - a.v0 - m_base : -1;
             float m = -__builtin_inff(), l = 0.f;
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+            for (int r = 0; r < kRuns; ++r)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (aim == 16 * i + e) a.at_target[n] = acc[i][j][e];
-                    acc[i][j][e] = m_base + 16 * i + e < a.rows_a ? acc[i][j][e] * kLog2e : -__builtin_inff();
-                    m = fmaxf(m, acc[i][j][e]);
+                for (int x = 0; x < kRun; ++x) {
+                    const float z = at(r, j, x), f = r * kStride + x < left ? z * kLog2e : -__builtin_inff();
+                    if (aim == r * kStride + x) a.at_target[n] = z;
+                    put(r, j, x, f);
+                    m = fmaxf(m, f);
                 }
             m = fmaxf(m, __shfl_xor(m, 16));
             m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), -3e38f);        // (a finite number where the wave has no row)
@@ -97,23 +161,28 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM /
                 for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(acc[i][j][e] - m);
             l += __shfl_xor(l, 16);
             l += __shfl_xor(l, 32);
-            if (quarter == 0) stat[wm * BN + wn * kN + 16 * j + r16] = float2{m, l};
+            if (lane < 16) {
+                if constexpr (WM > 1) stat[wm * BN + wn * kN + r16 * NI + j] = float2{m, l};
+                else if (n < a.rows_b) a.partial[int64_t(a.v0 / BM + ta) * a.rows_b + n] = float2{m, l};
+            }
         }
-        __syncthreads();
-        for (int c = threadIdx.x; c < BN; c += (WM * WN * kWave)) {
-            if (n0 + c >= a.rows_b) continue;
-            float m = stat[c].x, l = 0.f;
+        if constexpr (WM > 1) {
+            __syncthreads();
+            for (int c = threadIdx.x; c < BN; c += WM * WN * kWave) {
+                if (tb * BN + c >= a.rows_b) continue;
+                float m = stat[c].x, l = 0.f;
 #pragma unroll
-            for (int w = 1; w < WM; ++w) m = fmaxf(m, stat[w * BN + c].x);
+                for (int w = 1; w < WM; ++w) m = fmaxf(m, stat[w * BN + c].x);
 #pragma unroll
-            for (int w = 0; w < WM; ++w) l = fmaf(stat[w * BN + c].y, __builtin_amdgcn_exp2f(stat[w * BN + c].x - m), l);
-            a.partial[int64_t(a.v0 / BM + ta) * a.rows_b + n0 + c] = float2{m, l};
+                for (int w = 0; w < WM; ++w) l = fmaf(stat[w * BN + c].y, __builtin_amdgcn_exp2f(stat[w * BN + c].x - m), l);
+                a.partial[int64_t(a.v0 / BM + ta) * a.rows_b + tb * BN + c] = float2{m, l};
+            }
         }
     }
     if constexpr (EPILOGUE == kGradient || EPILOGUE == kGradientParts) {
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            const int n = n_base + 16 * j;
+            const int n = n_base + j;
             int64_t target = -1;
             float lse = 0.f, scale = 0.f;
             if (n < a.rows_b) {
@@ -124,38 +193,49 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM /
             const bool valid = target >= 0 && target < a.vocab;
             const int aim = valid ? int(target) - a.v0 - m_base : -1;
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int m = m_base + 16 * i;
-                float f[4];
+            for (int r = 0; r < kRuns; ++r) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    f[e] = __builtin_amdgcn_exp2f((acc[i][j][e] - lse) * kLog2e);
-                    if (aim == 16 * i + e) f[e] -= 1.f;
-                    f[e] = valid && m + e < a.rows_a ? f[e] * scale : 0.f;
+                for (int x = 0; x < kRun; ++x) {
+                    float f = __builtin_amdgcn_exp2f((at(r, j, x) - lse) * kLog2e);
+                    if (aim == r * kStride + x) f -= 1.f;
+                    put(r, j, x, valid && r * kStride + x < left ? f * scale : 0.f);
                 }
                 if constexpr (EPILOGUE == kGradient) {
-                    if (n < a.rows_b && m < a.rows_a) {
-                        T* const p = static_cast<T*>(a.out) + n * a.ldo + m;        // (ldo is a multiple of four)
-                        if constexpr (P == 1) *reinterpret_cast<u2*>(p) = u2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
-                        else *reinterpret_cast<f32x4*>(p) = f32x4{f[0], f[1], f[2], f[3]};
-                    }
-                    continue;
-                }
-                uint32_t part[4][3];
+                    float f[kRun];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (P == 1) part[e][0] = f32_to_bf16(f[e]);
-                    else split3(f[e], part[e]);
+                    for (int x = 0; x < kRun; ++x) f[x] = at(r, j, x);
+                    if (n < a.rows_b) store_run<T, kRun>(static_cast<T*>(a.out) + n * a.ldo + m_base + r * kStride, left - r * kStride, f);
                 }
+            }
+        }
+        if constexpr (EPILOGUE == kGradientParts) {
+            // g with zeros behind the rows of the piece, gt with zeros behind the tokens: their k is a whole number of steps
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r) {
+                const int m = m_base + r * kStride;
+                uint32_t part[kRun][NI][P];
+#pragma unroll
+                for (int x = 0; x < kRun; ++x)
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) {
+                        if constexpr (P == 1) part[x][j][0] = f32_to_bf16(at(r, j, x));
+                        else split3(at(r, j, x), part[x][j]);
+                    }
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    if (n < a.gt_depth && m < a.g_depth) {
-                        if (n < a.rows_b)
-                            *reinterpret_cast<u2*>(a.g + int64_t(n) * a.g_depth * P + int64_t(p) * a.g_depth + m) =
-                                u2{part[0][p] | part[1][p] << 16, part[2][p] | part[3][p] << 16};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (m + e < a.rows_a) a.gt[int64_t(m + e) * a.gt_depth * P + int64_t(p) * a.gt_depth + n] = uint16_t(part[e][p]);
+                    for (int j = 0; j < NI; ++j) {
+                        uint32_t v[kRun];
+#pragma unroll
+                        for (int x = 0; x < kRun; ++x) v[x] = part[x][j][p];
+                        if (n_base + j < a.rows_b && m < a.g_depth) store_parts<kRun>(a.g + int64_t(n_base + j) * a.g_depth * P + int64_t(p) * a.g_depth + m, v);
+                    }
+#pragma unroll
+                    for (int x = 0; x < kRun; ++x) {
+                        uint32_t v[NI];
+#pragma unroll
+                        for (int j = 0; j < NI; ++j) v[j] = part[x][j][p];
+                        if (r * kStride + x < left && n_base < a.gt_depth) store_parts<NI>(a.gt + int64_t(m + x) * a.gt_depth * P + int64_t(p) * a.gt_depth + n_base, v);
                     }
                 }
             }
@@ -165,42 +245,28 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM /
         float* const out = static_cast<float*>(a.out) + split * a.split_stride;
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            const int n = n_base + 16 * j;
-            if (n >= a.rows_b) continue;
+            if (n_base + j >= a.rows_b) continue;
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                if (m_base + 16 * i >= a.rows_a) continue;
-                f32x4* const p = reinterpret_cast<f32x4*>(out + n * a.ldo + m_base + 16 * i);
-                *p = a.fresh ? acc[i][j] : *p + acc[i][j];
-            }
+            for (int r = 0; r < kRuns; ++r)
+#pragma unroll
+                for (int x = 0; x < kRun; x += 4) {
+                    if (r * kStride + x >= left) continue;
+                    const f32x4 sum = {at(r, j, x), at(r, j, x + 1), at(r, j, x + 2), at(r, j, x + 3)};
+                    f32x4* const p = reinterpret_cast<f32x4*>(out + (n_base + j) * a.ldo + m_base + r * kStride + x);
+                    *p = a.fresh ? sum : *p + sum;
+                }
         }
     }
     if constexpr (EPILOGUE == kStore) {
-        T* const out = static_cast<T*>(a.out);
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            const int n = n_base + 16 * j;
-            if (n >= a.rows_b) continue;
+            if (n_base + j >= a.rows_b) continue;
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int m = m_base + 16 * i;
-                T* const p = out + n * a.ldo + m;
-                if (m + 4 <= a.rows_a) {
-                    if constexpr (P == 1) {
-                        typedef u2 u2e __attribute__((aligned(2)));
-                        *reinterpret_cast<u2e*>(p) = u2{pack_bf16x2(acc[i][j][0], acc[i][j][1]), pack_bf16x2(acc[i][j][2], acc[i][j][3])};
-                    } else {
-                        typedef f32x4 f32x4e __attribute__((aligned(4)));
-                        *reinterpret_cast<f32x4e*>(p) = acc[i][j];
-                    }
-                } else {
+            for (int r = 0; r < kRuns; ++r) {
+                float f[kRun];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (m + e < a.rows_a) {
-                            if constexpr (P == 1) p[e].bits = uint16_t(f32_to_bf16(acc[i][j][e]));
-                            else p[e] = acc[i][j][e];
-                        }
-                }
+                for (int x = 0; x < kRun; ++x) f[x] = at(r, j, x);
+                store_run<T, kRun>(static_cast<T*>(a.out) + (n_base + j) * a.ldo + m_base + r * kStride, left - r * kStride, f);
             }
         }
     }

@@ -2,7 +2,7 @@
 // into LDS fp32 values become three bf16 parts and columns become rows, so nothing is laid out beforehand; that work is done again in every tile that
 // reads an element, which is why large products prefer operands laid out once.
 //
-// A tile of BM x BN belongs to four waves.  The operands of the next step of k are on their way from memory into registers while the present one is
+// A tile of BM x BN belongs to four waves.  The operands of the next steps of k are on their way from memory into registers while the present one is
 // multiplied; LDS holds one step, so that several blocks share a compute unit and hide each other's waits.
 #pragma once
 #include "bns_head_device.hpp"
@@ -10,8 +10,8 @@
 namespace bns {
 
 // The elements of one operand's tile that a thread brings in: eight neighbours along k of a row (K_ROWS), or eight neighbouring rows at two
-// neighbouring k, which together give whole 32-bit words of LDS.
-template <typename T, int ROWS, int DEPTH, bool K_ROWS, int THREADS>
+// neighbouring k, which together give whole 32-bit words of LDS.  ROW, SLOT: which row of the tile lies at which place in LDS (row_m, slot_m, ...).
+template <typename T, int ROWS, int DEPTH, bool K_ROWS, int THREADS, int (*ROW)(int), int (*SLOT)(int)>
 struct Feed {
     static constexpr int P = planes_of<T>(), kRowBytes = DEPTH * 2, kPlane = ROWS * kRowBytes, kChunks = DEPTH / 8;
     static constexpr int kUnits = K_ROWS ? ROWS * DEPTH / 8 : (DEPTH / 2) * (ROWS / 8), kPer = (kUnits + THREADS - 1) / THREADS, kRaw = K_ROWS ? 1 : 2;
@@ -39,7 +39,7 @@ struct Feed {
             const int unit = i * THREADS + int(threadIdx.x);
             if (kUnits % THREADS != 0 && unit >= kUnits) break;
             if constexpr (K_ROWS) {
-                const int row = min(row0 + unit / kChunks, rows - 1), k = k0 + unit % kChunks * 8;
+                const int row = min(row0 + ROW(unit / kChunks), rows - 1), k = k0 + unit % kChunks * 8;
                 const T* p = base + row * ld + k;
                 if (inside) raw[i][0].load(p);
                 else fetch(raw[i][0], p, depth - k);
@@ -96,7 +96,7 @@ struct Feed {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const uint32_t even = raw[i][0].a[j / 2], odd = raw[i][1].a[j / 2];
-                        *reinterpret_cast<uint32_t*>(lds + at(row + j, pair / 4) + pair % 4 * 4) =
+                        *reinterpret_cast<uint32_t*>(lds + at(SLOT(row + j), pair / 4) + pair % 4 * 4) =
                             j % 2 ? even >> 16 | (odd & 0xffff0000u) : (even & 0xffffu) | odd << 16;
                     }
                 } else {
@@ -110,7 +110,7 @@ struct Feed {
                         split3(odd[j], hi);
 #pragma unroll
                         for (int p = 0; p < 3; ++p)
-                            *reinterpret_cast<uint32_t*>(lds + p * kPlane + at(row + j, pair / 4) + pair % 4 * 4) = lo[p] | hi[p] << 16;
+                            *reinterpret_cast<uint32_t*>(lds + p * kPlane + at(SLOT(row + j), pair / 4) + pair % 4 * 4) = lo[p] | hi[p] << 16;
                     }
                 }
             }
@@ -129,8 +129,8 @@ template <typename T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, 
 __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* lds) {
     using S = DirectTile<T, BM, BN, WM, WN>;
     constexpr int P = S::P, D = S::kDepth, MI = BM / WM / 16, NI = BN / WN / 16;
-    using FeedA = Feed<T, BM, D, A_ROWS, S::kThreads>;
-    using FeedB = Feed<T, BN, D, B_ROWS, S::kThreads>;
+    using FeedA = Feed<T, BM, D, A_ROWS, S::kThreads, row_m<MI>, slot_m<MI>>;
+    using FeedB = Feed<T, BN, D, B_ROWS, S::kThreads, row_n<NI>, slot_n<NI>>;
     char* const lds_b = lds + FeedA::kPlane * P;
     const int tiles = a.tiles_a * a.tiles_b, split = block / tiles, tile = block - split * tiles;
     int ta, tb;
@@ -140,45 +140,50 @@ __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* 
     const T *pa = static_cast<const T*>(a.a), *pb = static_cast<const T*>(a.b);
     const int64_t* const targets = A_ROWS ? nullptr : a.targets;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, wm = wave / WN, wn = wave % WN, r16 = lane % 16, quarter = lane / 16;
-    FeedA fa;
-    FeedB fb;
+    constexpr int kAhead = BM * BN > 64 * 64 ? 1 : 2;       // steps on their way
+    FeedA fa[kAhead];
+    FeedB fb[kAhead];
     f32x4 acc[MI][NI];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (first < end) {
-        fa.ask(pa, a.lda, m0, a.rows_a, first * D, a.depth, targets);
-        fb.ask(pb, a.ldb, n0, a.rows_b, first * D, a.depth, nullptr);
-    }
-    for (int step = first; step < end; ++step) {
-        __syncthreads();                    // (the step before has been read)
-        fa.put(lds, targets, a.vocab);
-        fb.put(lds_b, nullptr, 0);
-        __syncthreads();
-        if (step + 1 < end) {
-            fa.ask(pa, a.lda, m0, a.rows_a, (step + 1) * D, a.depth, targets);
-            fb.ask(pb, a.ldb, n0, a.rows_b, (step + 1) * D, a.depth, nullptr);
-        }
+    const auto ask = [&](int u, int step) {
+        fa[u].ask(pa, a.lda, m0, a.rows_a, step * D, a.depth, targets);
+        fb[u].ask(pb, a.ldb, n0, a.rows_b, step * D, a.depth, nullptr);
+    };
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk) {
-            bf16x8 x[MI][P], y[NI][P];
+    for (int u = 0; u < kAhead; ++u)
+        if (first + u < end) ask(u, first + u);
+    for (int at = first; at < end; at += kAhead) {
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
+        for (int u = 0; u < kAhead; ++u) {
+            if (at + u >= end) break;
+            __syncthreads();                    // (the step before has been read)
+            fa[u].put(lds, targets, a.vocab);
+            fb[u].put(lds_b, nullptr, 0);
+            __syncthreads();
+            if (at + u + kAhead < end) ask(u, at + u + kAhead);
 #pragma unroll
-                for (int j = 0; j < NI; ++j)
-                    y[j][p] = *reinterpret_cast<const bf16x8*>(lds_b + p * FeedB::kPlane + FeedB::at(wn * (BN / WN) + j * 16 + r16, kk * 4 + quarter));
+            for (int kk = 0; kk < D / 32; ++kk) {
+                bf16x8 x[MI][P], y[NI][P];
 #pragma unroll
-                for (int i = 0; i < MI; ++i)
-                    x[i][p] = *reinterpret_cast<const bf16x8*>(lds + p * FeedA::kPlane + FeedA::at(wm * (BM / WM) + i * 16 + r16, kk * 4 + quarter));
-            }
-#pragma unroll
-            for (int s = P == 1 ? 5 : 0; s < 6; ++s)
-#pragma unroll
-                for (int i = 0; i < MI; ++i)
+                for (int p = 0; p < P; ++p) {
 #pragma unroll
                     for (int j = 0; j < NI; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][plane_a(s)], y[j][plane_b(s)], acc[i][j], 0, 0, 0);
+                        y[j][p] = *reinterpret_cast<const bf16x8*>(lds_b + p * FeedB::kPlane + FeedB::at(wn * (BN / WN) + j * 16 + r16, kk * 4 + quarter));
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+                        x[i][p] = *reinterpret_cast<const bf16x8*>(lds + p * FeedA::kPlane + FeedA::at(wm * (BM / WM) + i * 16 + r16, kk * 4 + quarter));
+                }
+#pragma unroll
+                for (int s = P == 1 ? 5 : 0; s < 6; ++s)
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int j = 0; j < NI; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][plane_a(s)], y[j][plane_b(s)], acc[i][j], 0, 0, 0);
+            }
         }
     }
     finish<T, EPILOGUE, BM, BN, WM, WN>(a, acc, ta, tb, split, reinterpret_cast<float2*>(lds));

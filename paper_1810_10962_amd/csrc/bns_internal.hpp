@@ -96,8 +96,9 @@ struct Tuning {
     TuneInt nhwc_split_ordered{0};          // that kernel front to back (beyond the single launch): 1 whenever it can run, 2 never
     TuneInt nhwc_split_dx{0};               // backward writes dx outside S from the reduction kernel: 1 always (bits of the stage calls), 2 never, 0 as
                                             // nhwc_split_ordered says
-    TuneInt head_path{0};                   // loss over the vocabulary: 1 operands as they lie in memory, 2 laid out first, 0 by size
-    TuneInt head_tile{0};                   // its tiles in the first case: 64, 128, 0 by size
+    // loss over the vocabulary, kernels of the logits (forward, backward) and of the gradients' products: 1 few tokens, 2 / 3 operands as they lie in
+    // memory with tiles of 64 / 128, 4 / 5 operands laid out first with tiles of 256 / 128; 0 by size
+    TuneInt head_logits{0}, head_logits_backward{0}, head_gradients{0};
     // For the library's own tests of the give-up path only; a caller has no use for them.
     TuneInt test_spin_limit{0};             // polls a team member waits for a team-mate before giving up (default 2^21)
     TuneInt test_mute_exchange{0};          // 1: no member publishes its sums, so every wait runs out

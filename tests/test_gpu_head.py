@@ -14,17 +14,19 @@ from paper_1810_10962_amd import bns
 pytestmark = pytest.mark.gpu
 
 
-# How the operands are read: as they lie in memory (tiles by size, or of 128), or laid out first; see "head_path" and "head_tile".
-PATHS = {"direct": (1, 0), "direct128": (1, 128), "laid_out": (2, 0), "auto": (0, 0)}
+# Kernels of the forward pass's logits, the backward pass's and the gradients' products: see "head_logits" and the options behind it.
+PATHS = {"few": (1, 1, 1), "few_direct": (1, 1, 2), "direct64": (2, 2, 2), "direct64_few": (2, 2, 1), "direct128": (3, 3, 3), "laid_out256": (4, 4, 4), "laid_out128": (5, 5, 5),
+         "mixed": (5, 1, 4), "mixed2": (4, 3, 5), "auto": (0, 0, 0)}
+OPTIONS = ("head_logits", "head_logits_backward", "head_gradients")
 
 
 @pytest.fixture(params=PATHS)
 def path(request):
-    for name, value in zip(("head_path", "head_tile"), PATHS[request.param]):
+    for name, value in zip(OPTIONS, PATHS[request.param]):
         bns.bns_set_option(name, value)
     yield request.param
-    bns.bns_set_option("head_path", 0)
-    bns.bns_set_option("head_tile", 0)
+    for name in OPTIONS:
+        bns.bns_set_option(name, 0)
 
 
 def make(tokens, width, vocab, dtype, seed=0, ignored=0.2):
