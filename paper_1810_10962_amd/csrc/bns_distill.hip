@@ -42,9 +42,9 @@ struct Words;
 template <>
 struct Words<float> {
     static constexpr int kElems = 4;
-    typedef u4 u4e __attribute__((aligned(4)));
+    template <bool NT>
     static __device__ __forceinline__ u4 load(const float* p, int left) {
-        if (left >= 4) return *reinterpret_cast<const u4e*>(p);
+        if (left >= 4) return get16<NT>(p);
         const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
         const uint32_t none = 0xff800000u;
         return u4{left > 0 ? w[0] : none, left > 1 ? w[1] : none, left > 2 ? w[2] : none, none};
@@ -53,23 +53,24 @@ struct Words<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(w[i]);
     }
+    template <bool NT>
     static __device__ __forceinline__ void store(float* p, int left, const float (&f)[4]) {
         if (left >= 4) {
-            *reinterpret_cast<u4e*>(p) = u4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+            put16<NT>(p, u4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (i < left) p[i] = f[i];
         }
     }
-    static __device__ __forceinline__ void put(float* p, float f) { *p = f; }
+    static __device__ __forceinline__ void put_one(float* p, float f) { *p = f; }
 };
 template <>
 struct Words<bf16_t> {
     static constexpr int kElems = 8;
-    typedef u4 u4e __attribute__((aligned(2)));
+    template <bool NT>
     static __device__ __forceinline__ u4 load(const bf16_t* p, int left) {
-        if (left >= 8) return *reinterpret_cast<const u4e*>(p);
+        if (left >= 8) return get16<NT>(p);
         u4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -85,37 +86,51 @@ struct Words<bf16_t> {
             f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
-    static __device__ __forceinline__ void store(bf16_t* p, int left, const float (&f)[8]) { Row8<bf16_t>::store(p, left, f); }
-    static __device__ __forceinline__ void put(bf16_t* p, float f) { p->bits = uint16_t(f32_to_bf16(f)); }
+    template <bool NT>
+    static __device__ __forceinline__ void store(bf16_t* p, int left, const float (&f)[8]) { Row8<bf16_t>::store<NT>(p, left, f); }
+    static __device__ __forceinline__ void put_one(bf16_t* p, float f) { p->bits = uint16_t(f32_to_bf16(f)); }
 };
 
 // The teacher's part of a row, worked out by one wave.
 struct Teacher {
-    int32_t id[kMostEntries];   // -1: no entry
-    float q[kMostEntries];
-    float z[kMostEntries];      // the student's logit there (only of ids in [v0, v1))
-    float cross;                // sum q (log q - z / tau)
-    int32_t some;               // whether the row has an entry
+    alignas(16) int32_t id[kMostEntries];   // -1: no entry
+    alignas(16) float q[kMostEntries];      // (0 from entry k on to a multiple of four)
+    float z[kMostEntries];                  // the student's logit there (only of ids in [v0, v1))
+    float cross;                            // sum q (log q - z / tau)
+    int32_t some;                           // whether the row has an entry
+};
+
+// An entry that its lane has asked for; the first kWave of them are asked for before the row is, so that they arrive first.
+struct Entry {
+    int64_t id = -1;
+    float u = 0.f;
+    __device__ __forceinline__ void ask(const DistillArgs& a, int64_t row, int j) {
+        if (j < a.k) {
+            id = a.ids[row * a.k + j];
+            u = a.teacher[row * a.k + j];
+        }
+    }
 };
 
 template <typename T>
-__device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, int64_t row, const T* logits, int v0, int v1, bool cross) {
+__device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, int64_t row, const Entry& first, const T* logits, int v0, int v1, bool cross) {
     const int lane = threadIdx.x;
-    const int64_t* ids = a.ids + row * a.k;
-    const float* u = a.teacher + row * a.k;
     const float c = kLog2e / a.tau;
     float most = -__builtin_inff();
     bool some = false;
-    for (int j = lane; j < a.k; j += kWave) {
-        const int64_t id = ids[j];
-        const float v = u[j];
-        const bool valid = id >= 0 && id < a.vocab && !(v == -__builtin_inff());
-        s.id[j] = valid ? int32_t(id) : -1;
-        s.q[j] = v;
+    for (int j = lane; j < (a.k + 3) / 4 * 4; j += kWave) {
+        Entry e = first;
+        if (j >= kWave) {
+            e.id = -1;
+            e.ask(a, row, j);
+        }
+        const bool valid = j < a.k && e.id >= 0 && e.id < a.vocab && !(e.u == -__builtin_inff());
+        s.id[j] = valid ? int32_t(e.id) : -1;
+        s.q[j] = e.u;
         if (valid) {
-            if (id >= v0 && id < v1) s.z[j] = load_scalar<T>(logits + id);
+            if (e.id >= v0 && e.id < v1) s.z[j] = load_scalar<T>(logits + e.id);
             some = true;
-            most = fmaxf(most, v);
+            most = fmaxf(most, e.u);
         }
     }
     most = fmaxf(wave_max(most), -3e38f);
@@ -124,7 +139,7 @@ __device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, i
         if (s.id[j] >= 0) sum += __builtin_amdgcn_exp2f((s.q[j] - most) * c);
     const float total = wave_sum(sum), inv = 1.f / total, log2_total = __builtin_amdgcn_logf(total);
     float x = 0.f;
-    for (int j = lane; j < a.k; j += kWave) {
+    for (int j = lane; j < (a.k + 3) / 4 * 4; j += kWave) {
         if (s.id[j] < 0) {
             s.q[j] = 0.f;
             continue;
@@ -149,8 +164,12 @@ __device__ __forceinline__ void fix_entries(const Teacher& s, const DistillArgs&
         const int id = s.id[j];
         if (id < v0 || id >= v1) continue;
         float q = 0.f;
-        for (int i = 0; i < a.k; ++i) q += s.id[i] == id ? s.q[i] : 0.f;
-        Words<T>::put(dlogits + id, scale * (__builtin_amdgcn_exp2f(fmaf(s.z[j], c, -lse2)) - q));
+        for (int i = 0; i < a.k; i += 4) {
+            const int4 ids = *reinterpret_cast<const int4*>(s.id + i);
+            const float4 qs = *reinterpret_cast<const float4*>(s.q + i);
+            q += (ids.x == id ? qs.x : 0.f) + (ids.y == id ? qs.y : 0.f) + (ids.z == id ? qs.z : 0.f) + (ids.w == id ? qs.w : 0.f);
+        }
+        Words<T>::put_one(dlogits + id, scale * (__builtin_amdgcn_exp2f(fmaf(s.z[j], c, -lse2)) - q));
     }
 }
 
@@ -161,8 +180,9 @@ __device__ __forceinline__ void keep_packed(u4 (&w)[N]) {
     for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
 }
 
-// NV: 16-byte words per thread that hold the row; 0: the row is read again.
-template <typename T, int THREADS, int NV>
+// NV: 16-byte words per thread that hold the row; 0: the row is read again.  NT: with the non-temporal hint (4096x131072 bf16 with its gradient 400 against
+// 416 us, gradient of 2048x50304 fp32 162 against 172; 7x100003 bf16 6.7 against 6.4).
+template <typename T, int THREADS, int NV, bool NT>
 __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a) {
     constexpr int E = Words<T>::kElems, kWaves = THREADS / kWave;
     __shared__ Teacher teacher;
@@ -171,6 +191,8 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
     const float c = kLog2e / a.tau;
     for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
         const T* z = static_cast<const T*>(a.logits) + row * a.logits_stride;
+        Entry entry;
+        if (wave == 0) entry.ask(a, row, tid);
         u4 held[NV > 0 ? NV : 1];
         // The row's last word is moved back so that it ends with the row, and so are those behind it: all are on their way before any is
         // looked at.  What they hold twice does not change a maximum, is left out of the sum and written twice with the same bits.
@@ -180,10 +202,10 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int v = (j * THREADS + t) * E;
-                held[j] = Words<T>::load(z + min(v, a.vocab - E), E);
+                held[j] = Words<T>::template load<NT>(z + min(v, a.vocab - E), E);
             }
         }
-        if (wave == 0) work_teacher(teacher, a, row, z, 0, a.vocab, true);
+        if (wave == 0) work_teacher(teacher, a, row, entry, z, 0, a.vocab, true);
         // maximum of z / tau in powers of two, and sum of exp2 of what lies below it; a wave that meets only -infinity has a finite maximum
         float m = -__builtin_inff(), l = 0.f;
         if (NV > 0) {
@@ -217,7 +239,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
             m = kLeast;
             for (int v = tid * E; v < a.vocab; v += THREADS * E) {
                 float f[E], most = -__builtin_inff();
-                Words<T>::unpack(Words<T>::load(z + v, a.vocab - v), f);
+                Words<T>::unpack(Words<T>::template load<NT>(z + v, a.vocab - v), f);
 #pragma unroll
                 for (int i = 0; i < E; ++i) most = fmaxf(most, f[i]);
                 most = fmaxf(m, most * c);
@@ -256,7 +278,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
                 Words<T>::unpack(w, f);
 #pragma unroll
                 for (int i = 0; i < E; ++i) f[i] = some ? scale * __builtin_amdgcn_exp2f(fmaf(f[i], c, -lse2)) : 0.f;
-                Words<T>::store(out + v, left, f);
+                Words<T>::template store<NT>(out + v, left, f);
             };
             if (NV > 0) {
                 keep_packed(held);
@@ -268,7 +290,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
                     __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
-                for (int v = tid * E; v < a.vocab; v += THREADS * E) write(v, Words<T>::load(z + v, a.vocab - v), a.vocab - v);
+                for (int v = tid * E; v < a.vocab; v += THREADS * E) write(v, Words<T>::template load<NT>(z + v, a.vocab - v), a.vocab - v);
             }
             __syncthreads();
             if (some) fix_entries(teacher, a, out, 0, a.vocab, lse2, scale);
@@ -278,7 +300,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
 }
 
 // One segment of a row.
-template <typename T>
+template <typename T, bool NT>
 __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, int segments) {
     constexpr int E = Words<T>::kElems, kAtOnce = 4;
     __shared__ Teacher teacher;
@@ -288,23 +310,32 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, in
         const int v0 = int(b % segments) * a.segment, v1 = min(v0 + a.segment, a.vocab);
         const T* z = static_cast<const T*>(a.logits) + row * a.logits_stride;
         T* out = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
-        if (threadIdx.x < kWave) work_teacher(teacher, a, row, z, v0, v1, false);
-        const float lse2 = a.lse_in[row] * kLog2e;
+        Entry entry;
+        if (threadIdx.x < kWave) entry.ask(a, row, threadIdx.x);
+        const float lse2 = a.lse_in[row] * kLog2e, dloss = a.dloss[row];
+        // (the first words are on their way while the teacher is worked out; nothing is written before the teacher has read)
+        u4 w[kAtOnce];
+        const auto ask = [&](int v) {
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) w[j] = Words<T>::template load<NT>(z + v + j * 256 * E, v1 - v - j * 256 * E);
+        };
+        int v = v0 + int(threadIdx.x) * E;
+        ask(v);
+        if (threadIdx.x < kWave) work_teacher(teacher, a, row, entry, z, v0, v1, false);
         __syncthreads();
         const bool some = teacher.some;
-        const float scale = some ? a.tau * a.dloss[row] : 0.f;
-        for (int v = v0 + int(threadIdx.x) * E; v < v1; v += 256 * E * kAtOnce) {
-            u4 w[kAtOnce];
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) w[j] = Words<T>::load(z + v + j * 256 * E, v1 - v - j * 256 * E);
+        const float scale = some ? a.tau * dloss : 0.f;
+        while (v < v1) {
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 float f[E];
                 Words<T>::unpack(w[j], f);
 #pragma unroll
                 for (int i = 0; i < E; ++i) f[i] = some ? scale * __builtin_amdgcn_exp2f(fmaf(f[i], c, -lse2)) : 0.f;
-                if (v + j * 256 * E < v1) Words<T>::store(out + v + j * 256 * E, v1 - v - j * 256 * E, f);
+                if (v + j * 256 * E < v1) Words<T>::template store<NT>(out + v + j * 256 * E, v1 - v - j * 256 * E, f);
             }
+            v += 256 * E * kAtOnce;
+            if (v < v1) ask(v);
         }
         __syncthreads();
         if (some) fix_entries(teacher, a, out, v0, v1, lse2, scale);
@@ -314,36 +345,38 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, in
 
 constexpr int64_t kMostBlocks = int64_t(1) << 20;
 
+template <typename T, int THREADS, int NV>
+void launch_rows(const DistillArgs& a, hipStream_t st) {
+    const dim3 grid(uint32_t(std::min(a.tokens, kMostBlocks)));
+    if (size_t(a.tokens) * a.vocab * sizeof(T) * (a.dlogits ? 2 : 1) > kStreamBytes && NV > 0)
+        BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV, (NV > 0)>), grid, dim3(THREADS), 0, st, a);
+    else BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV, false>), grid, dim3(THREADS), 0, st, a);
+}
+
+// The smallest block that holds a row.
 template <typename T>
 void launch_forward(const DistillArgs& a, hipStream_t st) {
     const int64_t words = (a.vocab + Words<T>::kElems - 1) / Words<T>::kElems;
-    const dim3 grid(uint32_t(std::min(a.tokens, kMostBlocks)));
-#define BNS_DISTILL(THREADS, NV)                                                                          \
-    if (words <= int64_t(THREADS) * NV) {                                                                 \
-        BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV>), grid, dim3(THREADS), 0, st, a);              \
-        return;                                                                                           \
-    }
-    if (a.vocab >= Words<T>::kElems) {
-    BNS_DISTILL(256, 2)
-    BNS_DISTILL(256, 4)
-    BNS_DISTILL(512, 4)
-    BNS_DISTILL(1024, 4)
-    BNS_DISTILL(1024, 8)
-    BNS_DISTILL(1024, 12)
-    BNS_DISTILL(1024, 16)
-    }
-#undef BNS_DISTILL
-    BNS_LAUNCH((distill_forward_kernel<T, 1024, 0>), grid, dim3(1024), 0, st, a);
+    if (a.vocab < Words<T>::kElems || words > 1024 * 16) launch_rows<T, 1024, 0>(a, st);
+    else if (words <= 256 * 2) launch_rows<T, 256, 2>(a, st);
+    else if (words <= 256 * 4) launch_rows<T, 256, 4>(a, st);
+    else if (words <= 512 * 4) launch_rows<T, 512, 4>(a, st);
+    else if (words <= 1024 * 4) launch_rows<T, 1024, 4>(a, st);
+    else if (words <= 1024 * 8) launch_rows<T, 1024, 8>(a, st);
+    else if (words <= 1024 * 12) launch_rows<T, 1024, 12>(a, st);
+    else launch_rows<T, 1024, 16>(a, st);
 }
 
 template <typename T>
 void launch_backward(DistillArgs a, hipStream_t st) {
-    // Segments of a whole row where the rows alone fill the device, else shorter ones; a block takes 256 x 4 words at a time.
-    const int64_t least = 256 * 4 * Words<T>::kElems, want = std::max<int64_t>(1, 2048 / std::max<int64_t>(a.tokens, 1));
+    // Segments of a whole row where the rows alone fill the device, else shorter ones, down to half of the 256 x 4 words that a block takes at a time.
+    const int64_t least = 256 * 2 * Words<T>::kElems, want = std::max<int64_t>(1, 2048 / std::max<int64_t>(a.tokens, 1));
     const int64_t segments = std::max<int64_t>(1, std::min<int64_t>(want, (a.vocab + least - 1) / least));
     a.segment = int32_t(round_up((a.vocab + segments - 1) / segments, 8));
     const int count = int((a.vocab + a.segment - 1) / a.segment);
-    BNS_LAUNCH((distill_backward_kernel<T>), dim3(uint32_t(std::min(a.tokens * count, kMostBlocks))), dim3(256), 0, st, a, count);
+    const dim3 grid(uint32_t(std::min(a.tokens * count, kMostBlocks)));
+    if (size_t(a.tokens) * a.vocab * sizeof(T) * 2 > kStreamBytes) BNS_LAUNCH((distill_backward_kernel<T, true>), grid, dim3(256), 0, st, a, count);
+    else BNS_LAUNCH((distill_backward_kernel<T, false>), grid, dim3(256), 0, st, a, count);
 }
 
 bns_status check_tensors(const bns_distill* distill, const DistillDims& d, const void* logits, const void* ids, const void* teacher, const void* dlogits) {

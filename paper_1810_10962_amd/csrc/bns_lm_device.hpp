@@ -4,6 +4,32 @@
 
 namespace bns {
 
+// Accesses with the non-temporal hint, for calls that move more than the memory-side cache holds anyway: lines that nobody will find there are not
+// kept (see kStreamBytes).
+typedef uint32_t words4_t __attribute__((ext_vector_type(4)));
+typedef words4_t words4_f32_t __attribute__((aligned(4)));
+typedef words4_t words4_bf16_t __attribute__((aligned(2)));
+template <bool NT>
+__device__ __forceinline__ words4_t get16(const float* p) {
+    if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const words4_f32_t*>(p));
+    else return *reinterpret_cast<const words4_f32_t*>(p);
+}
+template <bool NT>
+__device__ __forceinline__ words4_t get16(const bf16_t* p) {
+    if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const words4_bf16_t*>(p));
+    else return *reinterpret_cast<const words4_bf16_t*>(p);
+}
+template <bool NT>
+__device__ __forceinline__ void put16(float* p, words4_t v) {
+    if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<words4_f32_t*>(p));
+    else *reinterpret_cast<words4_f32_t*>(p) = v;
+}
+template <bool NT>
+__device__ __forceinline__ void put16(bf16_t* p, words4_t v) {
+    if constexpr (NT) __builtin_nontemporal_store(v, reinterpret_cast<words4_bf16_t*>(p));
+    else *reinterpret_cast<words4_bf16_t*>(p) = v;
+}
+
 // Eight neighbouring elements of a row, as floats.  A row may begin at any element, so the accesses are declared for element alignment: the
 // hardware takes 128 bits from any address, and those that happen to be aligned cost nothing extra.  The last vector of a row that is no
 // multiple of eight goes element by element.
@@ -23,10 +49,11 @@ struct Row8<float> {
             for (int i = 0; i < 8; ++i) f[i] = i < left ? p[i] : 0.f;
         }
     }
+    template <bool NT = false>
     static __device__ __forceinline__ void store(float* p, int left, const float (&f)[8]) {
         if (left >= 8) {
-            *reinterpret_cast<v4e*>(p) = v4{f[0], f[1], f[2], f[3]};
-            *reinterpret_cast<v4e*>(p + 4) = v4{f[4], f[5], f[6], f[7]};
+            put16<NT>(p, __builtin_bit_cast(words4_t, v4{f[0], f[1], f[2], f[3]}));
+            put16<NT>(p + 4, __builtin_bit_cast(words4_t, v4{f[4], f[5], f[6], f[7]}));
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -50,10 +77,10 @@ struct Row8<bf16_t> {
             for (int i = 0; i < 8; ++i) f[i] = i < left ? bf16_to_f32(p[i].bits) : 0.f;
         }
     }
+    template <bool NT = false>
     static __device__ __forceinline__ void store(bf16_t* p, int left, const float (&f)[8]) {
         if (left >= 8) {
-            const u4 v = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-            *reinterpret_cast<u4e*>(p) = v;
+            put16<NT>(p, u4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])});
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -68,11 +95,11 @@ struct Raw8;
 template <>
 struct Raw8<float> {
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    typedef u4 u4e __attribute__((aligned(4)));
     u4 a, b;
+    template <bool NT = false>
     __device__ __forceinline__ void load(const float* p) {
-        a = *reinterpret_cast<const u4e*>(p);
-        b = *reinterpret_cast<const u4e*>(p + 4);
+        a = get16<NT>(p);
+        b = get16<NT>(p + 4);
     }
     __device__ __forceinline__ void load_left(const float* p, int left) {       // the first `left` elements, zeros behind them
 #pragma unroll
@@ -90,9 +117,9 @@ struct Raw8<float> {
 template <>
 struct Raw8<bf16_t> {
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    typedef u4 u4e __attribute__((aligned(2)));
     u4 a;
-    __device__ __forceinline__ void load(const bf16_t* p) { a = *reinterpret_cast<const u4e*>(p); }
+    template <bool NT = false>
+    __device__ __forceinline__ void load(const bf16_t* p) { a = get16<NT>(p); }
     __device__ __forceinline__ void load_left(const bf16_t* p, int left) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = uint32_t(2 * i < left ? p[2 * i].bits : 0) | uint32_t(2 * i + 1 < left ? p[2 * i + 1].bits : 0) << 16;

@@ -8,6 +8,9 @@ inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; 
 inline size_t dtype_bytes(int32_t dtype) { return dtype == BNS_F32 ? 4 : 2; }
 inline bool known_dtype(int32_t dtype) { return dtype == BNS_F32 || dtype == BNS_BF16; }
 
+// A call that moves more than this between memory and the compute units finds nothing of it in the memory-side cache (256 MB) a second time.
+constexpr size_t kStreamBytes = size_t(224) << 20;
+
 // A row-major matrix as the overlap checks see it: the bytes from its first element to its last.
 struct Matrix {
     const void* p;

@@ -41,13 +41,13 @@ __device__ __forceinline__ void load_weight(const void* w, int bf16, int col, in
 }
 
 // Sum / maximum over the TPR threads of a row; `lds` holds a float for every wave, and two calls in a row are given two different ones.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* lds) {
+template <int TPR, typename F>
+__device__ __forceinline__ F row_sum(F v, F* lds) {
     v = wave_sum(v);
     if (TPR == kWave) return v;
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
     __syncthreads();
-    float s = 0.f;
+    F s = 0;
 #pragma unroll
     for (int i = 0; i < TPR / kWave; ++i) s += lds[i];
     return s;
@@ -67,7 +67,7 @@ __device__ __forceinline__ float row_max(float v, float* lds) {
 // The vectors of a row that a thread holds.  RAGGED: the width is no multiple of eight, so the last vector goes element by element.  Otherwise
 // a vector lies in the row or behind it, and what lies behind is read from the row's last vector and cleared: the loads stand in no branch,
 // so that all of them are on their way at once.
-template <typename T, int TPR, int VPT, bool RAGGED>
+template <typename T, int TPR, int VPT, bool RAGGED, bool NT>
 struct RowOf {
     Raw8<T> raw[RAGGED ? 1 : VPT];
     float f[RAGGED ? VPT : 1][8];
@@ -84,7 +84,7 @@ struct RowOf {
                     for (int i = 0; i < 8; ++i) f[j][i] = 0.f;
                 }
             } else {
-                raw[j].load(p + min(col, width - 8));
+                raw[j].template load<NT>(p + min(col, width - 8));
             }
         }
     }
@@ -101,6 +101,14 @@ struct RowOf {
     }
 };
 
+// Mean and eps with a rounding each, as the formula is written: scales that are rounded up to powers of two hang on the last bit of rstd, and an implementation of it by
+// elementary operations comes to the same one.
+__device__ __forceinline__ float mean_and_eps(float sum, float inv_width, float eps) {
+#pragma clang fp contract(off)
+    const float mean = sum * inv_width;
+    return mean + eps;
+}
+
 // The scale of values whose largest magnitude is `most`: see include/bns.h.
 __device__ __forceinline__ float e4m3_scale(float most, int pow2) {
     const float s = fmaxf(most * (1.f / 448.f), 0x1p-126f);
@@ -112,17 +120,19 @@ __device__ __forceinline__ float e4m3_scale(float most, int pow2) {
 template <int TPR>
 constexpr int block_of() { return TPR == kWave ? 256 : TPR; }
 
-template <typename T, int TPR, int VPT, bool RAGGED>
+template <typename T, int TPR, int VPT, bool RAGGED, bool NT>
 __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a) {
     constexpr int kRows = block_of<TPR>() / TPR;
-    __shared__ float lds[2][block_of<TPR>() / kWave];
+    __shared__ double sums[block_of<TPR>() / kWave];
+    __shared__ float maxima[block_of<TPR>() / kWave];
     const int t = threadIdx.x % TPR;
     for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / TPR; row < a.rows; row += int64_t(gridDim.x) * kRows) {
-        RowOf<T, TPR, VPT, RAGGED> x, r;
+        RowOf<T, TPR, VPT, RAGGED, NT> x, r;
         x.load(static_cast<const T*>(a.x) + row * a.x_stride, t, a.width);
         if (a.residual) r.load(static_cast<const T*>(a.residual) + row * a.residual_stride, t, a.width);
         float s[VPT][8];
-        float square = 0.f;
+        // (the squares of a vector are added in fp32, the vectors in fp64: the mean is as good as exact, for a dozen instructions)
+        double squares = 0.0;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             x.get(j, t, a.width, s[j]);
@@ -132,17 +142,19 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s[j][i] += f[i];
             }
+            float square = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) square = fmaf(s[j][i], s[j][i], square);
+            squares += double(square);
         }
-        const float rstd = __frsqrt_rn(fmaf(row_sum<TPR>(square, lds[0]), a.inv_width, a.eps));
+        const float rstd = rsqrtf(mean_and_eps(float(row_sum<TPR>(squares, sums)), a.inv_width, a.eps));
         if (a.rstd && t == 0) a.rstd[row] = rstd;
         if (a.sum) {
             T* out = static_cast<T*>(a.sum) + row * a.sum_stride;
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
                 const int col = (j * TPR + t) * 8;
-                if (col < a.width) Row8<T>::store(out + col, RAGGED ? a.width - col : 8, s[j]);
+                if (col < a.width) Row8<T>::template store<NT>(out + col, RAGGED ? a.width - col : 8, s[j]);
             }
         }
 #pragma unroll
@@ -160,7 +172,7 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
                 const int col = (j * TPR + t) * 8;
-                if (col < a.width) Row8<T>::store(y + col, RAGGED ? a.width - col : 8, s[j]);
+                if (col < a.width) Row8<T>::template store<NT>(y + col, RAGGED ? a.width - col : 8, s[j]);
             }
             if (TPR > kWave) __syncthreads();       // (the sums have been read)
             continue;
@@ -174,7 +186,7 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
             whole = fmaxf(whole, most[j]);
         }
         if (a.group == 0) {
-            whole = row_max<TPR>(whole, lds[1]);
+            whole = row_max<TPR>(whole, maxima);
 #pragma unroll
             for (int j = 0; j < VPT; ++j) most[j] = whole;
         } else {
@@ -204,7 +216,8 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
             if (left >= 8) {
                 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
                 typedef u2 u2e __attribute__((aligned(1)));
-                *reinterpret_cast<u2e*>(y + col) = u2{q[0], q[1]};
+                if constexpr (NT) __builtin_nontemporal_store((u2{q[0], q[1]}), reinterpret_cast<u2e*>(y + col));
+                else *reinterpret_cast<u2e*>(y + col) = u2{q[0], q[1]};
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -217,7 +230,7 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
 
 // dx of every row, and dweight as one partial sum for each block: a thread meets the same columns in every row,
 // so their sums stay in its registers.  The next row is asked for before the present one is worked on, where the registers hold both.
-template <typename T, int TPR, int VPT, bool RAGGED>
+template <typename T, int TPR, int VPT, bool RAGGED, bool NT>
 __global__ void __launch_bounds__(block_of<TPR>()) rms_backward_kernel(RmsBackwardArgs a) {
     constexpr int kRows = block_of<TPR>() / TPR;
     constexpr bool kAhead = TPR < 1024;
@@ -229,7 +242,7 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_backward_kernel(RmsBackwa
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) dw[j][i] = 0.f;
-    RowOf<T, TPR, VPT, RAGGED> next_x, next_dy, next_ds;
+    RowOf<T, TPR, VPT, RAGGED, NT> next_x, next_dy, next_ds;
     float next_rstd = 0.f;
     const auto ask = [&](int64_t row) {
         next_rstd = a.rstd[row];
@@ -241,7 +254,7 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_backward_kernel(RmsBackwa
     int turn = 0;
     for (int64_t row = first; row < a.rows; row += step, turn ^= 1) {
         if (!kAhead) ask(row);
-        const RowOf<T, TPR, VPT, RAGGED> x = next_x, dy = next_dy, ds = next_ds;
+        const RowOf<T, TPR, VPT, RAGGED, NT> x = next_x, dy = next_dy, ds = next_ds;
         const float rstd = next_rstd;
         if (kAhead && row + step < a.rows) ask(row + step);
         float xh[VPT][8], g[VPT][8];
@@ -280,7 +293,7 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_backward_kernel(RmsBackwa
             if (a.dsum) ds.get(j, t, a.width, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = fmaf(rstd, fmaf(-xh[j][i], mean, g[j][i]), f[i]);
-            Row8<T>::store(dx + col, RAGGED ? a.width - col : 8, f);
+            Row8<T>::template store<NT>(dx + col, RAGGED ? a.width - col : 8, f);
         }
     }
     if constexpr (kRows > 1) {                      // the waves of a block add theirs up first
@@ -356,9 +369,12 @@ int64_t backward_blocks(const RmsPlan& p, int64_t rows) {
     return std::min<int64_t>(std::max<int64_t>((rows + per_block - 1) / per_block, 1), 512);
 }
 
+// nt: with the non-temporal hint (8192x5120 bf16 to 8 bits 53.5 against 59.5 us, backward of 16384x4096 bf16 91 against 99; small calls lose, 777x1001 fp32
+// 10.2 against 9.4).
 #define BNS_RMS_CASE(T, KERNEL, TPR, VPT, THREADS)                                                                    \
-    if (a.width % 8) BNS_LAUNCH((KERNEL<T, TPR, VPT, true>), grid, dim3(THREADS), 0, st, a);                          \
-    else BNS_LAUNCH((KERNEL<T, TPR, VPT, false>), grid, dim3(THREADS), 0, st, a);                                     \
+    if (a.width % 8) BNS_LAUNCH((KERNEL<T, TPR, VPT, true, false>), grid, dim3(THREADS), 0, st, a);                   \
+    else if (nt) BNS_LAUNCH((KERNEL<T, TPR, VPT, false, true>), grid, dim3(THREADS), 0, st, a);                       \
+    else BNS_LAUNCH((KERNEL<T, TPR, VPT, false, false>), grid, dim3(THREADS), 0, st, a);                              \
     break;
 #define BNS_RMS_FORWARD(T)                                              \
     switch (p.tpr * 10 + p.vpt) {                                       \
@@ -409,6 +425,7 @@ bns_status bns_rms_forward(const bns_rms* rms, const void* x, const void* residu
     const RmsArgs a = {x, residual, weight, sum, y, scales, rstd, d.rows, d.x_stride, d.residual_stride, d.sum_stride, d.y_stride,
                        d.width, d.groups, rms->group, rms->weight_dtype == BNS_BF16, e4m3, rms->pow2_scales, rms->eps, 1.f / float(d.width)};
     const RmsPlan p = forward_plan(d.rows, d.width);
+    const bool nt = size_t(d.rows) * (row * (residual ? sum ? 3 : 2 : 1) + yrow) > kStreamBytes;
     const int per_block = p.tpr == kWave ? 4 : 1;
     const dim3 grid(uint32_t(std::min<int64_t>((d.rows + per_block - 1) / per_block, kMostBlocks)));
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -442,6 +459,7 @@ bns_status bns_rms_backward(const bns_rms* rms, const void* x, const void* weigh
     const RmsBackwardArgs a = {x, weight, dy, dsum, rstd, dx, static_cast<float*>(workspace), d.rows, d.x_stride, d.residual_stride, d.sum_stride,
                                d.y_stride, d.width, rms->weight_dtype == BNS_BF16, 1.f / float(d.width)};
     const RmsPlan p = backward_plan(d.width);
+    const bool nt = size_t(d.rows) * row * (dsum ? 4 : 3) > kStreamBytes;
     const int64_t blocks = backward_blocks(p, d.rows);
     const dim3 grid{uint32_t(blocks)};
     hipStream_t st = static_cast<hipStream_t>(stream);
