@@ -18,19 +18,19 @@ using namespace bns;
 
 namespace {
 
-template <typename T, int BM, int BN, int WM, int WN, int EPILOGUE>
-__global__ void __launch_bounds__(WM* WN* kWave) direct_logits_kernel(GemmArgs a) {
-    __shared__ __attribute__((aligned(16))) char lds[DirectTile<T, BM, BN, WM, WN>::kBytes];
-    direct_tile<T, BM, BN, WM, WN, true, true, EPILOGUE>(a, int(blockIdx.x), lds);
+template <typename T, int BM, int BN, int WM, int WN, int GROUPS, int EPILOGUE>
+__global__ void __launch_bounds__(256 * GROUPS) direct_logits_kernel(GemmArgs a) {
+    __shared__ __attribute__((aligned(16))) char lds[GROUPS * DirectTile<T, BM, BN, WM, WN>::kBytes];
+    direct_tile<T, BM, BN, WM, WN, GROUPS, true, true, EPILOGUE>(a, int(blockIdx.x), lds);
 }
 
 // Both gradients from g in one launch: the first blocks take dhidden, whose k is the vocabulary, the others dweight, whose k is the tokens.
-template <typename T, int BM, int BN, int WM, int WN, int BW, int EPILOGUE>
-__global__ void __launch_bounds__(256) direct_gradients_kernel(GemmArgs h, GemmArgs w, int blocks_h) {
+template <typename T, int BM, int BN, int WM, int WN, int BW, int GROUPS, int EPILOGUE>
+__global__ void __launch_bounds__(256 * GROUPS) direct_gradients_kernel(GemmArgs h, GemmArgs w, int blocks_h) {
     constexpr int kH = DirectTile<T, BM, BN, WM, WN>::kBytes, kW = DirectTile<T, BW, BW, 2, 2>::kBytes;
-    __shared__ __attribute__((aligned(16))) char lds[kH > kW ? kH : kW];
-    if (int(blockIdx.x) < blocks_h) direct_tile<T, BM, BN, WM, WN, false, true, EPILOGUE>(h, int(blockIdx.x), lds);
-    else direct_tile<T, BW, BW, 2, 2, false, false, kStore>(w, int(blockIdx.x) - blocks_h, lds);
+    __shared__ __attribute__((aligned(16))) char lds[GROUPS * (kH > kW ? kH : kW)];
+    if (int(blockIdx.x) < blocks_h) direct_tile<T, BM, BN, WM, WN, GROUPS, false, true, EPILOGUE>(h, int(blockIdx.x), lds);
+    else direct_tile<T, BW, BW, 2, 2, GROUPS, false, false, kStore>(w, int(blockIdx.x) - blocks_h, lds);
 }
 
 // ---- what follows the products --------------------------------------------------------------------------------------
@@ -148,7 +148,7 @@ inline Kind logits_kind(const HeadDims& d, bool backward) {
     const auto tiles = [&](int tile) { return int64_t(tiles_of(d.tokens, tile)) * tiles_of(d.vocab, tile); };
     // Fewer tiles of 64 than compute units: what counts is how long a block takes along the width, which kStream divides between its waves (fp32
     // 9x1792x1071 18 against 53, 226x1728x1148 46 against 66; bf16 11 against 16, but 26 against 20).
-    if (tiles(64) < 128 && d.width >= 512 && (f32 || d.tokens <= 64)) return kStream;
+    if (tiles(64) < 128 && d.width >= 512 && (f32 || d.tokens <= 32)) return kStream;
     const bool well = lies_well(d, d.hidden_stride) && lies_well(d, d.weight_stride);
     // Tiles of 256 need two rounds of blocks (bf16 4096x4096x16384 411 against 472, 1021x1000x32003 95 against 108; fp32 364 against 418), tokens that fill
     // them, and copies tokens that read them often (fp32 256x4096x32000 1447 against 438).
@@ -270,6 +270,13 @@ bool gemm(GemmArgs a, Kind kind, hipStream_t st) {
 // Tokens of a tile in the kernels that have several sizes.
 inline int token_tile(int tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : 64; }
 
+// Whether the steps of a tile of 64 are divided between four groups of waves: no more tiles than compute units, each with steps for all groups (bf16
+// 37x3712x12160 25 against 35 us, 226x1728x1148 16 against 18, but 386x3456x2389, 266 tiles, 40 against 36; gradients of 3155x68x3073 99 against 117).
+inline bool divide_steps(int blocks, int steps) {
+    if (g_tuning.head_groups) return g_tuning.head_groups == 1;
+    return blocks <= 256 && steps >= 16;
+}
+
 template <typename T, int EPILOGUE>
 bool logits(const HeadDims& d, const HeadPlan& p, GemmArgs a, hipStream_t st) {
     // (gt is written up to its depth, a multiple of 64 or 32)
@@ -281,10 +288,14 @@ bool logits(const HeadDims& d, const HeadPlan& p, GemmArgs a, hipStream_t st) {
     a.tiles_a = tiles_of(std::max(a.rows_a, a.g_depth), m);
     a.tiles_b = tiles_of(a.rows_b, n);
     const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b);
-    if (p.kind == kDirect128) BNS_LAUNCH((direct_logits_kernel<T, 128, 128, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64 && n == 16) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64 && n == 32) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
+    const bool groups = divide_steps(a.tiles_a * a.tiles_b, a.depth / DirectTile<T, 64, 64, 2, 2>::kDepth);
+    if (p.kind == kDirect128) BNS_LAUNCH((direct_logits_kernel<T, 128, 128, 2, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (p.kind == kDirect64 && n == 16 && groups) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && n == 16) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (p.kind == kDirect64 && n == 32 && groups) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && n == 32) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+    else if (p.kind == kDirect64 && groups) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (m == 16 && n == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (m == 16 && n == 32) BNS_LAUNCH((stream_logits_kernel<T, 1, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (m == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 4, EPILOGUE>), grid, dim3(256), 0, st, a);
@@ -343,10 +354,12 @@ bool direct_gradients(GemmArgs h, GemmArgs w, Kind kind, hipStream_t st) {
     w.tiles_b = tiles_of(w.rows_b, m);
     const int blocks_h = h.tiles_a * h.tiles_b * h.splits;
     const dim3 grid(uint32_t(blocks_h) + uint32_t(w.tiles_a) * w.tiles_b);
-    if (n == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else if (n == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else if (n == 64) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else BNS_LAUNCH((direct_gradients_kernel<T, 128, 128, 2, 2, 128, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    const bool groups = divide_steps(w.tiles_a * w.tiles_b, w.depth / DirectTile<T, 64, 64, 2, 2>::kDepth);
+    if (n == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else if (n == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else if (n == 64 && groups) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, 4, EPILOGUE>), grid, dim3(1024), 0, st, h, w, blocks_h);
+    else if (n == 64) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    else BNS_LAUNCH((direct_gradients_kernel<T, 128, 128, 2, 2, 128, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
     return !failed();
 }
 

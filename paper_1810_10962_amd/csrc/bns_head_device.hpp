@@ -15,16 +15,16 @@ template <typename T>
 constexpr int planes_of() { return sizeof(T) == 4 ? 3 : 1; }
 
 // ---- parts of an fp32 value ---------------------------------------------------------------------------------------
-// x = hi + mid + lo exactly, each of them the bf16 nearest to what is left (cut off instead where that would overflow).  Infinities and NaN are
-// hi alone.  A product of two values needs the six pairs of parts whose exponents reach into an fp32 result: what is dropped is
-// at most 2^-24 of it.
-__device__ __forceinline__ void split3(float x, uint32_t (&part)[3]) {
-    part[0] = f32_to_bf16(x);
-    if (fabsf(x) > 0x1.fep127f) part[0] = __float_as_uint(x) >> 16;
-    float r = x - bf16_to_f32(part[0]);
-    if (!(fabsf(r) < __builtin_inff())) r = 0.f;
-    part[1] = f32_to_bf16(r);
-    part[2] = f32_to_bf16(r - bf16_to_f32(part[1]));
+// x = hi + mid + lo exactly, each of them the bf16 nearest to what is left.  What is infinite or NaN as a bf16 (from 3.39e38 on) is hi alone.  A
+// product of two values needs the six pairs of parts whose exponents reach into an fp32 result: what is dropped is at most 2^-24 of it.
+// Two values at a time: word p holds part p of x0 in its lower half, of x1 in its upper one.
+__device__ __forceinline__ void split3(float x0, float x1, uint32_t (&word)[3]) {
+    word[0] = pack_bf16x2(x0, x1);
+    float r0 = x0 - __uint_as_float(word[0] << 16), r1 = x1 - __uint_as_float(word[0] & 0xffff0000u);
+    r0 = fabsf(r0) < __builtin_inff() ? r0 : 0.f;
+    r1 = fabsf(r1) < __builtin_inff() ? r1 : 0.f;
+    word[1] = pack_bf16x2(r0, r1);
+    word[2] = pack_bf16x2(r0 - __uint_as_float(word[1] << 16), r1 - __uint_as_float(word[1] & 0xffff0000u));
 }
 
 // Which pairs of planes an fp32 product takes, smallest first.
@@ -215,11 +215,14 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM /
                 const int m = m_base + r * kStride;
                 uint32_t part[kRun][NI][P];
 #pragma unroll
-                for (int x = 0; x < kRun; ++x)
+                for (int x = 0; x < kRun; x += 2)
 #pragma unroll
                     for (int j = 0; j < NI; ++j) {
-                        if constexpr (P == 1) part[x][j][0] = f32_to_bf16(at(r, j, x));
-                        else split3(at(r, j, x), part[x][j]);
+                        uint32_t word[3];
+                        if constexpr (P == 1) word[0] = pack_bf16x2(at(r, j, x), at(r, j, x + 1));
+                        else split3(at(r, j, x), at(r, j, x + 1), word);
+#pragma unroll
+                        for (int p = 0; p < P; ++p) part[x][j][p] = word[p] & 0xffffu, part[x + 1][j][p] = word[p] >> 16;
                     }
 #pragma unroll
                 for (int p = 0; p < P; ++p) {

@@ -2,7 +2,8 @@
 // into LDS fp32 values become three bf16 parts and columns become rows, so nothing is laid out beforehand; that work is done again in every tile that
 // reads an element, which is why large products prefer operands laid out once.
 //
-// A tile of BM x BN belongs to four waves.  The operands of the next steps of k are on their way from memory into registers while the present one is
+// A tile of BM x BN belongs to four waves, or, where there are few tiles, to GROUPS times four, each of which takes every GROUPS-th step of k; their sums are added at the
+// end, in a fixed order.  The operands of the next steps of k are on their way from memory into registers while the present one is
 // multiplied; LDS holds one step, so that several blocks share a compute unit and hide each other's waits.
 #pragma once
 #include "bns_head_device.hpp"
@@ -32,11 +33,11 @@ struct Feed {
 
     // Rows [row0, row0 + ROWS) of `rows`, k in [k0, k0 + DEPTH) of `depth`; what lies outside is zero (rows of a K_ROWS operand: any row, their
     // results are left out).
-    __device__ __forceinline__ void ask(const T* base, int64_t ld, int row0, int rows, int k0, int depth, const int64_t* targets) {
+    __device__ __forceinline__ void ask(int tid, const T* base, int64_t ld, int row0, int rows, int k0, int depth, const int64_t* targets) {
         const bool inside = k0 + DEPTH <= depth && (K_ROWS || row0 + ROWS <= rows);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int unit = i * THREADS + int(threadIdx.x);
+            const int unit = i * THREADS + tid;
             if (kUnits % THREADS != 0 && unit >= kUnits) break;
             if constexpr (K_ROWS) {
                 const int row = min(row0 + ROW(unit / kChunks), rows - 1), k = k0 + unit % kChunks * 8;
@@ -61,10 +62,10 @@ struct Feed {
         }
     }
 
-    __device__ __forceinline__ void put(char* lds, const int64_t* targets, int vocab) {
+    __device__ __forceinline__ void put(int tid, char* lds, const int64_t* targets, int vocab) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int unit = i * THREADS + int(threadIdx.x);
+            const int unit = i * THREADS + tid;
             if (kUnits % THREADS != 0 && unit >= kUnits) break;
             if constexpr (K_ROWS) {
                 const int to = at(unit / kChunks, unit % kChunks);
@@ -76,11 +77,10 @@ struct Feed {
                     u4 w[3];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        uint32_t lo[3], hi[3];
-                        split3(f[2 * j], lo);
-                        split3(f[2 * j + 1], hi);
+                        uint32_t word[3];
+                        split3(f[2 * j], f[2 * j + 1], word);
 #pragma unroll
-                        for (int p = 0; p < 3; ++p) w[p][j] = lo[p] | hi[p] << 16;
+                        for (int p = 0; p < 3; ++p) w[p][j] = word[p];
                     }
 #pragma unroll
                     for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(lds + p * kPlane + to) = w[p];
@@ -105,12 +105,11 @@ struct Feed {
                     raw[i][1].unpack(odd);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        uint32_t lo[3], hi[3];
-                        split3(even[j], lo);
-                        split3(odd[j], hi);
+                        uint32_t word[3];
+                        split3(even[j], odd[j], word);
 #pragma unroll
                         for (int p = 0; p < 3; ++p)
-                            *reinterpret_cast<uint32_t*>(lds + p * kPlane + at(SLOT(row + j), pair / 4) + pair % 4 * 4) = lo[p] | hi[p] << 16;
+                            *reinterpret_cast<uint32_t*>(lds + p * kPlane + at(SLOT(row + j), pair / 4) + pair % 4 * 4) = word[p];
                     }
                 }
             }
@@ -125,13 +124,17 @@ struct DirectTile {
 };
 
 // One tile of a product.  A_ROWS, B_ROWS: whether that operand's rows run along k (else m, n are its columns, and a.lda, a.ldb lead from one k to the next).
-template <typename T, int BM, int BN, int WM, int WN, bool A_ROWS, bool B_ROWS, int EPILOGUE>
+// `lds`: GROUPS times DirectTile::kBytes.
+template <typename T, int BM, int BN, int WM, int WN, int GROUPS, bool A_ROWS, bool B_ROWS, int EPILOGUE>
 __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* lds) {
     using S = DirectTile<T, BM, BN, WM, WN>;
     constexpr int P = S::P, D = S::kDepth, MI = BM / WM / 16, NI = BN / WN / 16;
+    static_assert(S::kThreads == 256 && MI * NI * int(sizeof(f32x4)) * 256 <= S::kBytes * (GROUPS > 1 ? 1 : 1000), "a group's sums fit its part of LDS");
     using FeedA = Feed<T, BM, D, A_ROWS, S::kThreads, row_m<MI>, slot_m<MI>>;
     using FeedB = Feed<T, BN, D, B_ROWS, S::kThreads, row_n<NI>, slot_n<NI>>;
-    char* const lds_b = lds + FeedA::kPlane * P;
+    const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(int(threadIdx.x) / 256) : 0, tid = GROUPS > 1 ? int(threadIdx.x) % 256 : int(threadIdx.x);
+    char* const lds_a = lds + group * S::kBytes;
+    char* const lds_b = lds_a + FeedA::kPlane * P;
     const int tiles = a.tiles_a * a.tiles_b, split = block / tiles, tile = block - split * tiles;
     int ta, tb;
     place(tile, tiles, a.tiles_a, a.tiles_b, ta, tb);
@@ -139,8 +142,8 @@ __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* 
     const int steps = (a.depth + D - 1) / D, first = int(int64_t(steps) * split / a.splits), end = int(int64_t(steps) * (split + 1) / a.splits);
     const T *pa = static_cast<const T*>(a.a), *pb = static_cast<const T*>(a.b);
     const int64_t* const targets = A_ROWS ? nullptr : a.targets;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, wm = wave / WN, wn = wave % WN, r16 = lane % 16, quarter = lane / 16;
-    constexpr int kAhead = BM * BN > 64 * 64 ? 1 : 2;       // steps on their way
+    const int lane = tid % kWave, wave = tid / kWave, wm = wave / WN, wn = wave % WN, r16 = lane % 16, quarter = lane / 16;
+    constexpr int kAhead = BM * BN > 64 * 64 || (GROUPS > 1 && P > 1) ? 1 : 2;      // steps on their way, as far as registers go
     FeedA fa[kAhead];
     FeedB fb[kAhead];
     f32x4 acc[MI][NI];
@@ -149,21 +152,25 @@ __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* 
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const auto ask = [&](int u, int step) {
-        fa[u].ask(pa, a.lda, m0, a.rows_a, step * D, a.depth, targets);
-        fb[u].ask(pb, a.ldb, n0, a.rows_b, step * D, a.depth, nullptr);
+        fa[u].ask(tid, pa, a.lda, m0, a.rows_a, step * D, a.depth, targets);
+        fb[u].ask(tid, pb, a.ldb, n0, a.rows_b, step * D, a.depth, nullptr);
     };
 #pragma unroll
     for (int u = 0; u < kAhead; ++u)
-        if (first + u < end) ask(u, first + u);
-    for (int at = first; at < end; at += kAhead) {
+        if (first + group + GROUPS * u < end) ask(u, first + group + GROUPS * u);
+    for (int at = first; at < end; at += GROUPS * kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (at + u >= end) break;
-            __syncthreads();                    // (the step before has been read)
-            fa[u].put(lds, targets, a.vocab);
-            fb[u].put(lds_b, nullptr, 0);
+            const int base = at + GROUPS * u, step = base + group;
+            if (base >= end) break;                 // (the same for all groups, which meet twice a step)
+            __syncthreads();                        // (the step before has been read)
+            if (step < end) {
+                fa[u].put(tid, lds_a, targets, a.vocab);
+                fb[u].put(tid, lds_b, nullptr, 0);
+            }
             __syncthreads();
-            if (at + u + kAhead < end) ask(u, at + u + kAhead);
+            if (step >= end) continue;
+            if (step + GROUPS * kAhead < end) ask(u, step + GROUPS * kAhead);
 #pragma unroll
             for (int kk = 0; kk < D / 32; ++kk) {
                 bf16x8 x[MI][P], y[NI][P];
@@ -174,7 +181,7 @@ __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* 
                         y[j][p] = *reinterpret_cast<const bf16x8*>(lds_b + p * FeedB::kPlane + FeedB::at(wn * (BN / WN) + j * 16 + r16, kk * 4 + quarter));
 #pragma unroll
                     for (int i = 0; i < MI; ++i)
-                        x[i][p] = *reinterpret_cast<const bf16x8*>(lds + p * FeedA::kPlane + FeedA::at(wm * (BM / WM) + i * 16 + r16, kk * 4 + quarter));
+                        x[i][p] = *reinterpret_cast<const bf16x8*>(lds_a + p * FeedA::kPlane + FeedA::at(wm * (BM / WM) + i * 16 + r16, kk * 4 + quarter));
                 }
 #pragma unroll
                 for (int s = P == 1 ? 5 : 0; s < 6; ++s)
@@ -184,6 +191,31 @@ __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* 
                         for (int j = 0; j < NI; ++j)
                             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][plane_a(s)], y[j][plane_b(s)], acc[i][j], 0, 0, 0);
             }
+        }
+    }
+    if constexpr (GROUPS > 1) {
+        __syncthreads();
+        if (group > 0) {
+            f32x4* const sums = reinterpret_cast<f32x4*>(lds_a);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) sums[(i * NI + j) * 256 + tid] = acc[i][j];
+        }
+        __syncthreads();
+        if (group > 0) {
+            if constexpr (EPILOGUE == kStatistics && WM > 1) {      // finish() meets twice
+                __syncthreads();
+                __syncthreads();
+            }
+            return;
+        }
+        for (int g = 1; g < GROUPS; ++g) {
+            const f32x4* const sums = reinterpret_cast<const f32x4*>(lds + g * S::kBytes);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) acc[i][j] += sums[(i * NI + j) * 256 + tid];
         }
     }
     finish<T, EPILOGUE, BM, BN, WM, WN>(a, acc, ta, tb, split, reinterpret_cast<float2*>(lds));

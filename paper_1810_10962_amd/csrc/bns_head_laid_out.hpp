@@ -37,11 +37,10 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) {
             u4 w[3];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                uint32_t lo[3], hi[3];
-                split3(f[2 * j], lo);
-                split3(f[2 * j + 1], hi);
+                uint32_t word[3];
+                split3(f[2 * j], f[2 * j + 1], word);
 #pragma unroll
-                for (int p = 0; p < 3; ++p) w[p][j] = lo[p] | hi[p] << 16;
+                for (int p = 0; p < 3; ++p) w[p][j] = word[p];
             }
 #pragma unroll
             for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(out + int64_t(p) * a.depth) = w[p];
@@ -83,11 +82,10 @@ __global__ void __launch_bounds__(256) pack_columns_kernel(PackArgs a) {
             u4 w[3];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                uint32_t lo[3], hi[3];
-                split3(tile[r + 2 * i][c], lo);
-                split3(tile[r + 2 * i + 1][c], hi);
+                uint32_t word[3];
+                split3(tile[r + 2 * i][c], tile[r + 2 * i + 1][c], word);
 #pragma unroll
-                for (int p = 0; p < 3; ++p) w[p][i] = lo[p] | hi[p] << 16;
+                for (int p = 0; p < 3; ++p) w[p][i] = word[p];
             }
 #pragma unroll
             for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(out + int64_t(p) * a.depth) = w[p];

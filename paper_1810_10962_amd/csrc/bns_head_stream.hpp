@@ -31,11 +31,10 @@ __device__ __forceinline__ void to_parts(const Raw8<float>& r, u4 (&w)[3]) {
     r.unpack(f);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        uint32_t lo[3], hi[3];
-        split3(f[2 * j], lo);
-        split3(f[2 * j + 1], hi);
+        uint32_t word[3];
+        split3(f[2 * j], f[2 * j + 1], word);
 #pragma unroll
-        for (int p = 0; p < 3; ++p) w[p][j] = lo[p] | hi[p] << 16;
+        for (int p = 0; p < 3; ++p) w[p][j] = word[p];
     }
 }
 // Column f of eight rows, the rows being neighbours along k.
@@ -49,11 +48,10 @@ __device__ __forceinline__ void column_parts(const Raw8<bf16_t> (&r)[8], int f, 
 __device__ __forceinline__ void column_parts(const Raw8<float> (&r)[8], int f, u4 (&w)[3]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        uint32_t lo[3], hi[3];
-        split3(__uint_as_float(f < 4 ? r[2 * j].a[f % 4] : r[2 * j].b[f % 4]), lo);
-        split3(__uint_as_float(f < 4 ? r[2 * j + 1].a[f % 4] : r[2 * j + 1].b[f % 4]), hi);
+        uint32_t word[3];
+        split3(__uint_as_float(f < 4 ? r[2 * j].a[f % 4] : r[2 * j].b[f % 4]), __uint_as_float(f < 4 ? r[2 * j + 1].a[f % 4] : r[2 * j + 1].b[f % 4]), word);
 #pragma unroll
-        for (int p = 0; p < 3; ++p) w[p][j] = lo[p] | hi[p] << 16;
+        for (int p = 0; p < 3; ++p) w[p][j] = word[p];
     }
 }
 

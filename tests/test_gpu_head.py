@@ -16,8 +16,8 @@ pytestmark = pytest.mark.gpu
 
 # Kernels of the forward pass's logits, the backward pass's and the gradients' products: see "head_logits" and the options behind it.
 PATHS = {"few": (1, 1, 1), "few_direct": (1, 1, 2), "direct64": (2, 2, 2), "direct64_few": (2, 2, 1), "direct128": (3, 3, 3), "laid_out256": (4, 4, 4), "laid_out128": (5, 5, 5),
-         "mixed": (5, 1, 4), "mixed2": (4, 3, 5), "auto": (0, 0, 0)}
-OPTIONS = ("head_logits", "head_logits_backward", "head_gradients")
+         "mixed": (5, 1, 4), "mixed2": (4, 3, 5), "divided64": (2, 2, 2, 1), "auto": (0, 0, 0)}
+OPTIONS = ("head_logits", "head_logits_backward", "head_gradients", "head_groups")
 
 
 @pytest.fixture(params=PATHS)
