@@ -2,8 +2,8 @@
 // include/bns.h for the equations.
 //
 // Both read every logit once and write every gradient once, so HBM bounds them.  Forward: a block takes a row and keeps it in registers
-// as it is stored (256 KB of the 512 KB of a compute unit), so that maximum, sum and gradient come from one read; longer rows are read
-// again, which the memory-side cache serves.  Wave 0 works the teacher's distribution out while the row is on its way.  The gradient is
+// as it is stored (256 KB of the 512 KB of a compute unit), so that maximum, sum and gradient come from one read; of longer rows the
+// rest is read again, which the memory-side cache serves.  Wave 0 works the teacher's distribution out while the row is on its way.  The gradient is
 // written as if the teacher were not there, then the few elements that it touches once more.
 #include <hip/hip_runtime.h>
 
@@ -180,11 +180,12 @@ __device__ __forceinline__ void keep_packed(u4 (&w)[N]) {
     for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
 }
 
-// NV: 16-byte words per thread that hold the row; 0: the row is read again.  NT: with the non-temporal hint (4096x131072 bf16 with its gradient 400 against
+// NV: 16-byte words per thread that hold the row, or with REST its beginning; what lies behind is read again (NV = 0: rows shorter than a word).  NT: with the non-temporal hint (4096x131072 bf16 with its gradient 400 against
 // 416 us, gradient of 2048x50304 fp32 162 against 172; 7x100003 bf16 6.7 against 6.4).
-template <typename T, int THREADS, int NV, bool NT>
+template <typename T, int THREADS, int NV, bool REST, bool NT>
 __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a) {
-    constexpr int E = Words<T>::kElems, kWaves = THREADS / kWave;
+    constexpr int E = Words<T>::kElems, kWaves = THREADS / kWave, kHeld = NV * THREADS * E;
+    static_assert(NV > 0 || REST, "somebody takes the row");
     __shared__ Teacher teacher;
     __shared__ float part[2][kWaves];
     const int tid = threadIdx.x, wave = tid / kWave;
@@ -194,7 +195,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
         Entry entry;
         if (wave == 0) entry.ask(a, row, tid);
         u4 held[NV > 0 ? NV : 1];
-        // The row's last word is moved back so that it ends with the row, and so are those behind it: all are on their way before any is
+        // Without REST the row's last word is moved back so that it ends with the row, and so are those behind it: all are on their way before any is
         // looked at.  What they hold twice does not change a maximum, is left out of the sum and written twice with the same bits.
         int t = tid;        // (opaque, here and before each use: nothing that follows from it is kept in registers from row to row)
         asm volatile("" : "+v"(t));
@@ -202,44 +203,16 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int v = (j * THREADS + t) * E;
-                held[j] = Words<T>::template load<NT>(z + min(v, a.vocab - E), E);
+                held[j] = Words<T>::template load<NT>(z + (REST ? v : min(v, a.vocab - E)), E);
             }
         }
         if (wave == 0) work_teacher(teacher, a, row, entry, z, 0, a.vocab, true);
         // maximum of z / tau in powers of two, and sum of exp2 of what lies below it; a wave that meets only -infinity has a finite maximum
-        float m = -__builtin_inff(), l = 0.f;
-        if (NV > 0) {
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                float f[E];
-                Words<T>::unpack(held[j], f);
-#pragma unroll
-                for (int i = 0; i < E; ++i) m = fmaxf(m, f[i]);
-                __builtin_amdgcn_sched_barrier(0);      // (registers: one word's values at a time)
-            }
-            m = fmaxf(wave_max(m) * c, kLeast);
-            keep_packed(held);
-            asm volatile("" : "+v"(t));
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                float f[E];
-                Words<T>::unpack(held[j], f);
-#pragma unroll
-                for (int i = 0; i < E; ++i) f[i] = __builtin_amdgcn_exp2f(fmaf(f[i], c, -m));
-                if ((j + 1) * THREADS * E > a.vocab) {
-                    const int twice = (j * THREADS + t + 1) * E - a.vocab;
-#pragma unroll
-                    for (int i = 0; i < E; ++i) f[i] = i < twice ? 0.f : f[i];
-                }
-#pragma unroll
-                for (int i = 0; i < E; ++i) l += f[i];
-                asm volatile("" : "+v"(l));             // (added here and now, for the same reason)
-            }
-        } else {
-            m = kLeast;
-            for (int v = tid * E; v < a.vocab; v += THREADS * E) {
+        float m = kLeast, l = 0.f;
+        if (REST) {
+            for (int v = kHeld + tid * E; v < a.vocab; v += THREADS * E) {
                 float f[E], most = -__builtin_inff();
-                Words<T>::unpack(Words<T>::template load<NT>(z + v, a.vocab - v), f);
+                Words<T>::unpack(Words<T>::template load<false>(z + v, a.vocab - v), f);
 #pragma unroll
                 for (int i = 0; i < E; ++i) most = fmaxf(most, f[i]);
                 most = fmaxf(m, most * c);
@@ -248,9 +221,40 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
 #pragma unroll
                 for (int i = 0; i < E; ++i) l += __builtin_amdgcn_exp2f(fmaf(f[i], c, -m));
             }
-            const float most = wave_max(m);
-            l *= __builtin_amdgcn_exp2f(m - most);
-            m = most;
+        }
+        float most = -__builtin_inff();
+        if (NV > 0) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float f[E];
+                Words<T>::unpack(held[j], f);
+#pragma unroll
+                for (int i = 0; i < E; ++i) most = fmaxf(most, f[i]);
+                __builtin_amdgcn_sched_barrier(0);      // (registers: one word's values at a time)
+            }
+            most *= c;
+        }
+        most = wave_max(fmaxf(most, m));
+        l *= __builtin_amdgcn_exp2f(m - most);
+        m = most;
+        if (NV > 0) {
+            keep_packed(held);
+            asm volatile("" : "+v"(t));
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float f[E];
+                Words<T>::unpack(held[j], f);
+#pragma unroll
+                for (int i = 0; i < E; ++i) f[i] = __builtin_amdgcn_exp2f(fmaf(f[i], c, -m));
+                if (!REST && (j + 1) * THREADS * E > a.vocab) {
+                    const int twice = (j * THREADS + t + 1) * E - a.vocab;
+#pragma unroll
+                    for (int i = 0; i < E; ++i) f[i] = i < twice ? 0.f : f[i];
+                }
+#pragma unroll
+                for (int i = 0; i < E; ++i) l += f[i];
+                asm volatile("" : "+v"(l));             // (added here and now, for the same reason)
+            }
         }
         l = wave_sum(l);
         if (tid % kWave == 0) {
@@ -286,11 +290,12 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
                     const int v = (j * THREADS + t) * E;
-                    if (v < a.vocab) write(min(v, a.vocab - E), held[j], E);
+                    if (REST || v < a.vocab) write(REST ? v : min(v, a.vocab - E), held[j], E);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-            } else {
-                for (int v = tid * E; v < a.vocab; v += THREADS * E) write(v, Words<T>::template load<NT>(z + v, a.vocab - v), a.vocab - v);
+            }
+            if (REST) {
+                for (int v = kHeld + tid * E; v < a.vocab; v += THREADS * E) write(v, Words<T>::template load<false>(z + v, a.vocab - v), a.vocab - v);
             }
             __syncthreads();
             if (some) fix_entries(teacher, a, out, 0, a.vocab, lse2, scale);
@@ -345,26 +350,27 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, in
 
 constexpr int64_t kMostBlocks = int64_t(1) << 20;
 
-template <typename T, int THREADS, int NV>
+template <typename T, int THREADS, int NV, bool REST = false>
 void launch_rows(const DistillArgs& a, hipStream_t st) {
     const dim3 grid(uint32_t(std::min(a.tokens, kMostBlocks)));
-    if (size_t(a.tokens) * a.vocab * sizeof(T) * (a.dlogits ? 2 : 1) > kStreamBytes && NV > 0)
-        BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV, (NV > 0)>), grid, dim3(THREADS), 0, st, a);
-    else BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV, false>), grid, dim3(THREADS), 0, st, a);
+    if (size_t(a.tokens) * a.vocab * sizeof(T) * (a.dlogits ? 2 : 1) > kStreamBytes)
+        BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV, REST, true>), grid, dim3(THREADS), 0, st, a);
+    else BNS_LAUNCH((distill_forward_kernel<T, THREADS, NV, REST, false>), grid, dim3(THREADS), 0, st, a);
 }
 
 // The smallest block that holds a row.
 template <typename T>
 void launch_forward(const DistillArgs& a, hipStream_t st) {
     const int64_t words = (a.vocab + Words<T>::kElems - 1) / Words<T>::kElems;
-    if (a.vocab < Words<T>::kElems || words > 1024 * 16) launch_rows<T, 1024, 0>(a, st);
+    if (a.vocab < Words<T>::kElems) launch_rows<T, 64, 0, true>(a, st);
     else if (words <= 256 * 2) launch_rows<T, 256, 2>(a, st);
     else if (words <= 256 * 4) launch_rows<T, 256, 4>(a, st);
     else if (words <= 512 * 4) launch_rows<T, 512, 4>(a, st);
     else if (words <= 1024 * 4) launch_rows<T, 1024, 4>(a, st);
     else if (words <= 1024 * 8) launch_rows<T, 1024, 8>(a, st);
     else if (words <= 1024 * 12) launch_rows<T, 1024, 12>(a, st);
-    else launch_rows<T, 1024, 16>(a, st);
+    else if (words <= 1024 * 16) launch_rows<T, 1024, 16>(a, st);
+    else launch_rows<T, 1024, 16, true>(a, st);
 }
 
 template <typename T>

@@ -150,9 +150,9 @@ inline Kind logits_kind(const HeadDims& d, bool backward) {
     // 9x1792x1071 18 against 53, 226x1728x1148 46 against 66; bf16 11 against 16, but 26 against 20).
     if (tiles(64) < 128 && d.width >= 512 && (f32 || d.tokens <= 32)) return kStream;
     const bool well = lies_well(d, d.hidden_stride) && lies_well(d, d.weight_stride);
-    // Tiles of 256 need two rounds of blocks (bf16 4096x4096x16384 411 against 472, 1021x1000x32003 95 against 108; fp32 364 against 418), tokens that fill
-    // them, and copies tokens that read them often (fp32 256x4096x32000 1447 against 438).
-    if (tiles(256) >= 400 && d.tokens > (well ? 192 : 1000)) return kGemm256;
+    // Tiles of 256 need two rounds of blocks (bf16 4096x4096x16384 411 against 472) and tokens that fill them; copies need many uses of what they lay out
+    // (fp32 4096x4096x16384 2607 against 2711, but bf16 1068x110x102656 190 against 121).
+    if (tiles(256) >= 400 && (well ? d.tokens > 192 : d.tokens >= 2048 && d.width >= 1024)) return kGemm256;
     // Without copies the laid-out kernels win as soon as they have the blocks (1024x1024x8192 25 against 30; 226x1728x1148 23 against 20).
     if (well && d.tokens > 32 && tiles(128) >= 128) return kGemm128;
     // fp32 256x512x32000 60 against 89, 1663x128x1920 19 against 18
@@ -169,11 +169,13 @@ inline Kind gradients_kind(const HeadDims& d) {
     // bf16 16x2048x50257 135 against 178, 2x384x85765 48 against 64, 40x1024x4096 29 against 24; fp32 1x3520x87977 999 against 1085, 16x2048x50257 400 against 393
     if (few && matrix >= (int64_t(1) << (f32 ? 27 : 23))) return kStream;
     const double work = double(matrix) * double(d.tokens);
-    // Laying operands out pays where each of them is read many times: bf16 512x2048x8192 99 against 120, 256x4096x32000 492 against 397; fp32
-    // 1021x1000x32003 1243 against 1444, 1024x1024x8192 344 against 341.
-    if (d.tokens >= 512 && work >= (f32 ? 3e10 : 5e9)) return d.tokens >= (f32 ? 1000 : 2048) && d.width >= (f32 ? 1000 : 2048) ? kGemm256 : kGemm128;
-    // bf16 256x4096x32000 397 against 446, 256x512x32000 86 against 77; fp32 40x1024x4096 41 against 51, 9x1792x1071 35 against 30, 1663x128x1920 152 against 130
-    if (f32 ? d.width >= 192 && matrix >= (int64_t(1) << 21) : work >= 1.5e10) return kDirect128;
+    // Laying operands out pays where each of them is read many times: bf16 512x2048x8192 97 against 124, 2853x576x2248 79 against 96, but 256x4096x32000
+    // 492 against 397 and 1024x256x32000 141 against 119; fp32 4096x4096x16384 7989 against 8615, but 1024x1024x8192 331 against 301.
+    const bool often = f32 ? d.tokens >= 1000 && work >= 3e10 : (d.tokens >= 512 && d.width >= 512 && work >= 5e9) || (d.tokens >= 2048 && work >= 1e9);
+    if (often) return d.tokens >= (f32 ? 1000 : 2048) && d.width >= (f32 ? 1000 : 2048) ? kGemm256 : kGemm128;
+    // bf16 256x4096x32000 397 against 446, 256x512x32000 86 against 77; fp32 40x1024x4096 36 against 42, 374x68x130472 358 against 518, but 9x1792x1071 30
+    // against 25, 1068x110x102656 1289 against 1190
+    if (f32 ? matrix >= (int64_t(1) << 21) && (d.width >= 192 || d.tokens < 512) : work >= 1.5e10) return kDirect128;
     return kDirect64;
 }
 
@@ -376,8 +378,8 @@ bool stream_gradients(GemmArgs h, GemmArgs w, hipStream_t st) {
 
 template <typename T>
 bool forward(const HeadDims& d, const HeadPlan& p, const void* hidden, const void* weight, const int64_t* targets, float* loss, float* lse, char* ws, hipStream_t st) {
-    // (without copies the whole vocabulary is one piece, as far as a launch goes: 2^22 blocks)
-    const int64_t most = std::max<int64_t>(1, (1 << 22) / ((d.tokens + 15) / 16)) * 256, step = p.copy_w ? p.piece : std::min<int64_t>(d.vocab, most);
+    // (without copies the whole vocabulary is one piece, as far as a launch goes)
+    const int64_t most = std::max<int64_t>(1, (1 << 20) / ((d.tokens + 15) / 16)) * 256, step = p.copy_w ? p.piece : std::min<int64_t>(d.vocab, most);
     for (int64_t v0 = 0; v0 < d.vocab; v0 += step) {
         GemmArgs a = {};
         if (!logits_operands<T>(d, p, hidden, weight, targets, ws, v0, int(std::min<int64_t>(step, d.vocab - v0)), st, &a)) return false;
