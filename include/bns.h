@@ -341,6 +341,12 @@ bns_status bns_copy_reference(void* dst, const void* src, size_t bytes, void* st
  *   "norm_nt", "dx_nt"   non-temporal access mask + 1: bit 0 loads, bit 1 stores
  *   "reduce_nt"      the same for the backward reduction: bit 0 loads of x, bit 1 loads of dy, for the channels
  *                    that "cache_reuse" keeps (the others are loaded non-temporally)
+ * The loss over the vocabulary (bns_head_*; the workspace depends on them, so they are set before it is asked for):
+ *   "head_logits", "head_logits_backward"   kernels of the logits in the forward and in the backward pass, "head_gradients" those of the two
+ *                    gradients: 1 few tokens (gradients: from 33 tokens in fp32, 65 in bf16 on the choice by size holds), 2 / 3 operands read as they
+ *                    lie in memory, tiles of 64 / 128, 4 / 5 operands laid out first, tiles of 256 / 128; 0: by size.  (Logits of 4 and 5 in the
+ *                    backward pass need gradients of 1, 4 or 5; with others 3 takes their place.)
+ *   "head_groups"    tiles of 64 share the steps along the summed dimension out between four groups of waves: 1 always, 2 never; 0: by size
  * Three more exist for the library's own tests only; they make results wrong on purpose and a caller has no
  * use for them:
  *   "test_spin_limit"    polls a block of a fused kernel waits for a team-mate's sums before it gives up
@@ -440,6 +446,7 @@ size_t bns_head_workspace_bytes(const bns_head* head);
 /* Softmax cross entropy of the logits z = hidden weight^T, which are never stored whole:
  *   lse[t] = log sum over v of exp(z[t][v])              loss[t] = lse[t] - z[t][targets[t]]
  * A token whose target lies outside [0, vocab) is left out: its loss is 0 (its lse is not).
+ * Logits of -infinity count for nothing in the sum; a token with a logit that is NaN or +infinity has a loss that is NaN (or infinite).
  * Products of bf16 are summed in fp32; f32 operands enter the matrix units as three bf16 parts each, the six products
  * that reach an fp32 result's last bits.
  * in: hidden[tokens][width], weight[vocab][width], targets[tokens].  out: loss[tokens], lse[tokens]. */
@@ -469,14 +476,16 @@ typedef struct {
 /* Distillation from a teacher's top logits.  With tau = temperature, over the row's entries j whose id lies in [0, vocab):
  *   q = softmax(teacher / tau)        p = softmax(logits / tau) over the vocabulary        lse = log sum exp(logits / tau)
  *   loss[t] = tau^2 * sum over j of q_j (log q_j - log p[id_j])
- * A row without such an entry has loss 0 and gradient 0.  An id may occur more than once: its q add up in the gradient.
+ * A row without such an entry has loss 0 and gradient 0, whatever its logits hold.  An id may occur more than once: its q add up in the gradient.
+ * A teacher's logit of -infinity is no entry; one that is NaN or +infinity makes its row NaN, and so does a logit of the student that is.  A student's
+ * logit of -infinity has p = 0; with q > 0 there the loss is infinite.
  * dlogits = tau * dloss[t] * (p - q), in the same pass over the logits, where dlogits is given (then dloss is needed too).
  * in: logits[tokens][vocab], ids[tokens][k], teacher[tokens][k] (dense), dloss[tokens] (NULL without dlogits).
  * out: loss[tokens], lse[tokens], dlogits (may be NULL).  In place: dlogits on logits. */
 bns_status bns_distill_forward(const bns_distill* distill, const void* logits, const int64_t* ids, const float* teacher,
                                const float* dloss, float* loss, float* lse, void* dlogits, void* stream);
 
-/* The gradient on its own, from the lse of the forward call.
+/* The gradient on its own, from the lse of the forward call (probabilities carry its rounding, 2^-24 of |lse|; the forward call's own gradient does not).
  * in: logits, ids, teacher, lse, dloss.  out: dlogits.  In place: dlogits on logits. */
 bns_status bns_distill_backward(const bns_distill* distill, const void* logits, const int64_t* ids, const float* teacher,
                                 const float* lse, const float* dloss, void* dlogits, void* stream);

@@ -18,7 +18,7 @@ using namespace bns;
 namespace {
 
 constexpr int kMostEntries = 1024;
-constexpr float kLeast = -3e38f;
+constexpr float kLeast = -3.40282347e38f;      // the lowest finite value: a maximum of only -infinity is this, one of rows masked with it is exact
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct DistillArgs {
@@ -96,7 +96,8 @@ struct Teacher {
     alignas(16) int32_t id[kMostEntries];   // -1: no entry
     alignas(16) float q[kMostEntries];      // (0 from entry k on to a multiple of four)
     float z[kMostEntries];                  // the student's logit there (only of ids in [v0, v1))
-    float cross;                            // sum q (log q - z / tau)
+    float cross;                            // sum q (log q - (z - z0) / tau)
+    float z0;                               // the student's largest logit at the entries
     int32_t some;                           // whether the row has an entry
 };
 
@@ -116,7 +117,7 @@ template <typename T>
 __device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, int64_t row, const Entry& first, const T* logits, int v0, int v1, bool cross) {
     const int lane = threadIdx.x;
     const float c = kLog2e / a.tau;
-    float most = -__builtin_inff();
+    float most = -__builtin_inff(), z0 = kLeast;
     bool some = false;
     for (int j = lane; j < (a.k + 3) / 4 * 4; j += kWave) {
         Entry e = first;
@@ -128,12 +129,16 @@ __device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, i
         s.id[j] = valid ? int32_t(e.id) : -1;
         s.q[j] = e.u;
         if (valid) {
-            if (e.id >= v0 && e.id < v1) s.z[j] = load_scalar<T>(logits + e.id);
+            if (e.id >= v0 && e.id < v1) {
+                s.z[j] = load_scalar<T>(logits + e.id);
+                z0 = fmaxf(z0, s.z[j]);
+            }
             some = true;
             most = fmaxf(most, e.u);
         }
     }
-    most = fmaxf(wave_max(most), -3e38f);
+    most = fmaxf(wave_max(most), kLeast);
+    if (cross) z0 = wave_max(z0);
     float sum = 0.f;
     for (int j = lane; j < a.k; j += kWave)
         if (s.id[j] >= 0) sum += __builtin_amdgcn_exp2f((s.q[j] - most) * c);
@@ -146,20 +151,20 @@ __device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, i
         }
         const float e = (s.q[j] - most) * c, q = __builtin_amdgcn_exp2f(e) * inv;
         s.q[j] = q;
-        if (cross && !(q == 0.f)) x += q * ((e - log2_total) * kLn2 - s.z[j] / a.tau);
+        if (cross && !(q == 0.f)) x += q * ((e - log2_total) * kLn2 - (s.z[j] - z0) / a.tau);
     }
     x = cross ? wave_sum(x) : 0.f;
     const bool any = __any(some);
     if (lane == 0) {
         s.cross = x;
+        s.z0 = z0;
         s.some = any;
     }
 }
 
 // The gradient where the teacher has entries: what all entries of one id add up to is taken off the student's probability.
-template <typename T>
-__device__ __forceinline__ void fix_entries(const Teacher& s, const DistillArgs& a, T* dlogits, int v0, int v1, float lse2, float scale) {
-    const float c = kLog2e / a.tau;
+template <typename T, typename P>
+__device__ __forceinline__ void fix_entries(const Teacher& s, const DistillArgs& a, T* dlogits, int v0, int v1, float scale, P probability) {
     for (int j = threadIdx.x; j < a.k; j += blockDim.x) {
         const int id = s.id[j];
         if (id < v0 || id >= v1) continue;
@@ -169,7 +174,7 @@ __device__ __forceinline__ void fix_entries(const Teacher& s, const DistillArgs&
             const float4 qs = *reinterpret_cast<const float4*>(s.q + i);
             q += (ids.x == id ? qs.x : 0.f) + (ids.y == id ? qs.y : 0.f) + (ids.z == id ? qs.z : 0.f) + (ids.w == id ? qs.w : 0.f);
         }
-        Words<T>::put_one(dlogits + id, scale * (__builtin_amdgcn_exp2f(fmaf(s.z[j], c, -lse2)) - q));
+        Words<T>::put_one(dlogits + id, scale * (probability(s.z[j]) - q));
     }
 }
 
@@ -189,7 +194,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
     __shared__ Teacher teacher;
     __shared__ float part[2][kWaves];
     const int tid = threadIdx.x, wave = tid / kWave;
-    const float c = kLog2e / a.tau;
+    const float inv_tau = 1.f / a.tau, c = kLog2e / a.tau;
     for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
         const T* z = static_cast<const T*>(a.logits) + row * a.logits_stride;
         Entry entry;
@@ -207,7 +212,8 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
             }
         }
         if (wave == 0) work_teacher(teacher, a, row, entry, z, 0, a.vocab, true);
-        // maximum of z / tau in powers of two, and sum of exp2 of what lies below it; a wave that meets only -infinity has a finite maximum
+        // Maximum, and sum of exp2 of what lies below it.  The difference is taken before it is scaled, so that logits of the type's lowest value, which a
+        // mask may hold everywhere, do not overflow.
         float m = kLeast, l = 0.f;
         if (REST) {
             for (int v = kHeld + tid * E; v < a.vocab; v += THREADS * E) {
@@ -215,11 +221,11 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
                 Words<T>::unpack(Words<T>::template load<false>(z + v, a.vocab - v), f);
 #pragma unroll
                 for (int i = 0; i < E; ++i) most = fmaxf(most, f[i]);
-                most = fmaxf(m, most * c);
-                l *= __builtin_amdgcn_exp2f(m - most);
+                most = fmaxf(m, most);
+                l *= __builtin_amdgcn_exp2f((m - most) * c);
                 m = most;
 #pragma unroll
-                for (int i = 0; i < E; ++i) l += __builtin_amdgcn_exp2f(fmaf(f[i], c, -m));
+                for (int i = 0; i < E; ++i) l += __builtin_amdgcn_exp2f((f[i] - m) * c);
             }
         }
         float most = -__builtin_inff();
@@ -232,10 +238,9 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
                 for (int i = 0; i < E; ++i) most = fmaxf(most, f[i]);
                 __builtin_amdgcn_sched_barrier(0);      // (registers: one word's values at a time)
             }
-            most *= c;
         }
         most = wave_max(fmaxf(most, m));
-        l *= __builtin_amdgcn_exp2f(m - most);
+        l *= __builtin_amdgcn_exp2f((m - most) * c);
         m = most;
         if (NV > 0) {
             keep_packed(held);
@@ -245,7 +250,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
                 float f[E];
                 Words<T>::unpack(held[j], f);
 #pragma unroll
-                for (int i = 0; i < E; ++i) f[i] = __builtin_amdgcn_exp2f(fmaf(f[i], c, -m));
+                for (int i = 0; i < E; ++i) f[i] = __builtin_amdgcn_exp2f((f[i] - m) * c);
                 if (!REST && (j + 1) * THREADS * E > a.vocab) {
                     const int twice = (j * THREADS + t + 1) * E - a.vocab;
 #pragma unroll
@@ -267,21 +272,22 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
         for (int i = 1; i < kWaves; ++i) m = fmaxf(m, part[0][i]);
         l = 0.f;
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) l = fmaf(part[1][i], __builtin_amdgcn_exp2f(part[0][i] - m), l);
-        const float lse2 = m + __builtin_amdgcn_logf(l), lse = lse2 * kLn2;
+        for (int i = 0; i < kWaves; ++i) l = fmaf(part[1][i], __builtin_amdgcn_exp2f((part[0][i] - m) * c), l);
+        const float log2_l = __builtin_amdgcn_logf(l), ln_l = log2_l * kLn2;
         const bool some = teacher.some;
         if (tid == 0) {
-            a.lse[row] = lse;
-            a.loss[row] = some ? a.tau * a.tau * (teacher.cross + lse) : 0.f;
+            a.lse[row] = fmaf(m, inv_tau, ln_l);
+            a.loss[row] = some ? a.tau * a.tau * (teacher.cross + fmaf(m - teacher.z0, inv_tau, ln_l)) : 0.f;
         }
         if (a.dlogits) {
             T* out = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
             const float scale = some ? a.tau * a.dloss[row] : 0.f;
+            const auto probability = [&](float f) { return __builtin_amdgcn_exp2f(fmaf(f - m, c, -log2_l)); };
             const auto write = [&](int v, u4 w, int left) {
                 float f[E];
                 Words<T>::unpack(w, f);
 #pragma unroll
-                for (int i = 0; i < E; ++i) f[i] = some ? scale * __builtin_amdgcn_exp2f(fmaf(f[i], c, -lse2)) : 0.f;
+                for (int i = 0; i < E; ++i) f[i] = some ? scale * probability(f[i]) : 0.f;
                 Words<T>::template store<NT>(out + v, left, f);
             };
             if (NV > 0) {
@@ -298,7 +304,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
                 for (int v = kHeld + tid * E; v < a.vocab; v += THREADS * E) write(v, Words<T>::template load<false>(z + v, a.vocab - v), a.vocab - v);
             }
             __syncthreads();
-            if (some) fix_entries(teacher, a, out, 0, a.vocab, lse2, scale);
+            if (some) fix_entries(teacher, a, out, 0, a.vocab, scale, probability);
         }
         __syncthreads();        // (the teacher's part is free again)
     }
@@ -309,7 +315,7 @@ template <typename T, bool NT>
 __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, int segments) {
     constexpr int E = Words<T>::kElems, kAtOnce = 4;
     __shared__ Teacher teacher;
-    const float c = kLog2e / a.tau;
+    const float inv_tau = 1.f / a.tau;
     for (int64_t b = blockIdx.x; b < a.tokens * segments; b += gridDim.x) {
         const int64_t row = b / segments;
         const int v0 = int(b % segments) * a.segment, v1 = min(v0 + a.segment, a.vocab);
@@ -317,7 +323,8 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, in
         T* out = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
         Entry entry;
         if (threadIdx.x < kWave) entry.ask(a, row, threadIdx.x);
-        const float lse2 = a.lse_in[row] * kLog2e, dloss = a.dloss[row];
+        const float lse = a.lse_in[row], dloss = a.dloss[row];
+        const auto probability = [&](float f) { return __builtin_amdgcn_exp2f(fmaf(f, inv_tau, -lse) * kLog2e); };
         // (the first words are on their way while the teacher is worked out; nothing is written before the teacher has read)
         u4 w[kAtOnce];
         const auto ask = [&](int v) {
@@ -336,14 +343,14 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, in
                 float f[E];
                 Words<T>::unpack(w[j], f);
 #pragma unroll
-                for (int i = 0; i < E; ++i) f[i] = some ? scale * __builtin_amdgcn_exp2f(fmaf(f[i], c, -lse2)) : 0.f;
+                for (int i = 0; i < E; ++i) f[i] = some ? scale * probability(f[i]) : 0.f;
                 if (v + j * 256 * E < v1) Words<T>::template store<NT>(out + v + j * 256 * E, v1 - v - j * 256 * E, f);
             }
             v += 256 * E * kAtOnce;
             if (v < v1) ask(v);
         }
         __syncthreads();
-        if (some) fix_entries(teacher, a, out, v0, v1, lse2, scale);
+        if (some) fix_entries(teacher, a, out, v0, v1, scale, probability);
         __syncthreads();
     }
 }

@@ -132,3 +132,33 @@ def test_gradient_against_differences():
     value(0.0)
     slope = float((out.double().cpu() * d.double()).sum())
     assert abs(slope - measured) < 2e-3 * float(out.double().cpu().norm() * d.double().norm()) / vocab ** 0.5
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [5, 1001, 8192, 70001, 140001])
+def test_rows_of_the_lowest_value(vocab, dtype):
+    """A mask of the type's lowest value that leaves nothing: all logits are alike, and so are the probabilities.  As a softmax does not change when a
+    constant is taken off, the definition is evaluated on the differences to the row's maximum."""
+    tokens, k, tau = 4, 5, 1.0
+    logits, ids, teacher, dloss = make(tokens, vocab, k, dtype, seed=4, missing=0.0)
+    ids[:, :] = torch.arange(k)
+    lowest = torch.finfo(TYPES[dtype]).min
+    logits[:2] = lowest
+    teacher[1] = teacher[3] = torch.finfo(torch.float32).min
+    logits[2] = 1e30                                        # alike, and far from zero
+    spec = bns.make_distill(tokens, vocab, k, dtype, temperature=tau)
+    print(f"[gpu-case] distill lowest value {vocab} {dtype}", flush=True)
+    z, out = logits.cuda(), torch.empty(tokens, vocab, dtype=TYPES[dtype], device="cuda")
+    loss, lse = torch.empty(tokens, device="cuda"), torch.empty(tokens, device="cuda")
+    bns.bns_distill_forward(spec, z, ids.cuda(), teacher.cuda(), dloss.cuda(), loss, lse, out)
+    apart = logits.double() - logits.double().amax(1, keepdim=True)
+    want_loss, _, want = ref.distill(apart, ids, (teacher - teacher.amax(1, keepdim=True)).double(), tau, dloss.double())
+    p_off, q_off = bounds(apart, teacher - teacher.amax(1, keepdim=True), tau)
+    assert bool(((loss.double().cpu() - want_loss).abs() <= (p_off + 2 * q_off) * (apart.abs().amax(1) + 30)).all())
+    assert bool(((lse.double().cpu() - logits.double().amax(1)).abs() <= 12 + 2.0 ** -22 * logits.double().abs().amax(1)).all())    # (ln 140001 < 12)
+    p = torch.softmax(apart, 1)
+    terms = dloss.double()[:, None] * (p * p_off[:, None] + (want / dloss.double()[:, None] - p).abs() * q_off[:, None])
+    assert bool(((out.double().cpu() - want).abs() <= HALF_ULP[dtype] * want.abs() + 2 * terms + 1e-37).all())
+    back = torch.empty_like(out)
+    bns.bns_distill_backward(spec, z, ids.cuda(), teacher.cuda(), lse, dloss.cuda(), back)
+    assert bool(torch.isfinite(back).all())                 # (its probabilities are as good as an lse of 2^-24 of its size, which is no good here)
