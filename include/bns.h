@@ -346,7 +346,7 @@ bns_status bns_copy_reference(void* dst, const void* src, size_t bytes, void* st
  *                    gradients: 1 few tokens (gradients: from 33 tokens in fp32, 65 in bf16 on the choice by size holds), 2 / 3 operands read as they
  *                    lie in memory, tiles of 64 / 128, 4 / 5 operands laid out first, tiles of 256 / 128; 0: by size.  (Logits of 4 and 5 in the
  *                    backward pass need gradients of 1, 4 or 5; with others 3 takes their place.)
- *   "head_groups"    tiles of 64 share the steps along the summed dimension out between four groups of waves: 1 always, 2 never; 0: by size
+ *   "head_groups"    tiles of 64 share the steps along the summed dimension out between groups of waves: 1 always four, 2 never, 3 logits between two; 0: by size
  * Three more exist for the library's own tests only; they make results wrong on purpose and a caller has no
  * use for them:
  *   "test_spin_limit"    polls a block of a fused kernel waits for a team-mate's sums before it gives up

@@ -93,7 +93,7 @@ const TuningEntry kTuningTable[] = {
     {"cache_reuse", &Tuning::cache_reuse, 2, 0, false},
     {"head_logits", &Tuning::head_logits, 5, 0, false},
     {"head_logits_backward", &Tuning::head_logits_backward, 5, 0, false},
-    {"head_groups", &Tuning::head_groups, 2, 0, false},
+    {"head_groups", &Tuning::head_groups, 3, 0, false},
     {"head_gradients", &Tuning::head_gradients, 5, 0, false},
 };
 

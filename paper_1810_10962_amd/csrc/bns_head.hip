@@ -18,10 +18,10 @@ using namespace bns;
 
 namespace {
 
-template <typename T, int BM, int BN, int WM, int WN, int GROUPS, int EPILOGUE>
+template <typename T, int BM, int BN, int WM, int WN, int GROUPS, int EPILOGUE, bool NT = false>
 __global__ void __launch_bounds__(256 * GROUPS) direct_logits_kernel(GemmArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[GROUPS * DirectTile<T, BM, BN, WM, WN>::kBytes];
-    direct_tile<T, BM, BN, WM, WN, GROUPS, true, true, EPILOGUE>(a, int(blockIdx.x), lds);
+    direct_tile<T, BM, BN, WM, WN, GROUPS, true, true, EPILOGUE, NT>(a, int(blockIdx.x), lds);
 }
 
 // Both gradients from g in one launch: the first blocks take dhidden, whose k is the vocabulary, the others dweight, whose k is the tokens.
@@ -146,9 +146,10 @@ inline Kind logits_kind(const HeadDims& d, bool backward) {
     if (chosen) return Kind(chosen);
     const bool f32 = d.dtype == BNS_F32;
     const auto tiles = [&](int tile) { return int64_t(tiles_of(d.tokens, tile)) * tiles_of(d.vocab, tile); };
-    // Fewer tiles of 64 than compute units: what counts is how long a block takes along the width, which kStream divides between its waves (fp32
-    // 9x1792x1071 18 against 53, 226x1728x1148 46 against 66; bf16 11 against 16, but 26 against 20).
-    if (tiles(64) < 128 && d.width >= 512 && (f32 || d.tokens <= 32)) return kStream;
+    // Fewer tiles of 64 than half of the compute units and few tokens: what counts is how long a block takes along the width, which kStream divides between
+    // its waves without LDS (fp32 9x1792x1071 15 against 27, 16x4096x4000 24 against 53, 32x1024x2000 15 against 21, but 60x2048x7000 46 against 41;
+    // bf16 16x4096x4000 16 against 19, 4x2048x2000 11 against 12, but 32x4096x7000 31 against 22, 2x512x8000 11 against 8).
+    if (tiles(64) < 128 && (f32 ? d.tokens <= 32 && d.width >= 512 : d.tokens <= 16 && d.width >= 1536)) return kStream;
     const bool well = lies_well(d, d.hidden_stride) && lies_well(d, d.weight_stride);
     // Tiles of 256 need two rounds of blocks (bf16 4096x4096x16384 411 against 472) and tokens that fill them; copies need many uses of what they lay out
     // (fp32 4096x4096x16384 2607 against 2711, but bf16 1068x110x102656 190 against 121).
@@ -272,11 +273,20 @@ bool gemm(GemmArgs a, Kind kind, hipStream_t st) {
 // Tokens of a tile in the kernels that have several sizes.
 inline int token_tile(int tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : 64; }
 
-// Whether the steps of a tile of 64 are divided between four groups of waves: no more tiles than compute units, each with steps for all groups (bf16
+// Groups of waves between which the steps of a tile of 64 are divided.  Four: no more tiles than compute units, each with steps for all groups (bf16
 // 37x3712x12160 25 against 35 us, 226x1728x1148 16 against 18, but 386x3456x2389, 266 tiles, 40 against 36; gradients of 3155x68x3073 99 against 117).
-inline bool divide_steps(int blocks, int steps) {
-    if (g_tuning.head_groups) return g_tuning.head_groups == 1;
-    return blocks <= 256 && steps >= 16;
+// Two (logits only): up to twice as many tiles with enough steps (fp32 386x3456x2389 111 against 132 us, 200x4000x8000, 500 tiles, 137 against 159,
+// 16x1024x20000 26 against 33, bf16 386x3456x2389 33 against 36; but fp32 128x1024x20000, 626 tiles, 57 against 55, bf16 500x1001x4000, 16 steps, 19.4 against 19.0).
+inline int groups_of(int blocks, int steps, bool logits) {
+    if (g_tuning.head_groups) return g_tuning.head_groups == 1 ? 4 : g_tuning.head_groups == 3 && logits ? 2 : 1;
+    return blocks <= 256 && steps >= 16 ? 4 : logits && blocks <= 512 && steps >= 32 ? 2 : 1;
+}
+
+// Whether logits that read the vocabulary's matrix once do so with the non-temporal hint: more than the memory-side cache holds, in rows of whole cache lines
+// (bf16 16x4096x131072 159 against 180 us, 4x1024x200000 69 against 74, fp32 3x4096x100000 322 against 341; but 16x4008x131072 260 against 215, whose rows
+// share lines, and 16x2048x50257 found in the cache 51 against 38).
+inline bool stream_weight(const GemmArgs& a, size_t e) {
+    return a.tiles_b == 1 && size_t(a.rows_a) * size_t(a.lda) * e > kStreamBytes && size_t(a.lda) * e % 128 == 0 && reinterpret_cast<uintptr_t>(a.a) % 128 == 0;
 }
 
 template <typename T, int EPILOGUE>
@@ -290,13 +300,19 @@ bool logits(const HeadDims& d, const HeadPlan& p, GemmArgs a, hipStream_t st) {
     a.tiles_a = tiles_of(std::max(a.rows_a, a.g_depth), m);
     a.tiles_b = tiles_of(a.rows_b, n);
     const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b);
-    const bool groups = divide_steps(a.tiles_a * a.tiles_b, a.depth / DirectTile<T, 64, 64, 2, 2>::kDepth);
+    const int groups = groups_of(a.tiles_a * a.tiles_b, a.depth / DirectTile<T, 64, 64, 2, 2>::kDepth, true);
+    const bool nt = EPILOGUE == kStatistics && stream_weight(a, sizeof(T));
     if (p.kind == kDirect128) BNS_LAUNCH((direct_logits_kernel<T, 128, 128, 2, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64 && n == 16 && groups) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && n == 16 && groups == 4) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && n == 16 && groups == 2) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
+    else if (p.kind == kDirect64 && n == 16 && nt) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 1, EPILOGUE, EPILOGUE == kStatistics>), grid, dim3(256), 0, st, a);
     else if (p.kind == kDirect64 && n == 16) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64 && n == 32 && groups) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && n == 32 && groups == 4) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && n == 32 && groups == 2) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
+    else if (p.kind == kDirect64 && n == 32 && nt) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 1, EPILOGUE, EPILOGUE == kStatistics>), grid, dim3(256), 0, st, a);
     else if (p.kind == kDirect64 && n == 32) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64 && groups) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && groups == 4) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+    else if (p.kind == kDirect64 && groups == 2) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
     else if (p.kind == kDirect64) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (m == 16 && n == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (m == 16 && n == 32) BNS_LAUNCH((stream_logits_kernel<T, 1, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
@@ -356,7 +372,7 @@ bool direct_gradients(GemmArgs h, GemmArgs w, Kind kind, hipStream_t st) {
     w.tiles_b = tiles_of(w.rows_b, m);
     const int blocks_h = h.tiles_a * h.tiles_b * h.splits;
     const dim3 grid(uint32_t(blocks_h) + uint32_t(w.tiles_a) * w.tiles_b);
-    const bool groups = divide_steps(w.tiles_a * w.tiles_b, w.depth / DirectTile<T, 64, 64, 2, 2>::kDepth);
+    const bool groups = groups_of(w.tiles_a * w.tiles_b, w.depth / DirectTile<T, 64, 64, 2, 2>::kDepth, false) == 4;
     if (n == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
     else if (n == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
     else if (n == 64 && groups) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, 4, EPILOGUE>), grid, dim3(1024), 0, st, h, w, blocks_h);

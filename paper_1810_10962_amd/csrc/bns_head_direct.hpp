@@ -12,7 +12,8 @@ namespace bns {
 
 // The elements of one operand's tile that a thread brings in: eight neighbours along k of a row (K_ROWS), or eight neighbouring rows at two
 // neighbouring k, which together give whole 32-bit words of LDS.  ROW, SLOT: which row of the tile lies at which place in LDS (row_m, slot_m, ...).
-template <typename T, int ROWS, int DEPTH, bool K_ROWS, int THREADS, int (*ROW)(int), int (*SLOT)(int)>
+// NT: with the non-temporal hint.
+template <typename T, int ROWS, int DEPTH, bool K_ROWS, int THREADS, int (*ROW)(int), int (*SLOT)(int), bool NT = false>
 struct Feed {
     static constexpr int P = planes_of<T>(), kRowBytes = DEPTH * 2, kPlane = ROWS * kRowBytes, kChunks = DEPTH / 8;
     static constexpr int kUnits = K_ROWS ? ROWS * DEPTH / 8 : (DEPTH / 2) * (ROWS / 8), kPer = (kUnits + THREADS - 1) / THREADS, kRaw = K_ROWS ? 1 : 2;
@@ -42,7 +43,7 @@ struct Feed {
             if constexpr (K_ROWS) {
                 const int row = min(row0 + ROW(unit / kChunks), rows - 1), k = k0 + unit % kChunks * 8;
                 const T* p = base + row * ld + k;
-                if (inside) raw[i][0].load(p);
+                if (inside) raw[i][0].template load<NT>(p);
                 else fetch(raw[i][0], p, depth - k);
             } else {
                 const int row = row0 + unit % (ROWS / 8) * 8, k = k0 + unit / (ROWS / 8) * 2;
@@ -124,13 +125,13 @@ struct DirectTile {
 };
 
 // One tile of a product.  A_ROWS, B_ROWS: whether that operand's rows run along k (else m, n are its columns, and a.lda, a.ldb lead from one k to the next).
-// `lds`: GROUPS times DirectTile::kBytes.
-template <typename T, int BM, int BN, int WM, int WN, int GROUPS, bool A_ROWS, bool B_ROWS, int EPILOGUE>
+// `lds`: GROUPS times DirectTile::kBytes.  NT: A, which nobody reads again, with the non-temporal hint.
+template <typename T, int BM, int BN, int WM, int WN, int GROUPS, bool A_ROWS, bool B_ROWS, int EPILOGUE, bool NT = false>
 __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* lds) {
     using S = DirectTile<T, BM, BN, WM, WN>;
     constexpr int P = S::P, D = S::kDepth, MI = BM / WM / 16, NI = BN / WN / 16;
     static_assert(S::kThreads == 256 && MI * NI * int(sizeof(f32x4)) * 256 <= S::kBytes * (GROUPS > 1 ? 1 : 1000), "a group's sums fit its part of LDS");
-    using FeedA = Feed<T, BM, D, A_ROWS, S::kThreads, row_m<MI>, slot_m<MI>>;
+    using FeedA = Feed<T, BM, D, A_ROWS, S::kThreads, row_m<MI>, slot_m<MI>, NT>;
     using FeedB = Feed<T, BN, D, B_ROWS, S::kThreads, row_n<NI>, slot_n<NI>>;
     const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(int(threadIdx.x) / 256) : 0, tid = GROUPS > 1 ? int(threadIdx.x) % 256 : int(threadIdx.x);
     char* const lds_a = lds + group * S::kBytes;

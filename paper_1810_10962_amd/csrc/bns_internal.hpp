@@ -99,7 +99,7 @@ struct Tuning {
     // loss over the vocabulary, kernels of the logits (forward, backward) and of the gradients' products: 1 few tokens, 2 / 3 operands as they lie in
     // memory with tiles of 64 / 128, 4 / 5 operands laid out first with tiles of 256 / 128; 0 by size
     TuneInt head_logits{0}, head_logits_backward{0}, head_gradients{0};
-    TuneInt head_groups{0};                 // 1: the steps of its tiles of 64 always divided between groups of waves, 2 never
+    TuneInt head_groups{0};                 // the steps of its tiles of 64: 1 always divided between four groups of waves, 2 never, 3 logits between two
     // For the library's own tests of the give-up path only; a caller has no use for them.
     TuneInt test_spin_limit{0};             // polls a team member waits for a team-mate before giving up (default 2^21)
     TuneInt test_mute_exchange{0};          // 1: no member publishes its sums, so every wait runs out

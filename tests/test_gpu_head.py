@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 
 # Kernels of the forward pass's logits, the backward pass's and the gradients' products: see "head_logits" and the options behind it.
 PATHS = {"few": (1, 1, 1), "few_direct": (1, 1, 2), "direct64": (2, 2, 2), "direct64_few": (2, 2, 1), "direct128": (3, 3, 3), "laid_out256": (4, 4, 4), "laid_out128": (5, 5, 5),
-         "mixed": (5, 1, 4), "mixed2": (4, 3, 5), "divided64": (2, 2, 2, 1), "auto": (0, 0, 0)}
+         "mixed": (5, 1, 4), "mixed2": (4, 3, 5), "divided64": (2, 2, 2, 1), "halved64": (2, 2, 2, 3), "auto": (0, 0, 0)}
 OPTIONS = ("head_logits", "head_logits_backward", "head_gradients", "head_groups")
 
 
@@ -199,3 +199,16 @@ def test_gradient_against_differences():
     measured = (value(h) - value(-h)) / (2 * h)
     size = float(gh.double().cpu().norm() * dh.double().norm() / width ** 0.5 + gw.double().cpu().norm() * dw.double().norm() / vocab ** 0.5)
     assert abs(slope - measured) < 5e-3 * size
+
+
+@pytest.mark.parametrize("tokens,width,vocab,dtype,stride", [(5, 1024, 115000, "bf16", 1024), (20, 500, 115011, "f32", 512), (3, 1000, 120000, "bf16", 1001), (17, 1001, 60001, "f32", 1001)])
+def test_a_matrix_beyond_the_cache(tokens, width, vocab, dtype, stride):
+    """More than 224 MB of weights (rows of whole cache lines or not), read once."""
+    hidden, weight, targets, _ = make(tokens, width, vocab, dtype, seed=6)
+    print(f"[gpu-case] head beyond the cache {tokens}x{width}x{vocab} {dtype} stride={stride}", flush=True)
+    spec = bns.make_head(tokens, width, vocab, dtype, weight_stride=stride)
+    ws = torch.full((bns.bns_head_workspace_bytes(spec),), 255, dtype=torch.uint8, device="cuda")
+    w = Rows(weight, stride)
+    loss, lse = written(tokens), written(tokens)
+    bns.bns_head_forward(spec, hidden.cuda(), w, targets.cuda(), loss, lse, ws)
+    check_forward(loss.check()[0], lse.check()[0], hidden, weight, targets, dtype)
