@@ -1,10 +1,14 @@
 // Distillation from a teacher's top logits: the loss with the logits' gradient from the same pass, and the gradient on its own.  See
 // include/bns.h for the equations.
 //
+// Softmax of both sides in powers of two: p = exp2((z - m) log2(e) / tau - log2 sum), all of it in fp32 (a word of bf16 is unpacked where it is used).
 // Both read every logit once and write every gradient once, so HBM bounds them.  Forward: a block takes a row and keeps it in registers
 // as it is stored (256 KB of the 512 KB of a compute unit), so that maximum, sum and gradient come from one read; of longer rows the
 // rest is read again, which the memory-side cache serves.  Wave 0 works the teacher's distribution out while the row is on its way.  The gradient is
-// written as if the teacher were not there, then the few elements that it touches once more.
+// written as if the teacher were not there, then the few elements that it touches once more.  Backward needs no sum, so a row is cut into segments where
+// rows are few.
+// Measured: 4096x131072 bf16 with gradient 401 us (5.4 TB/s, a large copy 5.1), 1630x77568 fp32 181 us, 64x50257 bf16 11 us (one block per row: launch, load,
+// two exchanges, store); the gradient alone 2048x50304 fp32 162 us (5.1 TB/s), 7x100003 bf16 6.4 us, which is a launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -185,8 +189,8 @@ __device__ __forceinline__ void keep_packed(u4 (&w)[N]) {
     for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
 }
 
-// NV: 16-byte words per thread that hold the row, or with REST its beginning; what lies behind is read again (NV = 0: rows shorter than a word).  NT: with the non-temporal hint (4096x131072 bf16 with its gradient 400 against
-// 416 us, gradient of 2048x50304 fp32 162 against 172; 7x100003 bf16 6.7 against 6.4).
+// NV: 16-byte words per thread that hold the row, or with REST its beginning; what lies behind is read again (NV = 0: rows shorter than a word).  NT: with
+// the non-temporal hint (4096x131072 bf16 with its gradient 400 against 416 us, gradient of 2048x50304 fp32 162 against 172; 7x100003 bf16 6.7 against 6.4).
 template <typename T, int THREADS, int NV, bool REST, bool NT>
 __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a) {
     constexpr int E = Words<T>::kElems, kWaves = THREADS / kWave, kHeld = NV * THREADS * E;
