@@ -52,11 +52,13 @@ struct GemmArgs {
     int32_t fresh;              // kAccumulate: out holds nothing yet
 };
 
-// Block -> tile.  Blocks go round robin over the eight dies, each with an L2 of its own: a die gets a contiguous range of tiles, walked in groups of
-// four rows of tiles, so that the tiles in flight share their operands.
-__device__ __forceinline__ void place(int block, int total, int tiles_a, int tiles_b, int& ta, int& tb) {
-    const int die = block % 8, q = total / 8, r = total % 8;
-    const int i = die * q + min(die, r) + block / 8;
+// Block -> split and tile.  Blocks go round robin over the eight dies, each with an L2 of its own: a die gets a contiguous range of tiles, split after split,
+// walked in groups of four rows of tiles, so that the tiles in flight share their operands.
+__device__ __forceinline__ void place(int block, int splits, int tiles_a, int tiles_b, int& split, int& ta, int& tb) {
+    const int tiles = tiles_a * tiles_b, total = tiles * splits, die = block % 8, q = total / 8, r = total % 8;
+    const int at = die * q + min(die, r) + block / 8;
+    split = at / tiles;
+    const int i = at - split * tiles;
     const int group = i / (4 * tiles_b), in = i - group * 4 * tiles_b, high = min(4, tiles_a - 4 * group);
     tb = in / high;
     ta = 4 * group + in - tb * high;

@@ -140,9 +140,8 @@ __device__ __forceinline__ void direct_tile(const GemmArgs& a, int block, char* 
     const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(int(threadIdx.x) / 256) : 0, tid = GROUPS > 1 ? int(threadIdx.x) % 256 : int(threadIdx.x);
     char* const lds_a = lds + group * S::kBytes;
     char* const lds_b = lds_a + FeedA::kPlane * P;
-    const int tiles = a.tiles_a * a.tiles_b, split = block / tiles, tile = block - split * tiles;
-    int ta, tb;
-    place(tile, tiles, a.tiles_a, a.tiles_b, ta, tb);
+    int split, ta, tb;
+    place(block, a.splits, a.tiles_a, a.tiles_b, split, ta, tb);
     const int m0 = ta * BM, n0 = tb * BN;
     const int steps = (a.depth + D - 1) / D, first = int(int64_t(steps) * split / a.splits), end = int(int64_t(steps) * (split + 1) / a.splits);
     const T *pa = static_cast<const T*>(a.a), *pb = static_cast<const T*>(a.b);

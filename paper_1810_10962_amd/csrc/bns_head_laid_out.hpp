@@ -119,9 +119,8 @@ __global__ void __launch_bounds__(WM* WN* kWave) gemm_kernel(GemmArgs a) {
     constexpr int P = planes_of<T>(), kSegments = P == 1 ? 1 : 6;
     __shared__ __attribute__((aligned(1024))) char lds[2][S::kBytes];
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave), lane = threadIdx.x % kWave;
-    const int tiles = a.tiles_a * a.tiles_b, split = int(blockIdx.x) / tiles;
-    int ta, tb;
-    place(int(blockIdx.x) - split * tiles, tiles, a.tiles_a, a.tiles_b, ta, tb);
+    int split, ta, tb;
+    place(int(blockIdx.x), a.splits, a.tiles_a, a.tiles_b, split, ta, tb);
     const int m0 = ta * BM, n0 = tb * BN;
 
     // Staging: a wave brings in eight rows of 128 bytes with one instruction, which puts lane after lane into LDS; the 16-byte chunks of row r
