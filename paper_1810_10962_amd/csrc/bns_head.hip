@@ -170,13 +170,24 @@ inline Kind gradients_kind(const HeadDims& d) {
     // bf16 16x2048x50257 135 against 178, 2x384x85765 48 against 64, 40x1024x4096 29 against 24; fp32 1x3520x87977 999 against 1085, 16x2048x50257 400 against 393
     if (few && matrix >= (int64_t(1) << (f32 ? 27 : 23))) return kStream;
     const double work = double(matrix) * double(d.tokens);
-    // Laying operands out pays where each of them is read many times: bf16 512x2048x8192 97 against 124, 2853x576x2248 79 against 96, but 256x4096x32000
-    // 492 against 397 and 1024x256x32000 141 against 119; fp32 4096x4096x16384 7989 against 8615, but 1024x1024x8192 331 against 301.
-    const bool often = f32 ? d.tokens >= 1000 && work >= 3e10 : (d.tokens >= 512 && d.width >= 512 && work >= 5e9) || (d.tokens >= 2048 && work >= 1e9);
-    if (often) return d.tokens >= (f32 ? 1000 : 2048) && d.width >= (f32 ? 1000 : 2048) ? kGemm256 : kGemm128;
-    // bf16 256x4096x32000 397 against 446, 256x512x32000 86 against 77; fp32 40x1024x4096 36 against 42, 374x68x130472 358 against 518, but 9x1792x1071 30
-    // against 25, 1068x110x102656 1289 against 1190
-    if (f32 ? matrix >= (int64_t(1) << 21) && (d.width >= 192 || d.tokens < 512) : work >= 1.5e10) return kDirect128;
+    // Laying operands out pays where each of them is read many times: bf16 512x2048x8192 97 against 124, 450x700x30000 168 against 189, 600x1000x9000 87
+    // against 110, 1189x320x60672 331 against 353, 1130x392x39552 262 against 309, 2000x100x30000 183 against 277, but 256x4096x32000 506 against 402,
+    // 1024x256x32000 141 against 119, 500x600x17000 121 against 105, 1200x64x100000 401 against 249; fp32 4096x4096x16384 7989 against 8615,
+    // 2000x800x10000 698 against 835, 4000x400x6000 595 against 780, but 1024x1024x8192 331 against 301, 3000x1000x1000 328 against 221,
+    // 1100x128x100000 1385 against 1033.
+    const bool often = f32 ? d.width >= 256 && ((d.tokens >= 1000 && work >= 1.2e10) || (d.tokens >= 2048 && work >= 5e9))
+                           : (d.tokens >= 400 && d.width >= 512 && work >= (d.width >= 900 ? 5e9 : 8e9)) ||
+                                 (d.tokens >= 1000 && d.width >= (d.tokens >= 1200 ? 96 : 320) && work >= 5e9) || (d.tokens >= 2048 && work >= 1e9);
+    if (often) {
+        // Tiles of 256 need enough of them in dweight (fp32 1500x1500x6000, 144 tiles, 613 against 631; 2500x1000x3000, 48, 554 against 369; bf16
+        // 4096x4096x2048, 128, 255 against 231) and room along the others (fp32 2000x800x10000 698 against 749, 4000x500x20000 2215 against 1893; bf16
+        // 450x3000x12000 221 against 207).
+        const int64_t tiles = int64_t(tiles_of(d.width, 256)) * tiles_of(std::min(d.vocab, 16384), 256);
+        return tiles > 128 && d.tokens >= (f32 ? 1000 : 2048) && d.width >= (f32 ? 768 : 2048) ? kGemm256 : kGemm128;
+    }
+    // bf16 256x4096x32000 397 against 446, but 256x512x32000 86 against 77, 400x400x100000 355 against 326; fp32 40x1024x4096 36 against 42, 374x68x130472 358
+    // against 518, but 9x1792x1071 30 against 25, 1068x110x102656 1289 against 1190
+    if (f32 ? matrix >= (int64_t(1) << 21) && (d.width >= 192 || d.tokens < 512) : work >= 1.5e10 && d.width >= 512) return kDirect128;
     return kDirect64;
 }
 
