@@ -24,13 +24,15 @@ __global__ void __launch_bounds__(256 * GROUPS) direct_logits_kernel(GemmArgs a)
     direct_tile<T, BM, BN, WM, WN, GROUPS, true, true, EPILOGUE, NT>(a, int(blockIdx.x), lds);
 }
 
-// Both gradients from g in one launch: the first blocks take dhidden, whose k is the vocabulary, the others dweight, whose k is the tokens.
+// Both gradients from g in one launch: `blocks_h` blocks take dhidden, whose k is the vocabulary, the others dweight, whose k is the tokens.  `ahead` of the
+// latter (all or none) go first, where their chains of steps are the longer ones (700x700x7000 fp32 181 against 200 us, 1200x64x100000 bf16 232 against 253).
 template <typename T, int BM, int BN, int WM, int WN, int BW, int GROUPS, int EPILOGUE>
-__global__ void __launch_bounds__(256 * GROUPS) direct_gradients_kernel(GemmArgs h, GemmArgs w, int blocks_h) {
+__global__ void __launch_bounds__(256 * GROUPS) direct_gradients_kernel(GemmArgs h, GemmArgs w, int blocks_h, int ahead) {
     constexpr int kH = DirectTile<T, BM, BN, WM, WN>::kBytes, kW = DirectTile<T, BW, BW, 2, 2>::kBytes;
     __shared__ __attribute__((aligned(16))) char lds[GROUPS * (kH > kW ? kH : kW)];
-    if (int(blockIdx.x) < blocks_h) direct_tile<T, BM, BN, WM, WN, GROUPS, false, true, EPILOGUE>(h, int(blockIdx.x), lds);
-    else direct_tile<T, BW, BW, 2, 2, GROUPS, false, false, kStore>(w, int(blockIdx.x) - blocks_h, lds);
+    const int b = int(blockIdx.x) - ahead;
+    if (b >= 0 && b < blocks_h) direct_tile<T, BM, BN, WM, WN, GROUPS, false, true, EPILOGUE>(h, b, lds);
+    else direct_tile<T, BW, BW, 2, 2, GROUPS, false, false, kStore>(w, b < 0 ? int(blockIdx.x) : b - blocks_h, lds);
 }
 
 // ---- what follows the products --------------------------------------------------------------------------------------
@@ -191,6 +193,15 @@ inline Kind gradients_kind(const HeadDims& d) {
     return kDirect64;
 }
 
+// Groups of waves between which the steps of a tile of 64 are divided.  Four: no more tiles than compute units, each with steps for all groups (bf16
+// 37x3712x12160 25 against 35 us, 226x1728x1148 16 against 18, but 386x3456x2389, 266 tiles, 40 against 36; gradients of 3155x68x3073 99 against 117).
+// Two (logits only): up to twice as many tiles with enough steps (fp32 386x3456x2389 111 against 132 us, 200x4000x8000, 500 tiles, 137 against 159,
+// 16x1024x20000 26 against 33, bf16 386x3456x2389 33 against 36; but fp32 128x1024x20000, 626 tiles, 57 against 55, bf16 500x1001x4000, 16 steps, 19.4 against 19.0).
+inline int groups_of(int blocks, int steps, bool logits) {
+    if (g_tuning.head_groups) return g_tuning.head_groups == 1 ? 4 : g_tuning.head_groups == 3 && logits ? 2 : 1;
+    return blocks <= 256 && steps >= 16 ? 4 : logits && blocks <= 512 && steps >= 32 ? 2 : 1;
+}
+
 HeadPlan head_plan(const HeadDims& d, bool backward) {
     HeadPlan p = {};
     const size_t e = dtype_bytes(d.dtype), T = size_t(d.tokens);
@@ -233,8 +244,11 @@ HeadPlan head_plan(const HeadDims& d, bool backward) {
             p.splits_w = int(std::max<int64_t>(1, std::min<int64_t>(1024 / groups, rows / 128)));
         } else if (p.gradients <= kDirect128) {
             const int m = p.gradients == kDirect128 ? 128 : 64;
-            const int64_t tiles = ((d.width + m - 1) / m) * ((d.tokens + m - 1) / m), steps = rows / (f32 ? 32 : 64);
-            p.splits = int(std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(tiles, 1), steps / 4)));
+            const int64_t across = (d.width + m - 1) / m, tiles = across * ((d.tokens + m - 1) / m), depth = f32 ? 32 : 64, steps = rows / depth;
+            // Steps enough for a block to be worth its sums: four, or four for each of four groups of waves (2870x256x1294 bf16 51 us against 68 with one for
+            // each, 923x704x1024 fp32 64 against 80).  Eight instead of four: 425x1088x3328 fp32 102 against 106, but 40x1024x4096 46 against 41.
+            const bool groups = m == 64 && d.tokens > 32 && groups_of(int(across * ((rows + m - 1) / m)), int(d.tokens / depth), false) == 4;
+            p.splits = int(std::max<int64_t>(1, std::min<int64_t>((groups ? 512 : 1024) / std::max<int64_t>(tiles, 1), steps / (groups ? 16 : 4))));
         } else {
             const int m = p.gradients == kGemm128 ? 128 : 256;
             const int64_t tiles = ((d.width + m - 1) / m) * ((d.tokens + m - 1) / m);
@@ -283,15 +297,6 @@ bool gemm(GemmArgs a, Kind kind, hipStream_t st) {
 
 // Tokens of a tile in the kernels that have several sizes.
 inline int token_tile(int tokens) { return tokens <= 16 ? 16 : tokens <= 32 ? 32 : 64; }
-
-// Groups of waves between which the steps of a tile of 64 are divided.  Four: no more tiles than compute units, each with steps for all groups (bf16
-// 37x3712x12160 25 against 35 us, 226x1728x1148 16 against 18, but 386x3456x2389, 266 tiles, 40 against 36; gradients of 3155x68x3073 99 against 117).
-// Two (logits only): up to twice as many tiles with enough steps (fp32 386x3456x2389 111 against 132 us, 200x4000x8000, 500 tiles, 137 against 159,
-// 16x1024x20000 26 against 33, bf16 386x3456x2389 33 against 36; but fp32 128x1024x20000, 626 tiles, 57 against 55, bf16 500x1001x4000, 16 steps, 19.4 against 19.0).
-inline int groups_of(int blocks, int steps, bool logits) {
-    if (g_tuning.head_groups) return g_tuning.head_groups == 1 ? 4 : g_tuning.head_groups == 3 && logits ? 2 : 1;
-    return blocks <= 256 && steps >= 16 ? 4 : logits && blocks <= 512 && steps >= 32 ? 2 : 1;
-}
 
 // Whether logits that read the vocabulary's matrix once do so with the non-temporal hint: more than the memory-side cache holds, in rows of whole cache lines
 // (bf16 16x4096x131072 159 against 180 us, 4x1024x200000 69 against 74, fp32 3x4096x100000 322 against 341; but 16x4008x131072 260 against 215, whose rows
@@ -382,13 +387,14 @@ bool direct_gradients(GemmArgs h, GemmArgs w, Kind kind, hipStream_t st) {
     h.tiles_b = tiles_of(h.rows_b, n);
     w.tiles_b = tiles_of(w.rows_b, m);
     const int blocks_h = h.tiles_a * h.tiles_b * h.splits;
-    const dim3 grid(uint32_t(blocks_h) + uint32_t(w.tiles_a) * w.tiles_b);
-    const bool groups = groups_of(w.tiles_a * w.tiles_b, w.depth / DirectTile<T, 64, 64, 2, 2>::kDepth, false) == 4;
-    if (n == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else if (n == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else if (n == 64 && groups) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, 4, EPILOGUE>), grid, dim3(1024), 0, st, h, w, blocks_h);
-    else if (n == 64) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
-    else BNS_LAUNCH((direct_gradients_kernel<T, 128, 128, 2, 2, 128, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h);
+    const int blocks_w = w.tiles_a * w.tiles_b, ahead = w.depth > h.depth / h.splits ? blocks_w : 0;
+    const dim3 grid(uint32_t(blocks_h) + uint32_t(blocks_w));
+    const bool groups = groups_of(blocks_w, w.depth / DirectTile<T, 64, 64, 2, 2>::kDepth, false) == 4;
+    if (n == 16) BNS_LAUNCH((direct_gradients_kernel<T, 64, 16, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h, ahead);
+    else if (n == 32) BNS_LAUNCH((direct_gradients_kernel<T, 64, 32, 4, 1, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h, ahead);
+    else if (n == 64 && groups) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, 4, EPILOGUE>), grid, dim3(1024), 0, st, h, w, blocks_h, ahead);
+    else if (n == 64) BNS_LAUNCH((direct_gradients_kernel<T, 64, 64, 2, 2, 64, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h, ahead);
+    else BNS_LAUNCH((direct_gradients_kernel<T, 128, 128, 2, 2, 128, 1, EPILOGUE>), grid, dim3(256), 0, st, h, w, blocks_h, ahead);
     return !failed();
 }
 
