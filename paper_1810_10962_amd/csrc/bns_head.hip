@@ -194,7 +194,7 @@ inline Kind gradients_kind(const HeadDims& d) {
 }
 
 // Groups of waves between which the steps of a tile of 64 are divided.  Four: no more tiles than compute units, each with steps for all groups (bf16
-// 37x3712x12160 25 against 35 us, 226x1728x1148 16 against 18, but 386x3456x2389, 266 tiles, 40 against 36; gradients of 3155x68x3073 99 against 117).
+// 37x3712x12160 25 against 35 us, 226x1728x1148 16 against 18, but 386x3456x2389, 266 tiles, 40 against 36; gradients of 3155x68x3073 58 against 109, of 923x704x1024 fp32 64 against 74).
 // Two (logits only): up to twice as many tiles with enough steps (fp32 386x3456x2389 111 against 132 us, 200x4000x8000, 500 tiles, 137 against 159,
 // 16x1024x20000 26 against 33, bf16 386x3456x2389 33 against 36; but fp32 128x1024x20000, 626 tiles, 57 against 55, bf16 500x1001x4000, 16 steps, 19.4 against 19.0).
 inline int groups_of(int blocks, int steps, bool logits) {
