@@ -15,16 +15,45 @@ template <typename T>
 constexpr int planes_of() { return sizeof(T) == 4 ? 3 : 1; }
 
 // ---- parts of an fp32 value ---------------------------------------------------------------------------------------
-// x = hi + mid + lo exactly, each of them the bf16 nearest to what is left.  What is infinite or NaN as a bf16 (from 3.39e38 on) is hi alone.  A
-// product of two values needs the six pairs of parts whose exponents reach into an fp32 result: what is dropped is at most 2^-24 of it.
+// x = hi + mid + lo exactly, each of them the bf16 nearest to what is left.  A product of two values needs the six pairs of parts whose exponents reach
+// into an fp32 result: what is dropped is at most 2^-24 of it.
 // Two values at a time: word p holds part p of x0 in its lower half, of x1 in its upper one.
+// BEYOND: values that the nearest bf16 would make infinite are among them.  The finite ones take the largest finite bf16 as their first part, the others
+// carry the rest.  An infinite one is its last part alone: that part meets nothing but first parts, which are zero only where the value is, so that no
+// product is infinity times a zero part and infinity times x is what it is in fp32.  (Infinity times infinity is NaN.)
+constexpr float kBeyondBf16 = 0x1.ffp127f, kLargestBf16 = 0x1.fep127f;
+template <bool BEYOND>
 __device__ __forceinline__ void split3(float x0, float x1, uint32_t (&word)[3]) {
-    word[0] = pack_bf16x2(x0, x1);
+    const bool i0 = BEYOND && fabsf(x0) == __builtin_inff(), i1 = BEYOND && fabsf(x1) == __builtin_inff();
+    const auto first = [](float x, bool infinite) { return infinite ? 0.f : BEYOND && fabsf(x) >= kBeyondBf16 ? copysignf(kLargestBf16, x) : x; };
+    word[0] = pack_bf16x2(first(x0, i0), first(x1, i1));
     float r0 = x0 - __uint_as_float(word[0] << 16), r1 = x1 - __uint_as_float(word[0] & 0xffff0000u);
-    r0 = fabsf(r0) < __builtin_inff() ? r0 : 0.f;
-    r1 = fabsf(r1) < __builtin_inff() ? r1 : 0.f;
-    word[1] = pack_bf16x2(r0, r1);
-    word[2] = pack_bf16x2(r0 - __uint_as_float(word[1] << 16), r1 - __uint_as_float(word[1] & 0xffff0000u));
+    word[1] = pack_bf16x2(i0 ? 0.f : r0, i1 ? 0.f : r1);
+    r0 -= __uint_as_float(word[1] << 16);
+    r1 -= __uint_as_float(word[1] & 0xffff0000u);
+    word[2] = pack_bf16x2(r0, r1);
+}
+// N pairs; one look at all of them says whether some lane has a value beyond the range of bf16 (NaN needs no care).
+template <int N>
+__device__ __forceinline__ void split3(const float (&x0)[N], const float (&x1)[N], uint32_t (&word)[N][3]) {
+    float most = 0.f;       // (one instruction a pair, where fmaxf would quiet every operand first)
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(most) : "v"(x0[j]), "v"(x1[j]));
+    if (__builtin_expect(__any(most >= kBeyondBf16), 0)) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) split3<true>(x0[j], x1[j], word[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) split3<false>(x0[j], x1[j], word[j]);
+    }
+}
+// Eight neighbours: word j of part p.
+__device__ __forceinline__ void split3(const float (&f)[8], u4 (&w)[3]) {
+    const float x0[4] = {f[0], f[2], f[4], f[6]}, x1[4] = {f[1], f[3], f[5], f[7]};
+    uint32_t word[4][3];
+    split3(x0, x1, word);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) w[p] = u4{word[0][p], word[1][p], word[2][p], word[3][p]};
 }
 
 // Which pairs of planes an fp32 product takes, smallest first.
@@ -217,15 +246,22 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM /
                 const int m = m_base + r * kStride;
                 uint32_t part[kRun][NI][P];
 #pragma unroll
-                for (int x = 0; x < kRun; x += 2)
+                for (int j = 0; j < NI; ++j) {
+                    float even[kRun / 2], odd[kRun / 2];
+                    uint32_t word[kRun / 2][3];
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) {
-                        uint32_t word[3];
-                        if constexpr (P == 1) word[0] = pack_bf16x2(at(r, j, x), at(r, j, x + 1));
-                        else split3(at(r, j, x), at(r, j, x + 1), word);
+                    for (int x = 0; x < kRun / 2; ++x) even[x] = at(r, j, 2 * x), odd[x] = at(r, j, 2 * x + 1);
+                    if constexpr (P == 1) {
 #pragma unroll
-                        for (int p = 0; p < P; ++p) part[x][j][p] = word[p] & 0xffffu, part[x + 1][j][p] = word[p] >> 16;
+                        for (int x = 0; x < kRun / 2; ++x) word[x][0] = pack_bf16x2(even[x], odd[x]);
+                    } else {
+                        split3(even, odd, word);
                     }
+#pragma unroll
+                    for (int x = 0; x < kRun / 2; ++x)
+#pragma unroll
+                        for (int p = 0; p < P; ++p) part[2 * x][j][p] = word[x][p] & 0xffffu, part[2 * x + 1][j][p] = word[x][p] >> 16;
+                }
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
 #pragma unroll

@@ -80,13 +80,7 @@ struct Feed {
                     float f[8];
                     raw[i][0].unpack(f);
                     u4 w[3];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t word[3];
-                        split3(f[2 * j], f[2 * j + 1], word);
-#pragma unroll
-                        for (int p = 0; p < 3; ++p) w[p][j] = word[p];
-                    }
+                    split3(f, w);
 #pragma unroll
                     for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(lds + p * kPlane + to) = w[p];
                 }
@@ -108,14 +102,13 @@ struct Feed {
                     float even[8], odd[8];
                     raw[i][0].unpack(even);
                     raw[i][1].unpack(odd);
+                    uint32_t word[8][3];
+                    split3(even, odd, word);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        uint32_t word[3];
-                        split3(even[j], odd[j], word);
+                    for (int j = 0; j < 8; ++j)
 #pragma unroll
                         for (int p = 0; p < 3; ++p)
-                            *reinterpret_cast<uint32_t*>(lds + p * kPlane + at(SLOT(row + j), pair / 4) + pair % 4 * 4) = word[p];
-                    }
+                            *reinterpret_cast<uint32_t*>(lds + p * kPlane + at(SLOT(row + j), pair / 4) + pair % 4 * 4) = word[j][p];
                 }
             }
         }

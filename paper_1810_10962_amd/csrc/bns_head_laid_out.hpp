@@ -35,13 +35,7 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(PackArgs a) {
             *reinterpret_cast<u4*>(out) = u4{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
         } else {
             u4 w[3];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t word[3];
-                split3(f[2 * j], f[2 * j + 1], word);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) w[p][j] = word[p];
-            }
+            split3(f, w);
 #pragma unroll
             for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(out + int64_t(p) * a.depth) = w[p];
         }
@@ -80,14 +74,11 @@ __global__ void __launch_bounds__(256) pack_columns_kernel(PackArgs a) {
             for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(tile[r + 2 * i][c], tile[r + 2 * i + 1][c]);
             *reinterpret_cast<u4*>(out) = w;
         } else {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = tile[r + i][c];
             u4 w[3];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t word[3];
-                split3(tile[r + 2 * i][c], tile[r + 2 * i + 1][c], word);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) w[p][i] = word[p];
-            }
+            split3(f, w);
 #pragma unroll
             for (int p = 0; p < 3; ++p) *reinterpret_cast<u4*>(out + int64_t(p) * a.depth) = w[p];
         }

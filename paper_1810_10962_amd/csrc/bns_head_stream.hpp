@@ -31,13 +31,7 @@ __device__ __forceinline__ void to_parts(const Raw8<bf16_t>& r, u4 (&w)[1]) { w[
 __device__ __forceinline__ void to_parts(const Raw8<float>& r, u4 (&w)[3]) {
     float f[8];
     r.unpack(f);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t word[3];
-        split3(f[2 * j], f[2 * j + 1], word);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) w[p][j] = word[p];
-    }
+    split3(f, w);
 }
 // Column f of eight rows, the rows being neighbours along k.
 __device__ __forceinline__ void column_parts(const Raw8<bf16_t> (&r)[8], int f, u4 (&w)[1]) {
@@ -48,13 +42,10 @@ __device__ __forceinline__ void column_parts(const Raw8<bf16_t> (&r)[8], int f, 
     }
 }
 __device__ __forceinline__ void column_parts(const Raw8<float> (&r)[8], int f, u4 (&w)[3]) {
+    float column[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        uint32_t word[3];
-        split3(__uint_as_float(f < 4 ? r[2 * j].a[f % 4] : r[2 * j].b[f % 4]), __uint_as_float(f < 4 ? r[2 * j + 1].a[f % 4] : r[2 * j + 1].b[f % 4]), word);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) w[p][j] = word[p];
-    }
+    for (int j = 0; j < 8; ++j) column[j] = __uint_as_float(f < 4 ? r[j].a[f % 4] : r[j].b[f % 4]);
+    split3(column, w);
 }
 
 // Logits of 16 MI rows of the vocabulary and 16 NI tokens.  The four waves of a block take every fourth step of k each.

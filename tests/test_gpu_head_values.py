@@ -1,0 +1,79 @@
+"""Loss over the vocabulary on the GPU: logits that are infinite, NaN or as low as the type goes, in tokens that count.  A masked row of the vocabulary holds
+-infinity or the type's lowest value in a column that is positive in every token, as a bias does; what it adds to a softmax is nothing, so the definition (lm_reference) is
+evaluated without those rows, with the tolerances of test_gpu_head."""
+import pytest
+import torch
+
+from lm_reference import TYPES
+from paper_1810_10962_amd import bns
+from test_gpu_head import check_backward, check_forward, make, path, run  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+BIAS, MASKED = 7, 40        # the column, and how many of the vocabulary's last rows are masked
+
+
+def masked(tokens, width, vocab, dtype, value):
+    hidden, weight, targets, dloss = make(tokens, width, vocab, dtype, seed=11)
+    targets = torch.where((targets >= vocab - MASKED) & (targets < vocab), targets - MASKED, targets)
+    weight[:, BIAS] = 0
+    # one, which is its own first part, values with three parts of mixed signs, one whose product with the lowest value overflows
+    hidden[:, BIAS] = torch.tensor([1.0, 0.1, 1.5, 300.7, 1e-3, 0.7])[torch.arange(tokens) % 6].to(TYPES[dtype])
+    weight[vocab - MASKED:, BIAS] = value
+    return hidden, weight, targets, dloss
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,width,vocab", [(9, 64, 300), (140, 72, 700), (20, 512, 1100)])
+def test_masked_rows_of_the_vocabulary_count_for_nothing(tokens, width, vocab, dtype, path):  # noqa: F811
+    for value in (-float("inf"), float(torch.finfo(TYPES[dtype]).min)):
+        print(f"[gpu-case] head masked by {value} {tokens}x{width}x{vocab} {dtype} {path}", flush=True)
+        hidden, weight, targets, dloss = masked(tokens, width, vocab, dtype, value)
+        left = torch.where(targets >= vocab - MASKED, -1, targets)      # (a target outside the smaller vocabulary is one outside the larger)
+        loss, lse, dh, dw = run(hidden, weight, targets, dloss, dtype)
+        check_forward(loss, lse, hidden, weight[:-MASKED], left, dtype)
+        assert bool((dw[-MASKED:] == 0).all())
+        clean = weight[:-MASKED]
+        if value == -float("inf"):          # zero times infinity: the column's gradient is NaN by the formula
+            dh = dh.clone()
+            dh[:, BIAS] = 0
+        check_backward(dh, dw[:-MASKED], hidden, clean, left, dloss, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,width,vocab", [(9, 64, 300), (140, 72, 700)])
+def test_infinity_and_nan_stay_in_their_token(tokens, width, vocab, dtype, path):  # noqa: F811
+    hidden, weight, targets, dloss = masked(tokens, width, vocab, dtype, -float("inf"))
+    targets = torch.randint(0, vocab - MASKED, (tokens,), generator=torch.Generator().manual_seed(3))
+    hidden[1, BIAS] = -0.3                  # logits of +infinity
+    hidden[3, 5] = float("nan")
+    hidden[4, BIAS] = 0                     # zero times infinity
+    hidden[6, 2] = float("inf")             # logits of both infinities
+    targets[7] = vocab - 3                  # a target that is masked
+    print(f"[gpu-case] head infinity and NaN {tokens}x{width}x{vocab} {dtype} {path}", flush=True)
+    loss, lse, _, _ = run(hidden, weight, targets, dloss, dtype)
+    loss, lse = loss.cpu(), lse.cpu()
+    for t in (1, 3, 4, 6):
+        assert not bool(torch.isfinite(loss[t])) and not bool(torch.isfinite(lse[t])), t
+    assert bool(torch.isnan(loss[3])) and bool(torch.isnan(lse[3]))
+    assert float(loss[7]) == float("inf") and bool(torch.isfinite(lse[7]))
+    rest = torch.tensor([t not in (1, 3, 4, 6, 7) for t in range(tokens)])
+    check_forward(loss[rest], lse[rest], hidden[rest], weight[:-MASKED], targets[rest], dtype)
+    check_forward(lse[7:8] * 0, lse[7:8], hidden[7:8], weight[:-MASKED], torch.tensor([-1]), dtype)
+
+
+def test_the_whole_range_of_fp32(path):  # noqa: F811
+    """Operands from the largest finite value down, one product a logit, and the other a power of two: every logit is exact, so is the difference of two of them."""
+    tokens, width, vocab = 30, 64, 300
+    big = torch.tensor([torch.finfo(torch.float32).max, 3.3961775292304957e38, 3.39e38, 3.3895313892515355e38, 1.7e38, 1e30])
+    weight, hidden = torch.zeros(vocab, width), torch.zeros(tokens, width)
+    weight[torch.arange(tokens), torch.arange(tokens)] = big[torch.arange(tokens) % 6]
+    hidden[torch.arange(tokens), torch.arange(tokens)] = 2.0 ** -(121 + torch.arange(tokens).float() % 3)
+    weight[vocab - 1], hidden[:, width - 1] = 0, 0
+    want = (weight[:tokens].double() * hidden.double()).sum(1)          # every token has one logit that is not zero
+    print(f"[gpu-case] head range of fp32 {path}", flush=True)
+    spec = bns.make_head(tokens, width, vocab, "f32")
+    ws = torch.empty(bns.bns_head_workspace_bytes(spec), dtype=torch.uint8, device="cuda")
+    loss, lse = torch.empty(tokens, device="cuda"), torch.empty(tokens, device="cuda")
+    bns.bns_head_forward(spec, hidden.cuda(), weight.cuda(), torch.full((tokens,), vocab - 1).cuda(), loss, lse, ws)
+    top = torch.log(torch.exp(want) + vocab - 1)
+    assert bool(((loss.double().cpu() - top).abs() <= 2.0 ** -20 * (1 + top.abs())).all())
