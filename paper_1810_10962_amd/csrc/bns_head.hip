@@ -43,13 +43,13 @@ __global__ void __launch_bounds__(256) join_statistics_kernel(const float2* part
     constexpr int kLanes = 256 / TOKENS;
     __shared__ float2 part[kLanes][TOKENS];
     const int c = threadIdx.x % TOKENS, lane = threadIdx.x / TOKENS, token = blockIdx.x * TOKENS + c;
-    float m = -3e38f, l = 0.f;
+    float m = kLowest, l = 0.f;
     if (token < tokens) {
 #pragma unroll 4
         for (int i = lane; i < tiles; i += kLanes) {
             const float2 p = partial[int64_t(i) * tokens + token];
             const float most = fmaxf(m, p.x);
-            l = l * __builtin_amdgcn_exp2f(m - most) + p.y * __builtin_amdgcn_exp2f(p.x - most);
+            l = l * __builtin_amdgcn_exp2f((m - most) * kLog2e) + p.y * __builtin_amdgcn_exp2f((p.x - most) * kLog2e);
             m = most;
         }
     }
@@ -59,15 +59,16 @@ __global__ void __launch_bounds__(256) join_statistics_kernel(const float2* part
         if (lane >= half) continue;
         const float2 p = part[lane + half][c];
         const float most = fmaxf(m, p.x);
-        l = l * __builtin_amdgcn_exp2f(m - most) + p.y * __builtin_amdgcn_exp2f(p.x - most);
+        l = l * __builtin_amdgcn_exp2f((m - most) * kLog2e) + p.y * __builtin_amdgcn_exp2f((p.x - most) * kLog2e);
         m = most;
         part[lane][c] = float2{m, l};
     }
     if (lane != 0 || token >= tokens) return;
-    const float all = (m + __builtin_amdgcn_logf(l)) * kLn2;
+    // (m is a logit, so m - z is exact near zero and never below it, and neither is the logarithm of a sum that holds exp(0))
+    const float log2_l = __builtin_amdgcn_logf(l);
     const int64_t target = targets[token];
-    lse[token] = all;
-    loss[token] = target >= 0 && target < vocab ? all - at_target[token] : 0.f;
+    lse[token] = fmaf(log2_l, kLn2, m);
+    loss[token] = target >= 0 && target < vocab ? fmaf(log2_l, kLn2, m - at_target[token]) : 0.f;
 }
 
 // dhidden from the sums that the splits left behind: 8 columns x 32 a block and row, LANES threads each take every LANES-th split.

@@ -5,6 +5,7 @@
 namespace bns {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLowest = -3.40282347e38f;      // a maximum of only -infinity is this
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -71,7 +72,7 @@ struct GemmArgs {
     // logits: m = row of the piece, n = token
     const int64_t* targets;     // (gradients: tokens whose rows of A count as zeros are those left out by them; NULL: none)
     const float *lse, *dloss;
-    float2* partial;            // [tile of the whole vocabulary][token]: maximum and sum of a tile's logits, in powers of two
+    float2* partial;            // [tile of the whole vocabulary][token]: maximum m of a tile's logits and sum of exp(z - m)
     float* at_target;           // [token]
     uint16_t *g, *gt;           // kGradientParts: [token][planes][g_depth], [row of the piece][planes][gt_depth]
     int32_t v0, vocab, g_depth, gt_depth;
@@ -179,17 +180,18 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM /
             for (int r = 0; r < kRuns; ++r)
 #pragma unroll
                 for (int x = 0; x < kRun; ++x) {
-                    const float z = at(r, j, x), f = r * kStride + x < left ? z * kLog2e : -__builtin_inff();
+                    const float z = at(r, j, x), f = r * kStride + x < left ? z : -__builtin_inff();
                     if (aim == r * kStride + x) a.at_target[n] = z;
                     put(r, j, x, f);
                     m = fmaxf(m, f);
                 }
             m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), -3e38f);        // (a finite number where the wave has no row)
+            m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), kLowest);        // (a finite number where the wave has no row)
+            // (The difference is taken before it is scaled: it is exact where it counts, and does not overflow.)
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f(acc[i][j][e] - m);
+                for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f((acc[i][j][e] - m) * kLog2e);
             l += __shfl_xor(l, 16);
             l += __shfl_xor(l, 32);
             if (lane < 16) {
@@ -205,7 +207,7 @@ __device__ __forceinline__ void finish(const GemmArgs& a, f32x4 (&acc)[BM / WM /
 #pragma unroll
                 for (int w = 1; w < WM; ++w) m = fmaxf(m, stat[w * BN + c].x);
 #pragma unroll
-                for (int w = 0; w < WM; ++w) l = fmaf(stat[w * BN + c].y, __builtin_amdgcn_exp2f(stat[w * BN + c].x - m), l);
+                for (int w = 0; w < WM; ++w) l = fmaf(stat[w * BN + c].y, __builtin_amdgcn_exp2f((stat[w * BN + c].x - m) * kLog2e), l);
                 a.partial[int64_t(a.v0 / BM + ta) * a.rows_b + tb * BN + c] = float2{m, l};
             }
         }

@@ -77,3 +77,55 @@ def test_the_whole_range_of_fp32(path):  # noqa: F811
     bns.bns_head_forward(spec, hidden.cuda(), weight.cuda(), torch.full((tokens,), vocab - 1).cuda(), loss, lse, ws)
     top = torch.log(torch.exp(want) + vocab - 1)
     assert bool(((loss.double().cpu() - top).abs() <= 2.0 ** -20 * (1 + top.abs())).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1, 8, 32])
+def test_the_loss_of_a_sure_model_is_zero(scale, dtype, path):  # noqa: F811
+    """Logits scale (32 + t) on the target, zero and below elsewhere, all exact: what a softmax leaves to the others is below 700 exp(-32) = 1e-11, so the loss is
+    neither negative nor more than a unit in the last place of one, and lse is the target's logit."""
+    tokens, width, vocab = 64, 64, 700
+    weight = torch.zeros(vocab, width)
+    weight[torch.arange(vocab), torch.arange(vocab) % width] = float(scale)
+    weight[width:] *= -1
+    top = 32.0 + torch.arange(tokens)
+    hidden, targets = torch.diag(top), torch.arange(tokens)
+    print(f"[gpu-case] head sure {scale} {dtype} {path}", flush=True)
+    loss, lse, _, _ = run(hidden.to(TYPES[dtype]), weight.to(TYPES[dtype]), targets, torch.ones(tokens), dtype)
+    assert bool((loss >= 0).all()) and bool((loss <= 2.0 ** -23).all())
+    assert torch.equal(lse.cpu(), scale * top)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("base", [0.0, 512.0, -2048.0])
+@pytest.mark.parametrize("tokens", [12, 130])
+def test_logits_far_from_zero(tokens, base, dtype, path):  # noqa: F811
+    """Exact logits, base plus multiples of 1/8 between -4 and 4: the loss does not depend on the base.  Exponents below 12 in powers of two and an exponential's own unit cost
+    (12 + 2) 2^-24 of a term, the sums in turn and in a tree 30 2^-24, the logarithm two units of a number below 16: 3e-6 + 2e-6."""
+    width, vocab = 64, 700
+    g = torch.Generator().manual_seed(17)
+    weight, hidden = torch.zeros(vocab, width), torch.zeros(tokens, width)
+    weight[:, 0], weight[:, 1], weight[:, 2] = base, torch.randint(-16, 17, (vocab,), generator=g) / 8.0, torch.randint(-16, 17, (vocab,), generator=g) / 8.0
+    hidden[:, 0] = 1
+    hidden[torch.arange(tokens), 1 + torch.arange(tokens) % 2] = 2.0 - (torch.arange(tokens) % 4).float()
+    targets = torch.randint(0, vocab, (tokens,), generator=g)
+    print(f"[gpu-case] head base {base} {tokens} {dtype} {path}", flush=True)
+    loss, lse, _, _ = run(hidden.to(TYPES[dtype]), weight.to(TYPES[dtype]), targets, torch.ones(tokens), dtype)
+    z = hidden.double() @ weight.double().T
+    want = torch.logsumexp(z, 1)
+    assert bool(((loss.double().cpu() - (want - z[torch.arange(tokens), targets])).abs() <= 5e-6).all())
+    assert bool(((lse.double().cpu() - want).abs() <= 5e-6 + 2.0 ** -24 * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [12, 130])
+def test_logits_at_the_ends_of_the_range(tokens, dtype, path):  # noqa: F811
+    """All logits of a token are the type's lowest value, or its largest: alike, so the loss is log(vocab)."""
+    width, vocab = 64, 700
+    weight, hidden = torch.zeros(vocab, width), torch.zeros(tokens, width)
+    weight[:, 0] = torch.finfo(TYPES[dtype]).max
+    hidden[:, 0] = 1.0 - 2 * (torch.arange(tokens) % 2)
+    print(f"[gpu-case] head ends of the range {tokens} {dtype} {path}", flush=True)
+    loss, lse, _, _ = run(hidden.to(TYPES[dtype]), weight.to(TYPES[dtype]), torch.arange(tokens), torch.ones(tokens), dtype)
+    assert bool(((loss.double().cpu() - torch.log(torch.tensor(float(vocab), dtype=torch.float64))).abs() <= 5e-6).all())
+    assert torch.equal(lse.cpu(), hidden[:, 0] * torch.finfo(TYPES[dtype]).max)
