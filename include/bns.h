@@ -477,7 +477,7 @@ typedef struct {
  *   q = softmax(teacher / tau)        p = softmax(logits / tau) over the vocabulary        lse = log sum exp(logits / tau)
  *   loss[t] = tau^2 * sum over j of q_j (log q_j - log p[id_j])
  * A row without such an entry has loss 0 and gradient 0, whatever its logits hold.  An id may occur more than once: its q add up in the gradient.
- * A teacher's logit of -infinity is no entry; one that is NaN or +infinity makes its row NaN, and so does a logit of the student that is.  A student's
+ * A teacher's logit of -infinity is no entry; one that is NaN or +infinity makes its row NaN, loss and gradient, and so does a logit of the student that is.  A student's
  * logit of -infinity has p = 0; with q > 0 there the loss is infinite.
  * dlogits = tau * dloss[t] * (p - q), in the same pass over the logits, where dlogits is given (then dloss is needed too).
  * in: logits[tokens][vocab], ids[tokens][k], teacher[tokens][k] (dense), dloss[tokens] (NULL without dlogits).

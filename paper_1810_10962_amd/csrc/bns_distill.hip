@@ -103,6 +103,7 @@ struct Teacher {
     float cross;                            // sum q (log q - (z - z0) / tau)
     float z0;                               // the student's largest logit at the entries
     int32_t some;                           // whether the row has an entry
+    float one;                              // 1; NaN where a teacher's logit is NaN or +infinity, which makes all of the row's gradient so
 };
 
 // An entry that its lane has asked for; the first kWave of them are asked for before the row is, so that they arrive first.
@@ -163,6 +164,7 @@ __device__ __forceinline__ void work_teacher(Teacher& s, const DistillArgs& a, i
         s.cross = x;
         s.z0 = z0;
         s.some = any;
+        s.one = total == total ? 1.f : total;
     }
 }
 
@@ -285,7 +287,7 @@ __global__ void __launch_bounds__(THREADS) distill_forward_kernel(DistillArgs a)
         }
         if (a.dlogits) {
             T* out = static_cast<T*>(a.dlogits) + row * a.dlogits_stride;
-            const float scale = some ? a.tau * a.dloss[row] : 0.f;
+            const float scale = some ? a.tau * a.dloss[row] * teacher.one : 0.f;
             const auto probability = [&](float f) { return __builtin_amdgcn_exp2f(fmaf(f - m, c, -log2_l)); };
             const auto write = [&](int v, u4 w, int left) {
                 float f[E];
@@ -340,7 +342,7 @@ __global__ void __launch_bounds__(256) distill_backward_kernel(DistillArgs a, in
         if (threadIdx.x < kWave) work_teacher(teacher, a, row, entry, z, v0, v1, false);
         __syncthreads();
         const bool some = teacher.some;
-        const float scale = some ? a.tau * dloss : 0.f;
+        const float scale = some ? a.tau * dloss * teacher.one : 0.f;
         while (v < v1) {
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
