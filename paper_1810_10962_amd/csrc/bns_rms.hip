@@ -113,9 +113,15 @@ __device__ __forceinline__ float mean_and_eps(float sum, float inv_width, float 
     return mean + eps;
 }
 
+// a / b to nearest, as a division gives it, from inv = 1 / b to nearest: the remainder of the product is exact (for a from 2^-102 on), one step takes it in.
+__device__ __forceinline__ float quotient(float a, float b, float inv) {
+    const float q = a * inv;
+    return fmaf(fmaf(-q, b, a), inv, q);
+}
+
 // The scale of values whose largest magnitude is `most`: see include/bns.h.
 __device__ __forceinline__ float e4m3_scale(float most, int pow2) {
-    const float s = fmaxf(most * (1.f / 448.f), 0x1p-126f);
+    const float by = quotient(most, 448.f, 1.f / 448.f), s = most < __builtin_inff() ? fmaxf(by, 0x1p-126f) : most;
     if (!pow2) return s;
     const uint32_t bits = __float_as_uint(s);
     return __uint_as_float((bits + 0x7fffffu) & 0x7f800000u);
@@ -209,13 +215,19 @@ __global__ void __launch_bounds__(block_of<TPR>()) rms_forward_kernel(RmsArgs a)
         for (int j = 0; j < VPT; ++j) {
             const int col = (j * TPR + t) * 8, left = RAGGED ? a.width - col : 8;
             if (col >= a.width) continue;
-            const float scale = e4m3_scale(most[j], a.pow2), inv = 1.f / scale;
+            const float scale = e4m3_scale(most[j], a.pow2);
             if (a.group == 0 ? col == 0 : col % a.group == 0) scales[a.group == 0 ? 0 : col / a.group] = scale;
+            // Quotients, not products with the reciprocal, whose rounding would decide what lies halfway between two numbers of the type (divisions instead: 8192x5120
+            // bf16 57.6 against 54.2 us, 2000x2048 9.6 against 8.6).
+            const float inv = 1.f / scale, finite = fminf(scale, 0x1.fffffep127f);
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = quotient(s[j][i], finite, inv);
             uint32_t q[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                int v = __builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * h] * inv, s[j][4 * h + 1] * inv, 0, false);
-                q[h] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * h + 2] * inv, s[j][4 * h + 3] * inv, v, true));
+                int v = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h], f[4 * h + 1], 0, false);
+                q[h] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * h + 2], f[4 * h + 3], v, true));
             }
             if (left >= 8) {
                 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
