@@ -319,11 +319,18 @@ bool logits(const HeadDims& d, const HeadPlan& p, GemmArgs a, hipStream_t st) {
     const dim3 grid(uint32_t(a.tiles_a) * a.tiles_b);
     const int groups = groups_of(a.tiles_a * a.tiles_b, a.depth / DirectTile<T, 64, 64, 2, 2>::kDepth, true);
     const bool nt = EPILOGUE == kStatistics && stream_weight(a, sizeof(T));
+    if constexpr (EPILOGUE != kGradientParts) {     // (n is 32 or more there)
+        if (n == 16) {
+            if (p.kind == kDirect64 && groups == 4) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
+            else if (p.kind == kDirect64 && groups == 2) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
+            else if (p.kind == kDirect64 && nt) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 1, EPILOGUE, EPILOGUE == kStatistics>), grid, dim3(256), 0, st, a);
+            else if (p.kind == kDirect64) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+            else if (m == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+            else BNS_LAUNCH((stream_logits_kernel<T, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
+            return !failed();
+        }
+    }
     if (p.kind == kDirect128) BNS_LAUNCH((direct_logits_kernel<T, 128, 128, 2, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64 && n == 16 && groups == 4) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
-    else if (p.kind == kDirect64 && n == 16 && groups == 2) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
-    else if (p.kind == kDirect64 && n == 16 && nt) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 1, EPILOGUE, EPILOGUE == kStatistics>), grid, dim3(256), 0, st, a);
-    else if (p.kind == kDirect64 && n == 16) BNS_LAUNCH((direct_logits_kernel<T, 64, 16, 4, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (p.kind == kDirect64 && n == 32 && groups == 4) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
     else if (p.kind == kDirect64 && n == 32 && groups == 2) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
     else if (p.kind == kDirect64 && n == 32 && nt) BNS_LAUNCH((direct_logits_kernel<T, 64, 32, 4, 1, 1, EPILOGUE, EPILOGUE == kStatistics>), grid, dim3(256), 0, st, a);
@@ -331,10 +338,8 @@ bool logits(const HeadDims& d, const HeadPlan& p, GemmArgs a, hipStream_t st) {
     else if (p.kind == kDirect64 && groups == 4) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 4, EPILOGUE>), grid, dim3(1024), 0, st, a);
     else if (p.kind == kDirect64 && groups == 2) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 2, EPILOGUE>), grid, dim3(512), 0, st, a);
     else if (p.kind == kDirect64) BNS_LAUNCH((direct_logits_kernel<T, 64, 64, 2, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (m == 16 && n == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (m == 16 && n == 32) BNS_LAUNCH((stream_logits_kernel<T, 1, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (m == 16) BNS_LAUNCH((stream_logits_kernel<T, 1, 4, EPILOGUE>), grid, dim3(256), 0, st, a);
-    else if (n == 16) BNS_LAUNCH((stream_logits_kernel<T, 2, 1, EPILOGUE>), grid, dim3(256), 0, st, a);
     else if (n == 32) BNS_LAUNCH((stream_logits_kernel<T, 2, 2, EPILOGUE>), grid, dim3(256), 0, st, a);
     else BNS_LAUNCH((stream_logits_kernel<T, 2, 4, EPILOGUE>), grid, dim3(256), 0, st, a);
     return !failed();

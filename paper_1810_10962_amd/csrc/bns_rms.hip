@@ -392,16 +392,21 @@ int64_t backward_blocks(const RmsPlan& p, int64_t rows) {
     else if (nt) BNS_LAUNCH((KERNEL<T, TPR, VPT, false, true>), grid, dim3(THREADS), 0, st, a);                       \
     else BNS_LAUNCH((KERNEL<T, TPR, VPT, false, false>), grid, dim3(THREADS), 0, st, a);                              \
     break;
+// (plans of few rows, which never move that much)
+#define BNS_RMS_FEW(T, KERNEL, TPR, VPT, THREADS)                                                                     \
+    if (a.width % 8) BNS_LAUNCH((KERNEL<T, TPR, VPT, true, false>), grid, dim3(THREADS), 0, st, a);                   \
+    else BNS_LAUNCH((KERNEL<T, TPR, VPT, false, false>), grid, dim3(THREADS), 0, st, a);                              \
+    break;
 #define BNS_RMS_FORWARD(T)                                              \
     switch (p.tpr * 10 + p.vpt) {                                       \
         case 641: BNS_RMS_CASE(T, rms_forward_kernel, 64, 1, 256)       \
         case 642: BNS_RMS_CASE(T, rms_forward_kernel, 64, 2, 256)       \
         case 644: BNS_RMS_CASE(T, rms_forward_kernel, 64, 4, 256)       \
-        case 2561: BNS_RMS_CASE(T, rms_forward_kernel, 256, 1, 256)     \
+        case 2561: BNS_RMS_FEW(T, rms_forward_kernel, 256, 1, 256)      \
         case 2562: BNS_RMS_CASE(T, rms_forward_kernel, 256, 2, 256)     \
         case 2563: BNS_RMS_CASE(T, rms_forward_kernel, 256, 3, 256)     \
         case 2564: BNS_RMS_CASE(T, rms_forward_kernel, 256, 4, 256)     \
-        case 10241: BNS_RMS_CASE(T, rms_forward_kernel, 1024, 1, 1024)  \
+        case 10241: BNS_RMS_FEW(T, rms_forward_kernel, 1024, 1, 1024)   \
         default: BNS_RMS_CASE(T, rms_forward_kernel, 512, 4, 512)       \
     }
 #define BNS_RMS_BACKWARD(T)                                             \
