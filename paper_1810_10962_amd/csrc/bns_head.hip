@@ -267,6 +267,9 @@ HeadPlan head_plan(const HeadDims& d, bool backward) {
     return p;
 }
 
+// What either pass needs, `other` being the plan of the one that is not `p`'s.
+inline size_t workspace_of(const HeadPlan& p, const HeadPlan& other) { return std::max(p.bytes, other.bytes); }
+
 inline bool failed() { return hipGetLastError() != hipSuccess; }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
@@ -501,7 +504,7 @@ extern "C" {
 size_t bns_head_workspace_bytes(const bns_head* head) {
     HeadDims d;
     if (check_head(head, &d) != BNS_OK) return 0;
-    return std::max(head_plan(d, false).bytes, head_plan(d, true).bytes);
+    return workspace_of(head_plan(d, false), head_plan(d, true));
 }
 
 bns_status bns_head_forward(const bns_head* head, const void* hidden, const void* weight, const int64_t* targets, float* loss, float* lse,
@@ -513,7 +516,7 @@ bns_status bns_head_forward(const bns_head* head, const void* hidden, const void
     if (!hidden || !weight || !targets || !loss || !lse || !workspace) return BNS_EINVAL;
     if (!aligned16(hidden) || !aligned16(weight) || !aligned16(workspace)) return BNS_EINVAL;
     const HeadPlan p = head_plan(d, false);
-    if (workspace_bytes < bns_head_workspace_bytes(head)) return BNS_EWORKSPACE;
+    if (workspace_bytes < workspace_of(p, head_plan(d, true))) return BNS_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     const auto call = d.dtype == BNS_F32 ? forward<float> : forward<bf16_t>;
@@ -537,7 +540,7 @@ bns_status bns_head_backward(const bns_head* head, const void* hidden, const voi
             if (collide(out, in, false, row, row)) return BNS_EINVAL;
     if (collide(mdh, mdw, false, row, row)) return BNS_EINVAL;
     const HeadPlan p = head_plan(d, true);
-    if (workspace_bytes < bns_head_workspace_bytes(head)) return BNS_EWORKSPACE;
+    if (workspace_bytes < workspace_of(p, head_plan(d, false))) return BNS_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     if (d.tokens == 0) {
