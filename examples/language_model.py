@@ -10,6 +10,7 @@ import os
 import sys
 
 import torch
+from torch.autograd.function import once_differentiable
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_1810_10962_amd import bns  # noqa: E402
@@ -23,6 +24,7 @@ class AddNorm(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, delta, stream, weight):
+        delta, stream, weight = delta.contiguous(), stream.contiguous(), weight.contiguous()      # (the library is handed addresses)
         rows, width = stream.shape
         rms = bns.make_rms(rows, width, NAMES[stream.dtype], eps=EPS)
         total, y, rstd = torch.empty_like(stream), torch.empty_like(stream), torch.empty(rows, device=stream.device)
@@ -32,6 +34,7 @@ class AddNorm(torch.autograd.Function):
         return total, y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dtotal, dy):
         total, weight, rstd = ctx.saved_tensors
         dx, dweight = torch.empty_like(total), torch.empty_like(weight)
@@ -45,6 +48,7 @@ class HeadLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, hidden, weight, targets):
+        hidden, weight, targets = hidden.contiguous(), weight.contiguous(), targets.contiguous()
         head = bns.make_head(hidden.shape[0], hidden.shape[1], weight.shape[0], NAMES[hidden.dtype])
         workspace = torch.empty(bns.bns_head_workspace_bytes(head), dtype=torch.uint8, device=hidden.device)
         loss, lse = torch.empty(hidden.shape[0], device=hidden.device), torch.empty(hidden.shape[0], device=hidden.device)
@@ -55,6 +59,7 @@ class HeadLoss(torch.autograd.Function):
         return loss.sum() / count
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dmean):
         hidden, weight, targets, lse, count = ctx.saved_tensors
         dloss = (dmean / count).expand(hidden.shape[0]).contiguous()
@@ -69,6 +74,7 @@ class DistillLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, ids, teacher, temperature):
+        logits, ids, teacher = logits.contiguous(), ids.contiguous(), teacher.contiguous()
         tokens, vocab = logits.shape
         distill = bns.make_distill(tokens, vocab, ids.shape[1], NAMES[logits.dtype], temperature=temperature)
         loss, lse, dlogits = torch.empty(tokens, device=logits.device), torch.empty(tokens, device=logits.device), torch.empty_like(logits)
@@ -78,6 +84,7 @@ class DistillLoss(torch.autograd.Function):
         return loss.mean()
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dmean):
         return ctx.saved_tensors[0] * dmean, None, None, None
 
