@@ -129,3 +129,34 @@ def test_logits_at_the_ends_of_the_range(tokens, dtype, path):  # noqa: F811
     loss, lse, _, _ = run(hidden.to(TYPES[dtype]), weight.to(TYPES[dtype]), torch.arange(tokens), torch.ones(tokens), dtype)
     assert bool(((loss.double().cpu() - torch.log(torch.tensor(float(vocab), dtype=torch.float64))).abs() <= 5e-6).all())
     assert torch.equal(lse.cpu(), hidden[:, 0] * torch.finfo(TYPES[dtype]).max)
+
+
+def three_parts(n, seed):
+    """Values in [1, 2) with 24 significant bits, each of whose three parts is needed."""
+    return 1 + (torch.randint(0, 2 ** 22, (n,), generator=torch.Generator().manual_seed(seed)) * 2 + 1).float() * 2.0 ** -23
+
+
+@pytest.mark.parametrize("tokens,width,vocab", [(30, 64, 300), (30, 200, 1500), (140, 192, 700), (250, 256, 3000)])
+@pytest.mark.parametrize("which", ["hidden", "weight", "dloss", "middle"])
+def test_every_part_of_an_fp32_product_counts(which, tokens, width, vocab, path):  # noqa: F811
+    """Token t has one product that is not zero, x_t y_t = 64 to 128, with row 2 t of the vocabulary; its target is row 2 t + 1, whose logit is zero.  What the softmax
+    leaves to all other rows is below 3000 exp(-64) = 1e-24, so that loss = lse = x_t y_t, g = dloss and -dloss, and every result is a single product, which is exact in
+    fp32 where one factor is a power of two, or where both are 1 + 2^-9 times one (whose product of second parts is 2^-18 of the whole).  A pair of parts that is left out or
+    taken twice changes bits."""
+    t = torch.arange(tokens)
+    x, y, d = torch.full((tokens,), 8.0), torch.full((tokens,), 8.0), torch.full((tokens,), 0.25)
+    if which == "hidden":
+        x = x * three_parts(tokens, 1)
+    elif which == "weight":
+        y = y * three_parts(tokens, 2)
+    elif which == "dloss":
+        d = d * three_parts(tokens, 3)
+    else:
+        x, y, d = (v * (1 + 2.0 ** -9) for v in (x, y, d))
+    hidden, weight = torch.zeros(tokens, width), torch.zeros(vocab, width)
+    hidden[t, t], weight[2 * t, t] = x, y
+    print(f"[gpu-case] head parts {which} {tokens}x{width}x{vocab} {path}", flush=True)
+    loss, lse, dh, dw = (o.cpu() for o in run(hidden, weight, 2 * t + 1, d, "f32"))
+    assert torch.equal(loss, x * y) and torch.equal(lse, x * y)
+    assert torch.equal(dh[t, t], d * y)
+    assert torch.equal(dw[2 * t, t], d * x) and torch.equal(dw[2 * t + 1, t], -d * x)
