@@ -18,8 +18,9 @@ using namespace bns;
 
 namespace {
 
+// (Sixteen tokens stream the matrix, and seven waves on a unit that could hold six keep more of it on its way.)
 template <typename T, int BM, int BN, int WM, int WN, int GROUPS, int EPILOGUE, bool NT = false>
-__global__ void __launch_bounds__(256 * GROUPS) direct_logits_kernel(GemmArgs a) {
+__global__ void __launch_bounds__(256 * GROUPS, BN == 16 && GROUPS == 1 ? 7 : 1) direct_logits_kernel(GemmArgs a) {
     __shared__ __attribute__((aligned(16))) char lds[GROUPS * DirectTile<T, BM, BN, WM, WN>::kBytes];
     direct_tile<T, BM, BN, WM, WN, GROUPS, true, true, EPILOGUE, NT>(a, int(blockIdx.x), lds);
 }
