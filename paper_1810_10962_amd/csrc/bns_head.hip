@@ -151,16 +151,16 @@ inline Kind logits_kind(const HeadDims& d, bool backward) {
     const bool f32 = d.dtype == BNS_F32;
     const auto tiles = [&](int tile) { return int64_t(tiles_of(d.tokens, tile)) * tiles_of(d.vocab, tile); };
     // Fewer tiles of 64 than half of the compute units and few tokens: what counts is how long a block takes along the width, which kStream divides between
-    // its waves without LDS (fp32 9x1792x1071 15 against 27, 16x4096x4000 24 against 53, 32x1024x2000 15 against 21, but 60x2048x7000 46 against 41;
-    // bf16 16x4096x4000 16 against 19, 4x2048x2000 11 against 12, but 32x4096x7000 31 against 22, 2x512x8000 11 against 8).
+    // its waves without LDS (fp32 9x1792x1071 15 against 27, 16x4096x4000 26 against 53, 32x1024x2000 16 against 21, but 60x2048x7000 48 against 41;
+    // bf16 16x4096x4000 16 against 20, 4x2048x2000 12 against 13, but 32x4096x7000 32 against 22, 2x512x8000 12 against 10).
     if (tiles(64) < 128 && (f32 ? d.tokens <= 32 && d.width >= 512 : d.tokens <= 16 && d.width >= 1536)) return kStream;
     const bool well = lies_well(d, d.hidden_stride) && lies_well(d, d.weight_stride);
-    // Tiles of 256 need two rounds of blocks (bf16 4096x4096x16384 411 against 472) and tokens that fill them; copies need many uses of what they lay out
-    // (fp32 4096x4096x16384 2607 against 2711, but bf16 1068x110x102656 190 against 121).
+    // Tiles of 256 need two rounds of blocks (bf16 4096x4096x16384 435 against 523) and tokens that fill them; copies need many uses of what they lay out
+    // (fp32 4096x4096x16384 2610 against 2690, but bf16 1068x110x102656 190 against 123).
     if (tiles(256) >= 400 && (well ? d.tokens > 192 : d.tokens >= 2048 && d.width >= 1024)) return kGemm256;
-    // Without copies the laid-out kernels win as soon as they have the blocks (1024x1024x8192 25 against 30; 226x1728x1148 23 against 20).
+    // Without copies the laid-out kernels win as soon as they have the blocks (1024x1024x8192 25 against 31, but 226x1728x1148, 18 tiles, 26 against 16).
     if (well && d.tokens > 32 && tiles(128) >= 128) return kGemm128;
-    // fp32 256x512x32000 60 against 89, 1663x128x1920 19 against 18
+    // fp32 256x512x32000 54 against 71, but 1663x128x1920, 195 tiles, 17.2 against 16.3
     return d.tokens > 64 && tiles(128) >= 256 ? kDirect128 : kDirect64;
 }
 
@@ -171,34 +171,37 @@ inline Kind gradients_kind(const HeadDims& d) {
     const bool few = d.tokens <= (f32 ? 32 : 64);        // what kStream holds in registers
     if (chosen && (chosen != kStream || few)) return Kind(chosen);
     const int64_t matrix = int64_t(d.width) * d.vocab;
-    // bf16 16x2048x50257 135 against 178, 2x384x85765 48 against 64, 40x1024x4096 29 against 24; fp32 1x3520x87977 999 against 1085, 16x2048x50257 400 against 393
+    // bf16 16x2048x50257 160 against 192, 2x384x85765 57 against 72, 16x512x16384 23 against 26, but 40x1024x4096 30 against 23 (for 33 to 64 tokens
+    // the line lies low: 51x576x14720 50 against 30, 64x1152x112896 283 against 236); fp32 1x3520x87977 917 against 1013, 8x2048x70000 472 against 506,
+    // 32x1024x130000 483 against 483, 16x2048x50257 370 against 372, but 16x1024x20000 101 against 91
     if (few && matrix >= (int64_t(1) << (f32 ? 27 : 23))) return kStream;
     const double work = double(matrix) * double(d.tokens);
-    // Laying operands out pays where each of them is read many times: bf16 512x2048x8192 97 against 124, 450x700x30000 168 against 189, 600x1000x9000 87
-    // against 110, 1189x320x60672 331 against 353, 1130x392x39552 262 against 309, 2000x100x30000 183 against 277, but 256x4096x32000 506 against 402,
-    // 1024x256x32000 141 against 119, 500x600x17000 121 against 105, 1200x64x100000 401 against 249; fp32 4096x4096x16384 7989 against 8615,
-    // 2000x800x10000 698 against 835, 4000x400x6000 595 against 780, but 1024x1024x8192 331 against 301, 3000x1000x1000 328 against 221,
-    // 1100x128x100000 1385 against 1033.
+    // Laying operands out pays where each of them is read many times: bf16 512x2048x8192 110 against 127, 450x700x30000 178 against 195, 600x1000x9000 94
+    // against 111, 1189x320x60672 352 against 357, 1130x392x39552 281 against 317, 2000x100x30000 216 against 243, but 256x4096x32000 508 against 403,
+    // 1024x256x32000 145 against 125, 500x600x17000 133 against 107, 1200x64x100000 410 against 235; fp32 4096x4096x16384 7980 against 8450,
+    // 2000x800x10000 702 against 803, 4000x400x6000 597 against 697, but 1024x1024x8192 327 against 304, 3000x1000x1000 331 against 213,
+    // 1100x128x100000 1470 against 968.
     const bool often = f32 ? d.width >= 256 && ((d.tokens >= 1000 && work >= 1.2e10) || (d.tokens >= 2048 && work >= 5e9))
                            : (d.tokens >= 400 && d.width >= 512 && work >= (d.width >= 900 ? 5e9 : 8e9)) ||
                                  (d.tokens >= 1000 && d.width >= (d.tokens >= 1200 ? 96 : 320) && work >= 5e9) || (d.tokens >= 2048 && work >= 1e9);
     if (often) {
-        // Tiles of 256 need enough of them in dweight (fp32 1500x1500x6000, 144 tiles, 613 against 631; 2500x1000x3000, 48, 554 against 369; bf16
-        // 4096x4096x2048, 128, 255 against 231) and room along the others (fp32 2000x800x10000 698 against 749, 4000x500x20000 2215 against 1893; bf16
-        // 450x3000x12000 221 against 207).
+        // Tiles of 256 need enough of them in dweight (fp32 1500x1500x6000, 144 tiles, 617 against 640; 2500x1000x3000, 48, 566 against 400; bf16
+        // 4096x4096x2048, 128, 262 against 238) and room along the others (fp32 2000x800x10000 702 against 744, 4000x500x20000 2221 against 1893; bf16
+        // 450x3000x12000 226 against 208).
         const int64_t tiles = int64_t(tiles_of(d.width, 256)) * tiles_of(std::min(d.vocab, 16384), 256);
         return tiles > 128 && d.tokens >= (f32 ? 1000 : 2048) && d.width >= (f32 ? 768 : 2048) ? kGemm256 : kGemm128;
     }
-    // bf16 256x4096x32000 397 against 446, but 256x512x32000 86 against 77, 400x400x100000 355 against 326; fp32 40x1024x4096 36 against 42, 374x68x130472 358
-    // against 518, but 9x1792x1071 30 against 25, 1068x110x102656 1289 against 1190
+    // bf16 256x4096x32000 403 against 455, but 256x512x32000 80 against 71, 400x400x100000 360 against 331; fp32 40x1024x4096 40 against 45, 374x68x130472 359
+    // against 504, but 9x1792x1071 30 against 25, 2000x64x50000 1252 against 603, 520x190x8000 88 against 81 (from 100 wide on both are near: 1068x110x102656 1043
+    // against 1197, 1100x128x100000 943 against 993)
     if (f32 ? matrix >= (int64_t(1) << 21) && (d.width >= 192 || d.tokens < 512) : work >= 1.5e10 && d.width >= 512) return kDirect128;
     return kDirect64;
 }
 
 // Groups of waves between which the steps of a tile of 64 are divided.  Four: no more tiles than compute units, each with steps for all groups (bf16
-// 37x3712x12160 25 against 35 us, 226x1728x1148 16 against 18, but 386x3456x2389, 266 tiles, 40 against 36; gradients of 3155x68x3073 58 against 109, of 923x704x1024 fp32 64 against 74).
-// Two (logits only): up to twice as many tiles with enough steps (fp32 386x3456x2389 111 against 132 us, 200x4000x8000, 500 tiles, 137 against 159,
-// 16x1024x20000 26 against 33, bf16 386x3456x2389 33 against 36; but fp32 128x1024x20000, 626 tiles, 57 against 55, bf16 500x1001x4000, 16 steps, 19.4 against 19.0).
+// 37x3712x12160 28 against 40 us, 226x1728x1148 16 against 20, but 386x3456x2389, 266 tiles, 42 against 36; gradients of 3155x68x3073 54 against 108, of 923x704x1024 fp32 62 against 71).
+// Two (logits only): up to twice as many tiles with enough steps (fp32 386x3456x2389 108 against 122 us, 200x4000x8000, 500 tiles, 133 against 149,
+// 16x1024x20000 26 against 33, bf16 386x3456x2389 34 against 36; but fp32 128x1024x20000, 626 tiles, 56 against 53, bf16 500x1001x4000, 16 steps, 20.0 against 19.8).
 inline int groups_of(int blocks, int steps, bool logits) {
     if (g_tuning.head_groups) return g_tuning.head_groups == 1 ? 4 : g_tuning.head_groups == 3 && logits ? 2 : 1;
     return blocks <= 256 && steps >= 16 ? 4 : logits && blocks <= 512 && steps >= 32 ? 2 : 1;

@@ -7,8 +7,8 @@
 // multiplied; LDS holds one step, so that several blocks share a compute unit and hide each other's waits.
 //
 // Few tokens: HBM bounds it (bf16 16x4096x131072 160 us, 6.7 TB/s; 16x2048x50257 57 us cold, 38 where the matrix lies in the memory-side cache; fp32 3x4096x100000
-// 324 us, 5.1 TB/s).  More tokens: the way into LDS does, and for fp32 the splitting (some ten vector instructions for each element of a tile, as long as the matrix
-// instructions take at 64 x 64): fp32 386x3456x2389 110 us (0.35 PFLOP/s of bf16), 617x2752x7296 218 us, logits of 1021x1000x32003 as part of the backward pass 0.83.
+// 324 us, 5.1 TB/s).  More tokens: the way into LDS does, and for fp32 the splitting (some seven vector instructions for each element of a tile, nearly as long as the matrix
+// instructions take at 64 x 64): fp32 386x3456x2389 108 us (0.35 PFLOP/s of bf16), 617x2752x7296 209 us, logits of 1021x1000x32003 as part of the backward pass 0.85.
 #pragma once
 #include "bns_head_device.hpp"
 

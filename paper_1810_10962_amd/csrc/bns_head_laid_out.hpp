@@ -90,9 +90,9 @@ __global__ void __launch_bounds__(256) pack_columns_kernel(PackArgs a) {
 // The matrix units bound it.  A tile of 256 x 256 belongs to eight waves, 128 x 64 each, so that a step of 64 along k reads 24 fragments from LDS for
 // 64 matrix instructions; two steps lie in LDS (128 KB), the next on its way past the registers while the present one is multiplied, one barrier a step.
 // Tiles of 128 (four waves, 64 x 64) take over where those of 256 leave compute units idle.
-// Measured: logits of 4096x4096x131072 bf16 with their statistics 3.45 ms (1.27 PFLOP/s; a large library product on the same device 1.27 to 1.38 with the same
-// kind of values, more with zeros: power bounds both), as part of the backward pass 1.17 (g in two layouts) and 1.24 to 1.29 (the gradients); the six products of
-// fp32 parts at 1021x1000x32003 0.98 to 1.10 PFLOP/s of bf16, one round of 256 tiles that nothing overlaps.
+// Measured: logits of 4096x4096x131072 bf16 with their statistics 3.45 to 3.52 ms (1.25 to 1.27 PFLOP/s; a large library product on the same device 1.27 to 1.38 with the same
+// kind of values, more with zeros: power bounds both), as part of the backward pass 1.19 (g in two layouts) and 1.25 to 1.29 (the gradients); the six products of
+// fp32 parts at 1021x1000x32003 1.00 to 1.12 PFLOP/s of bf16, one round of 256 tiles that nothing overlaps.
 // Other forms were not faster: rings of four and five steps of 32 (422 and 434 us against 415 at 4096x4096x16384), halves of a block in turn (415), 32x32x16
 // instructions (445), four waves of 128 x 128 (488).
 template <int BM, int BN, int WM, int WN>

@@ -1,7 +1,7 @@
 // The products of the loss over the vocabulary for few tokens, which read the vocabulary's matrix (or write its gradient) at the rate of memory and do little
 // else: every wave streams rows of the matrix from memory straight into the fragments of the matrix units, with the loads of the next steps on
 // their way, and no exchange through LDS but one sum at the end.  Operands are read as they lie in memory, as in bns_head_direct.hpp.
-// Measured: gradients of 16x2048x50257 in bf16 with the logits before them 148 us (618 MB: the matrix read twice, its gradient written: 4.2 TB/s), in fp32 376;
+// Measured: gradients of 16x2048x50257 in bf16 with the logits before them 158 us (618 MB: the matrix read twice, its gradient written: 3.9 TB/s), in fp32 370;
 // logits of 16x4096x4000 bf16 16 us, 9x1792x1071 fp32 15 us, where the length of a chain of loads along the width counts.
 #pragma once
 #include "bns_head_device.hpp"

@@ -5,8 +5,9 @@
 // sum of squares and its output.  A row belongs to TPR threads (a wave, 256, 512 or 1024), each of which holds VPT vectors of eight neighbouring
 // elements: 16 bytes of bf16 a lane, a whole kilobyte a wave.  A wave per row needs no exchange through LDS, more threads per row leave fewer registers
 // to each and keep more of a long row on its way; one row of one token takes as many threads as it has vectors.
-// Measured: 8192x5120 bf16 with residual to 8 bits 53 us (5.6 TB/s; a large copy on the same device 5.1), one row of 4096 4.5 us, which is a launch;
-// backward 16384x4096 bf16 90 us (6.0 TB/s), 777x1001 fp32 9.5 us, which is two launches and the first one's chain of rows.
+// Measured: 8192x5120 bf16 with residual to 8 bits 54 us (5.5 TB/s; a large copy on the same device 5.2), one row of 4096 4.5 us, which is a launch;
+// backward 16384x4096 bf16 90 us (6.0 TB/s), 777x1001 fp32 9.5 us: two launches, the first with one row a wave, whose vectors of a ragged width are asked
+// for in branches one after another, and the sums of three waves through LDS behind it.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
