@@ -407,11 +407,12 @@ typedef struct {
 
 /* Residual addition and root-mean-square norm of every row:
  *   s = x + residual (s = x where residual is NULL)      rstd = 1 / sqrt(mean(s^2) + eps)      v = weight * s * rstd
- * s is held in fp32 on its way to the norm; sum receives it rounded to dtype.
+ * s is held in fp32 on its way to the norm; sum receives it rounded to dtype.  So are the squares: where elements beyond 1.8e19 make their mean overflow, rstd is 0, and
+ * with eps = 0 a row whose squares all underflow has rstd = infinity.
  * y = v rounded to dtype, or in 8 bits (OCP e4m3: 4 exponent bits, 3 mantissa bits, largest value 448) with
  *   scales[group] = max(max |v| / 448, 2^-126)           y = e4m3(v / scales[group]), round to nearest even
  * so that v = y * scales up to that rounding.  scales is float[rows][ceil(width / group)], dense (float[rows] for group = 0).
- * Elements that are NaN stay NaN in y; scales are those of the others.
+ * Elements that are NaN stay NaN in y; scales are those of the others.  An infinite v makes its group's scale infinite, its own y NaN and the others 0.
  * in: x, residual (may be NULL), weight[width].  out: sum (may be NULL; must be without residual), y, scales (BNS_OUT_E4M3, else NULL),
  * rstd[rows] (may be NULL).  In place: sum on x or on residual; y on x (BNS_OUT_SAME, no sum on it). */
 bns_status bns_rms_forward(const bns_rms* rms, const void* x, const void* residual, const void* weight,
@@ -440,13 +441,15 @@ typedef struct {
     int32_t piece;         /* rows of weight that the workspace holds something for at a time; 0: the library's choice */
 } bns_head;
 
-/* Bytes of workspace of bns_head_forward and bns_head_backward (the larger of the two); 0 for an invalid description. */
+/* Bytes of workspace of bns_head_forward and bns_head_backward (the larger of the two); 0 for an invalid description.  The backward pass needs most of it: a program
+ * that only scores takes a small piece, which costs the forward pass nothing where hidden and weight need no copies (bf16, width and strides multiples of 64 and 8). */
 size_t bns_head_workspace_bytes(const bns_head* head);
 
 /* Softmax cross entropy of the logits z = hidden weight^T, which are never stored whole:
  *   lse[t] = log sum over v of exp(z[t][v])              loss[t] = lse[t] - z[t][targets[t]]
  * A token whose target lies outside [0, vocab) is left out: its loss is 0 (its lse is not).
- * Logits of -infinity count for nothing in the sum; a token with a logit that is NaN or +infinity has a loss that is NaN (or infinite).
+ * Logits of -infinity count for nothing in the sum (as the target of a token that counts they make its loss infinite); a token with a logit that is NaN or +infinity
+ * has a loss that is NaN (or infinite).
  * Products of bf16 are summed in fp32; f32 operands enter the matrix units as three bf16 parts each, the six products
  * that reach an fp32 result's last bits.
  * in: hidden[tokens][width], weight[vocab][width], targets[tokens].  out: loss[tokens], lse[tokens]. */
