@@ -493,6 +493,114 @@ bns_status bns_distill_forward(const bns_distill* distill, const void* logits, c
 bns_status bns_distill_backward(const bns_distill* distill, const void* logits, const int64_t* ids, const float* teacher,
                                 const float* lse, const float* dloss, void* dlogits, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * A step on a model's own answers: queries and keys, log probabilities of the tokens that were drawn, the gradients' norm.
+ *
+ * The conventions of the language-model calls above hold, but for alignment: tensors and vectors may begin at any element of their type (slices of larger
+ * ones), the workspace on 16 bytes. */
+
+/* Where a tensor of heads lies: elements from token to token and from head to head; the `width` elements of a head are neighbours.  0 stands for dense
+ * tokens (heads x width) and dense heads (width).  Either the heads of a token come before the next token (slices of a projection's result) or the tokens
+ * of a head before the next head (head-major); the stride of a dimension of one entry does not matter. */
+typedef struct {
+    int64_t token;
+    int64_t head;
+} bns_head_strides;
+
+/* Queries and keys of `tokens` tokens.  Limits: tokens < 2^31, heads < 2^20 each, width <= 512, tensors that reach over fewer than 2^48 elements. */
+typedef struct {
+    int64_t tokens;
+    bns_head_strides q, k;          /* queries, keys */
+    bns_head_strides q_out, k_out;  /* forward: results; backward: gradients of the results */
+    bns_head_strides dq, dk;        /* backward: gradients of queries, keys */
+    int32_t q_heads, k_heads;       /* 0: none of them (their pointers may be NULL) */
+    int32_t width;                  /* of a head */
+    int32_t rotated;                /* the first `rotated` elements of a head take part in the rotation: even, 0 to width */
+    int32_t interleaved;            /* pairs of a rotation are 0: elements i and i + rotated / 2; 1: elements 2 i and 2 i + 1 */
+    int32_t dtype;                  /* bns_dtype of queries, keys, results and their gradients */
+    int32_t weight_dtype;           /* bns_dtype of the weights */
+    float eps;                      /* >= 0 */
+} bns_qk;
+
+/* Root-mean-square norm of every head of the queries and keys, and behind it the rotation by position:
+ *   v = weight * x / sqrt(mean(x^2) + eps)      (v = x where the weight is NULL)
+ *   y_a = v_a cos(w) - v_b sin(w),  y_b = v_a sin(w) + v_b cos(w)      for pair i = (a, b) of the rotated elements, w = positions[t] * frequencies[i]
+ *   y = v for the others.
+ * All in fp32 (squares and their mean as bns_rms_forward) and rounded once; w is formed and reduced in fp64, so that far positions (any whole number up to
+ * 2^31 in magnitude) turn as exactly as near ones.
+ * in: q, k, q_weight[width], k_weight[width] (NULL: no norm), positions[tokens], frequencies[rotated / 2] (fp64, radians per position; both may be
+ * NULL where rotated is 0).  out: q_out, k_out.  In place: q_out on q, k_out on k (address and strides). */
+bns_status bns_qk_forward(const bns_qk* qk, const void* q, const void* k, const void* q_weight, const void* k_weight, const int64_t* positions,
+                          const double* frequencies, void* q_out, void* k_out, void* stream);
+
+/* Bytes of workspace of bns_qk_backward; 0 for an invalid description. */
+size_t bns_qk_workspace_bytes(const bns_qk* qk);
+
+/* Gradients, with g the gradient of v (dq_out, dk_out turned back), r = 1 / sqrt(mean(x^2) + eps) and x^ = x r, worked out from x again:
+ *   dx = r (weight * g - x^ mean(weight * g * x^))  (dx = g without a weight)      dweight = sum over tokens and heads of g * x^
+ * in: q, k (NULL where there is no weight), the weights, positions, frequencies, dq_out, dk_out.  out: dq, dk, dq_weight[width], dk_weight[width] (float; NULL
+ * exactly where the weight is).  In place: dq on dq_out, dk on dk_out. */
+bns_status bns_qk_backward(const bns_qk* qk, const void* q, const void* k, const void* q_weight, const void* k_weight, const int64_t* positions,
+                           const double* frequencies, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of logits.  Limits: tokens < 2^31, vocab < 2^30, top <= 128 (and at most vocab), temperature from 10^-6 to 10^6, strides < 2^31. */
+typedef struct {
+    int64_t tokens;
+    int64_t logits_stride;  /* logits */
+    int64_t dlogits_stride; /* dlogits */
+    int32_t vocab;
+    int32_t top;            /* alternatives that are reported; 0: none */
+    int32_t dtype;          /* bns_dtype of logits, dlogits */
+    float temperature;      /* > 0 */
+} bns_logprob;
+
+/* Bytes of workspace of bns_logprob_forward; 0 for an invalid description. */
+size_t bns_logprob_workspace_bytes(const bns_logprob* logprob);
+
+/* Log probabilities, entropy and the most probable alternatives, with tau = temperature and, for each row,
+ *   m = largest logit      s = log sum over v of exp((logits[v] - m) / tau)      log p[v] = (logits[v] - m) / tau - s
+ *   logp[t] = log p[targets[t]] (0 where the target lies outside [0, vocab): left out)      entropy[t] = - sum over v of p[v] log p[v]
+ *   stats[t] = {m, s}      top_ids[t], top_logp[t]: the `top` largest logits in falling order, the lowest index first among equal ones, and their log p
+ * Logits of -infinity have p = 0 and count for nothing in the entropy; they come last among the alternatives, by index.  A row of nothing else has m = -infinity,
+ * s = 0, log p = -infinity and entropy 0.  Rows that hold the type's lowest value everywhere are equal probabilities.  A row with a logit that is NaN or
+ * +infinity has s, logp, entropy and top_logp that are NaN; its alternatives are those of the other logits (NaN ranks with -infinity).
+ * in: logits[tokens][vocab], targets[tokens] (may be NULL, then logp is).  out: logp[tokens], entropy[tokens] (may be NULL), stats[tokens][2] (may be NULL),
+ * top_ids[tokens][top], top_logp[tokens][top] (where top > 0, else NULL). */
+bns_status bns_logprob_forward(const bns_logprob* logprob, const void* logits, const int64_t* targets, float* logp, float* entropy, float* stats,
+                               int64_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of sum over t of dlogp[t] logp[t] + dentropy[t] entropy[t] (tokens that are left out: dlogp counts as 0, whatever it holds):
+ *   dlogits[t][v] = (dlogp[t] ([v = targets[t]] - p[v]) - dentropy[t] p[v] (log p[v] + entropy[t])) / tau
+ * A row for which dlogp and dentropy are 0, or which holds nothing but -infinity (m, as stats has it), gets 0 whatever else its logits hold.
+ * in: logits, targets (NULL exactly where dlogp is), stats and entropy of the forward call (entropy may be NULL where dentropy is), dlogp[tokens],
+ * dentropy[tokens] (either may be NULL, which stands for zeros).  out: dlogits.  In place: dlogits on logits. */
+bns_status bns_logprob_backward(const bns_logprob* logprob, const void* logits, const int64_t* targets, const float* stats, const float* entropy,
+                                const float* dlogp, const float* dentropy, void* dlogits, void* stream);
+
+/* One of many gradients, `elements` neighbouring elements, and where it goes when it is scaled (`out`: grad itself, or memory of its own). */
+typedef struct {
+    const void* grad;
+    void* out;
+    int64_t elements;   /* 0: nothing (the pointers may be NULL) */
+    int32_t dtype;      /* bns_dtype of grad and out */
+    int32_t reserved;   /* 0 */
+} bns_gradient;
+
+/* The norm of all gradients together, and their scaling down to a largest norm.  `gradients` is a HOST array of `count` entries (at most 65536, fewer than 2^40
+ * elements each and 2^44 together) that is read before the call returns; a captured call keeps what it said.
+ *   squares = sum over all elements of grad^2 (fp64: no gradient of finite elements overflows)      norm = sqrt(squares)
+ *   c = min(1, max_norm / (norm + 1e-6))      out = grad * c, rounded to dtype
+ * Where the norm is NaN so are c and what is scaled; where it is infinite, c = 0 (infinite elements become NaN).  Gradients in place with c = 1 are left as they are.
+ * bns_grads_clip does it all.  bns_grads_norm and bns_grads_scale are its two halves, for a caller whose gradients lie on several devices: squares are added up between.
+ * An `out` may be its own grad, and overlaps no other grad or out; a grad may occur more than once, and counts as often.
+ * max_norm: >= 0, finite.  squares[1], norm[1]: device; norm may be NULL in bns_grads_norm and bns_grads_scale. */
+size_t bns_grads_workspace_bytes(int32_t count);     /* 0 for a count out of range */
+bns_status bns_grads_norm(const bns_gradient* gradients /* HOST */, int32_t count, double* squares, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+bns_status bns_grads_scale(const bns_gradient* gradients /* HOST */, int32_t count, const double* squares, float max_norm, float* norm, void* workspace,
+                           size_t workspace_bytes, void* stream);
+bns_status bns_grads_clip(const bns_gradient* gradients /* HOST */, int32_t count, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

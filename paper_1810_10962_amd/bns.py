@@ -60,6 +60,25 @@ class bns_distill(C.Structure):
                 ("k", C.c_int32), ("dtype", C.c_int32), ("temperature", C.c_float)]
 
 
+class bns_head_strides(C.Structure):
+    _fields_ = [("token", C.c_int64), ("head", C.c_int64)]
+
+
+class bns_qk(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("q", bns_head_strides), ("k", bns_head_strides), ("q_out", bns_head_strides), ("k_out", bns_head_strides),
+                ("dq", bns_head_strides), ("dk", bns_head_strides), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("width", C.c_int32),
+                ("rotated", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32), ("weight_dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class bns_logprob(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("logits_stride", C.c_int64), ("dlogits_stride", C.c_int64), ("vocab", C.c_int32),
+                ("top", C.c_int32), ("dtype", C.c_int32), ("temperature", C.c_float)]
+
+
+class bns_gradient(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("elements", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
 class BnsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -71,7 +90,8 @@ _lib = _call = None
 _P = C.c_void_p
 _SHP, _SPC = C.POINTER(bns_shape), C.POINTER(bns_spec)
 _RMS, _HEAD, _DISTILL = C.POINTER(bns_rms), C.POINTER(bns_head), C.POINTER(bns_distill)
-_STRUCTURES = (_SHP, _SPC, _RMS, _HEAD, _DISTILL)
+_QK, _LOGPROB = C.POINTER(bns_qk), C.POINTER(bns_logprob)
+_STRUCTURES = (_SHP, _SPC, _RMS, _HEAD, _DISTILL, _QK, _LOGPROB)
 _PROTOS = {
     "bns_status_string": (C.c_char_p, [C.c_int]),
     "bns_sample_index": (C.c_int, [_SHP, _SPC, C.c_uint64, C.POINTER(bns_box)]),
@@ -105,18 +125,30 @@ _PROTOS = {
     "bns_head_backward": (C.c_int, [_HEAD, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
     "bns_distill_forward": (C.c_int, [_DISTILL, _P, _P, _P, _P, _P, _P, _P, _P]),
     "bns_distill_backward": (C.c_int, [_DISTILL, _P, _P, _P, _P, _P, _P, _P]),
+    "bns_qk_forward": (C.c_int, [_QK, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "bns_qk_workspace_bytes": (C.c_size_t, [_QK]),
+    "bns_qk_backward": (C.c_int, [_QK, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "bns_logprob_workspace_bytes": (C.c_size_t, [_LOGPROB]),
+    "bns_logprob_forward": (C.c_int, [_LOGPROB, _P, _P, _P, _P, _P, _P, _P, _P, C.c_size_t, _P]),
+    "bns_logprob_backward": (C.c_int, [_LOGPROB, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "bns_grads_workspace_bytes": (C.c_size_t, [C.c_int32]),
+    "bns_grads_norm": (C.c_int, [_P, C.c_int32, _P, _P, _P, C.c_size_t, _P]),
+    "bns_grads_scale": (C.c_int, [_P, C.c_int32, _P, C.c_float, _P, _P, C.c_size_t, _P]),
+    "bns_grads_clip": (C.c_int, [_P, C.c_int32, C.c_float, _P, _P, C.c_size_t, _P]),
 }
 
 
 _EVERY_STEP = ("forward", "backward", "forward_mixed", "backward_mixed", "inference")
 _EVERY_STEP_LM = ("rms_forward", "rms_backward", "head_forward", "head_backward", "distill_forward", "distill_backward")
 
+_EVERY_STEP_ANSWERS = ("qk_forward", "qk_backward", "logprob_forward", "logprob_backward", "grads_norm", "grads_scale", "grads_clip")
+
 
 class _NoExtension:
     """What _bnscall is to an interpreter that has none: every call is left to ctypes."""
 
 
-for _name in _EVERY_STEP + _EVERY_STEP_LM:
+for _name in _EVERY_STEP + _EVERY_STEP_LM + _EVERY_STEP_ANSWERS:
     setattr(_NoExtension, _name, staticmethod(lambda *args: None))
 
 
@@ -138,7 +170,7 @@ def load(reload: bool = False):
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
-    global _call, _raw_stream
+    global _call, _raw_stream, _current_device
     call = _NoExtension
     if os.path.exists(CALL_PATH):
         spec = importlib.util.spec_from_file_location("_bnscall", CALL_PATH)
@@ -146,9 +178,11 @@ def load(reload: bool = False):
         spec.loader.exec_module(call)
         call.bind(bns_shape, bns_spec, *(C.cast(getattr(lib, "bns_" + name), C.c_void_p).value for name in _EVERY_STEP))
         call.bind_lm(bns_rms, bns_head, bns_distill, *(C.cast(getattr(lib, "bns_" + name), C.c_void_p).value for name in _EVERY_STEP_LM))
+        call.bind_answers(bns_qk, bns_logprob, *(C.cast(getattr(lib, "bns_" + name), C.c_void_p).value for name in _EVERY_STEP_ANSWERS))
     # The current stream of a device as an integer: torch's own accessor where it has one, a tenth of the time of
     # building a Stream object (1.2 us of a call whose kernels take 4).
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _current_device = getattr(torch._C, "_cuda_getDevice", None)
     _lib, _call = lib, call
     return lib
 
@@ -177,7 +211,7 @@ def missing_symbols():
 # The prototypes in _PROTOS convert Python integers and floats themselves, so the calls below hand over plain values:
 # building a ctypes object for each argument took half of the 8.5 us that a call took on the host, ctypes itself another
 # 1.5 of 5.1 in the calls that now go through _bnscall, which adds 0.8 to the library and the launch.
-_raw_stream = None
+_raw_stream = _current_device = None
 
 
 def _ptr(t):
@@ -445,6 +479,103 @@ def bns_distill_backward(distill, logits, ids, teacher, lse, dloss, dlogits):
     if status is None:
         status = _by_ctypes("bns_distill_backward", distill, logits, ids, teacher, lse, dloss, dlogits, _stream(logits))
     _check(status, "bns_distill_backward")
+
+
+# --------------------------------------------------------------------------------------
+# a step on a language model's own answers
+# --------------------------------------------------------------------------------------
+def make_qk(tokens, q_heads, k_heads, width, dtype="bf16", *, rotated=None, interleaved=False, weight_dtype="f32", eps=1e-6, q=(0, 0), k=(0, 0),
+            q_out=(0, 0), k_out=(0, 0), dq=(0, 0), dk=(0, 0)) -> bns_qk:
+    """q, k, q_out, ...: strides from token to token and from head to head, in elements."""
+    strides = (bns_head_strides(*s) for s in (q, k, q_out, k_out, dq, dk))
+    return bns_qk(tokens, *strides, q_heads, k_heads, width, width if rotated is None else rotated, int(interleaved), _dtype(dtype), _dtype(weight_dtype), eps)
+
+
+def make_logprob(tokens, vocab, dtype="bf16", *, top=0, temperature=1.0, logits_stride=0, dlogits_stride=0) -> bns_logprob:
+    return bns_logprob(tokens, logits_stride, dlogits_stride, vocab, top, _dtype(dtype), temperature)
+
+
+class Gradients:
+    """Gradients as bns_grads_* take them, with where they go (``outs``; None: nowhere, for bns_grads_norm).  Holds the tensors, whose addresses it has: a program
+    that gets new tensors makes a new one."""
+
+    def __init__(self, grads, outs=None):
+        import torch
+        types = {torch.float32: BNS_F32, torch.bfloat16: BNS_BF16}
+        self.grads, self.outs, self.count = list(grads), None if outs is None else list(outs), len(grads)
+        if outs is not None and len(self.outs) != self.count:
+            raise ValueError(f"{self.count} gradients and {len(self.outs)} results")
+        self.array = (bns_gradient * max(1, self.count))()
+        for i, g in enumerate(self.grads):
+            out = None if outs is None else self.outs[i]
+            for t in (g,) if out is None else (g, out):
+                if t.dtype not in types or not t.is_contiguous():
+                    raise ValueError(f"gradient {i}: float32 or bfloat16 and contiguous is wanted")
+            if out is not None and (out.dtype != g.dtype or out.numel() != g.numel()):
+                raise ValueError(f"gradient {i}: its result has another type or size")
+            self.array[i] = bns_gradient(g.data_ptr(), None if out is None else out.data_ptr(), g.numel(), types[g.dtype], 0)
+
+    def data_ptr(self):
+        return C.addressof(self.array)
+
+
+def make_gradients(grads, outs=None) -> Gradients:
+    return Gradients(grads, outs)
+
+
+def _answers_call(name, at, *args):
+    """A call on the current stream of the device of tensor `at`."""
+    device = -1 if at is None else at.get_device()
+    if device >= 0 and _current_device is not None and device != _current_device():         # (a stream of 0 is the default one of the current device)
+        import torch
+        with torch.cuda.device(device):
+            return _answers_call(name, at, *args)
+    stream = 0 if at is None else _stream(at)        # (no tensor at all: nothing to do)
+    status = getattr(_calls(), name)(*args, stream)
+    if status is None:
+        status = _by_ctypes("bns_" + name, *args, stream)
+    _check(status, "bns_" + name)
+
+
+def bns_qk_forward(qk, q, k, q_weight, k_weight, positions, frequencies, q_out, k_out):
+    _answers_call("qk_forward", k_out if q_out is None else q_out, qk, q, k, q_weight, k_weight, positions, frequencies, q_out, k_out)
+
+
+def bns_qk_workspace_bytes(qk) -> int:
+    return int(load().bns_qk_workspace_bytes(C.byref(qk)))
+
+
+def bns_qk_backward(qk, q, k, q_weight, k_weight, positions, frequencies, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace):
+    _answers_call("qk_backward", workspace, qk, q, k, q_weight, k_weight, positions, frequencies, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace,
+                  workspace.nbytes)
+
+
+def bns_logprob_workspace_bytes(logprob) -> int:
+    return int(load().bns_logprob_workspace_bytes(C.byref(logprob)))
+
+
+def bns_logprob_forward(logprob, logits, targets, logp, entropy, stats, top_ids, top_logp, workspace):
+    _answers_call("logprob_forward", workspace, logprob, logits, targets, logp, entropy, stats, top_ids, top_logp, workspace, workspace.nbytes)
+
+
+def bns_logprob_backward(logprob, logits, targets, stats, entropy, dlogp, dentropy, dlogits):
+    _answers_call("logprob_backward", logits, logprob, logits, targets, stats, entropy, dlogp, dentropy, dlogits)
+
+
+def bns_grads_workspace_bytes(gradients) -> int:
+    return int(load().bns_grads_workspace_bytes(gradients.count))
+
+
+def bns_grads_norm(gradients, squares, norm, workspace):
+    _answers_call("grads_norm", workspace, gradients, gradients.count, squares, norm, workspace, workspace.nbytes)
+
+
+def bns_grads_scale(gradients, squares, max_norm, norm, workspace):
+    _answers_call("grads_scale", workspace, gradients, gradients.count, squares, max_norm, norm, workspace, workspace.nbytes)
+
+
+def bns_grads_clip(gradients, max_norm, norm, workspace):
+    _answers_call("grads_clip", workspace, gradients, gradients.count, max_norm, norm, workspace, workspace.nbytes)
 
 
 # --------------------------------------------------------------------------------------

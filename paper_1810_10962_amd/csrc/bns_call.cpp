@@ -27,8 +27,16 @@ decltype(&bns_head_forward) g_head_forward;
 decltype(&bns_head_backward) g_head_backward;
 decltype(&bns_distill_forward) g_distill_forward;
 decltype(&bns_distill_backward) g_distill_backward;
+decltype(&bns_qk_forward) g_qk_forward;
+decltype(&bns_qk_backward) g_qk_backward;
+decltype(&bns_logprob_forward) g_logprob_forward;
+decltype(&bns_logprob_backward) g_logprob_backward;
+decltype(&bns_grads_norm) g_grads_norm;
+decltype(&bns_grads_scale) g_grads_scale;
+decltype(&bns_grads_clip) g_grads_clip;
 PyObject *g_shape_type, *g_spec_type, *g_data_ptr;
 PyObject *g_rms_type, *g_head_type, *g_distill_type;
+PyObject *g_qk_type, *g_logprob_type;
 
 // Reads positional arguments one after the other; after one that is left to ctypes nothing more is read.  No exception stays set.
 struct Reader {
@@ -259,6 +267,96 @@ PyObject* distill_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return finish(r, [&] { return g_distill_backward(&distill, logits, ids, teacher, lse, dloss, dlogits, stream); });
 }
 
+PyObject* qk_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 10, g_qk_type);
+    const bns_qk qk = r.structure<bns_qk>(g_qk_type);
+    const void *q = r.pointer(), *k = r.pointer(), *q_weight = r.pointer(), *k_weight = r.pointer();
+    const int64_t* positions = static_cast<const int64_t*>(r.pointer());
+    const double* frequencies = static_cast<const double*>(r.pointer());
+    void *q_out = r.pointer(), *k_out = r.pointer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_qk_forward(&qk, q, k, q_weight, k_weight, positions, frequencies, q_out, k_out, stream); });
+}
+
+PyObject* qk_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 16, g_qk_type);
+    const bns_qk qk = r.structure<bns_qk>(g_qk_type);
+    const void *q = r.pointer(), *k = r.pointer(), *q_weight = r.pointer(), *k_weight = r.pointer();
+    const int64_t* positions = static_cast<const int64_t*>(r.pointer());
+    const double* frequencies = static_cast<const double*>(r.pointer());
+    const void *dq_out = r.pointer(), *dk_out = r.pointer();
+    void *dq = r.pointer(), *dk = r.pointer();
+    float *dq_weight = r.vector(), *dk_weight = r.vector();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] {
+        return g_qk_backward(&qk, q, k, q_weight, k_weight, positions, frequencies, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace, bytes, stream);
+    });
+}
+
+PyObject* logprob_forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 11, g_qk_type);
+    const bns_logprob logprob = r.structure<bns_logprob>(g_logprob_type);
+    const void* logits = r.pointer();
+    const int64_t* targets = static_cast<const int64_t*>(r.pointer());
+    float *logp = r.vector(), *entropy = r.vector(), *stats = r.vector();
+    int64_t* top_ids = static_cast<int64_t*>(r.pointer());
+    float* top_logp = r.vector();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_logprob_forward(&logprob, logits, targets, logp, entropy, stats, top_ids, top_logp, workspace, bytes, stream); });
+}
+
+PyObject* logprob_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 9, g_qk_type);
+    const bns_logprob logprob = r.structure<bns_logprob>(g_logprob_type);
+    const void* logits = r.pointer();
+    const int64_t* targets = static_cast<const int64_t*>(r.pointer());
+    const float *stats = r.vector(), *entropy = r.vector(), *dlogp = r.vector(), *dentropy = r.vector();
+    void* dlogits = r.pointer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_logprob_backward(&logprob, logits, targets, stats, entropy, dlogp, dentropy, dlogits, stream); });
+}
+
+PyObject* grads_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 7, g_qk_type);
+    const bns_gradient* gradients = static_cast<const bns_gradient*>(r.pointer());
+    const int32_t count = int32_t(r.integer());
+    double* squares = static_cast<double*>(r.pointer());
+    float* norm = r.vector();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_grads_norm(gradients, count, squares, norm, workspace, bytes, stream); });
+}
+
+PyObject* grads_scale(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 8, g_qk_type);
+    const bns_gradient* gradients = static_cast<const bns_gradient*>(r.pointer());
+    const int32_t count = int32_t(r.integer());
+    const double* squares = static_cast<const double*>(r.pointer());
+    const float max_norm = r.real();
+    float* norm = r.vector();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_grads_scale(gradients, count, squares, max_norm, norm, workspace, bytes, stream); });
+}
+
+PyObject* grads_clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    Reader r(args, n, 7, g_qk_type);
+    const bns_gradient* gradients = static_cast<const bns_gradient*>(r.pointer());
+    const int32_t count = int32_t(r.integer());
+    const float max_norm = r.real();
+    float* norm = r.vector();
+    void* workspace = r.pointer();
+    const size_t bytes = r.integer();
+    void* stream = r.stream();
+    return finish(r, [&] { return g_grads_clip(gradients, count, max_norm, norm, workspace, bytes, stream); });
+}
+
 // bind(type of bns_shape, type of bns_spec, addresses of the five functions)
 PyObject* bind(PyObject*, PyObject* args) {
     PyObject *shape, *spec;
@@ -297,11 +395,32 @@ PyObject* bind_lm(PyObject*, PyObject* args) {
     Py_RETURN_NONE;
 }
 
+// bind_answers(types of bns_qk, bns_logprob, addresses of the functions of a step on a model's own answers)
+PyObject* bind_answers(PyObject*, PyObject* args) {
+    PyObject *qk, *logprob;
+    unsigned long long f[7];
+    if (!PyArg_ParseTuple(args, "O!O!KKKKKKK", &PyType_Type, &qk, &PyType_Type, &logprob, &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6])) return nullptr;
+    g_qk_forward = reinterpret_cast<decltype(g_qk_forward)>(f[0]);
+    g_qk_backward = reinterpret_cast<decltype(g_qk_backward)>(f[1]);
+    g_logprob_forward = reinterpret_cast<decltype(g_logprob_forward)>(f[2]);
+    g_logprob_backward = reinterpret_cast<decltype(g_logprob_backward)>(f[3]);
+    g_grads_norm = reinterpret_cast<decltype(g_grads_norm)>(f[4]);
+    g_grads_scale = reinterpret_cast<decltype(g_grads_scale)>(f[5]);
+    g_grads_clip = reinterpret_cast<decltype(g_grads_clip)>(f[6]);
+    Py_INCREF(qk);
+    Py_INCREF(logprob);
+    Py_XSETREF(g_qk_type, qk);
+    Py_XSETREF(g_logprob_type, logprob);
+    Py_RETURN_NONE;
+}
+
 #define BNS_FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {{"bind", &bind, METH_VARARGS, nullptr}, BNS_FAST(forward), BNS_FAST(backward), BNS_FAST(forward_mixed),
                            BNS_FAST(backward_mixed),               BNS_FAST(inference),
                            {"bind_lm", &bind_lm, METH_VARARGS, nullptr}, BNS_FAST(rms_forward), BNS_FAST(rms_backward), BNS_FAST(head_forward),
-                           BNS_FAST(head_backward),                BNS_FAST(distill_forward), BNS_FAST(distill_backward), {nullptr, nullptr, 0, nullptr}};
+                           BNS_FAST(head_backward),                BNS_FAST(distill_forward), BNS_FAST(distill_backward),
+                           {"bind_answers", &bind_answers, METH_VARARGS, nullptr}, BNS_FAST(qk_forward), BNS_FAST(qk_backward), BNS_FAST(logprob_forward),
+                           BNS_FAST(logprob_backward), BNS_FAST(grads_norm), BNS_FAST(grads_scale), BNS_FAST(grads_clip), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_bnscall", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

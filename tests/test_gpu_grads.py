@@ -1,0 +1,165 @@
+"""The norm of many gradients and their scaling on the GPU against the definition in 64 bits.
+
+Tolerances, with u = 2^-24: squares are formed and added in fp64 (some 2^20 additions here, 2^-33 at most); norm is rounded once (u).  c is rounded once and the product
+once more: 2 u and, in bf16, half a unit of 2^-8; results below 2^-126 may lose what their type does not hold there."""
+import math
+
+import pytest
+import torch
+
+from answers_reference import HALF_ULP, U, tail_is_whole, written
+from paper_1810_10962_amd import bns
+
+pytestmark = pytest.mark.gpu
+NAMES = {torch.float32: "f32", torch.bfloat16: "bf16"}
+
+
+def make(sizes, types, seed=0, offsets=True):
+    """Gradients and places for them, each somewhere in a buffer of its own, with a pattern around the places."""
+    g = torch.Generator().manual_seed(seed)
+    grads, outs, rooms = [], [], []
+    for i, n in enumerate(sizes):
+        t = types[i % len(types)]
+        at = (3 * i + 1) % 9 if offsets else 0
+        whole = torch.full((n + 20,), float("nan")).to(t).cuda()
+        whole[at:at + n] = (torch.randn(n, generator=g) * math.exp(i % 5 - 2)).to(t).cuda()
+        grads.append(whole[at:at + n])
+        to = (5 * i + 2) % 11 if offsets else 0
+        room = torch.full((n + 20,), 7.0, device="cuda").to(t)
+        rooms.append((room, to, n))
+        outs.append(room[to:to + n])
+    return grads, outs, rooms
+
+
+def whole_norm(grads):
+    return math.sqrt(math.fsum(float(x.double().pow(2).sum()) for x in grads))
+
+
+def check(got, grads, scale):
+    for i, (o, x) in enumerate(zip(got, grads)):
+        want = x.double() * scale
+        off = (o.double() - want).abs() - want.abs() * (HALF_ULP[NAMES[x.dtype]] + 3 * U) - 2.0 ** -126
+        worst = float(off.max()) if off.numel() else 0.0
+        assert worst <= 0, f"gradient {i}: worst excess {worst:.3e}"
+
+
+SETS = {"one": [1], "none": [], "empty ones": [0, 5, 0, 0, 7, 0], "small": [1, 2, 3, 7, 8, 9, 15, 16, 17, 100], "ends of pieces": [8191, 8192, 8193, 16383, 16384, 16385, 32768, 32769],
+        "many": [(i * 37) % 501 + 1 for i in range(96)], "more than travel with a launch": [(i * 37) % 301 for i in range(330)], "large": [3_000_001, 5, 1_048_576]}
+
+
+@pytest.mark.parametrize("types", [(torch.float32,), (torch.bfloat16,), (torch.float32, torch.bfloat16, torch.bfloat16)], ids=["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("name", list(SETS))
+def test_clip(name, types):
+    print(f"[gpu-case] clip {name} {types}", flush=True)
+    grads, outs, rooms = make(SETS[name], types)
+    norm = whole_norm(grads)
+    gradients = bns.make_gradients(grads, outs)
+    room = bns.bns_grads_workspace_bytes(gradients)
+    workspace, space = written(room, dtype=torch.uint8)
+    kept = [x.clone() for x in grads]
+    for part in (0.3, 1.7):
+        max_norm = norm * part
+        got, one = written(1)
+        bns.bns_grads_clip(gradients, max_norm, one, space)
+        assert abs(float(one[0]) - norm) <= 2 * U * norm
+        check(outs, kept, min(1.0, max_norm / (norm + 1e-6)))
+        if part > 1:
+            assert all(torch.equal(o, x) for o, x in zip(outs, kept))
+        tail_is_whole(got, 1)
+    assert all(torch.equal(a, b) for a, b in zip(grads, kept))
+    for whole, to, n in rooms:
+        assert bool((whole[:to] == 7).all()) and bool((whole[to + n:] == 7).all())
+    tail_is_whole(workspace, room)
+    # the two halves of it, with the sum in between; the same bits
+    squares, norm2 = torch.empty(1, dtype=torch.float64, device="cuda"), torch.empty(1, device="cuda")
+    first = [o.clone() for o in outs]
+    bns.bns_grads_norm(bns.make_gradients(grads), squares, norm2, space)
+    assert abs(float(squares[0]) - norm * norm) <= 2.0 ** -33 * norm * norm and torch.equal(norm2, one)
+    bns.bns_grads_scale(gradients, squares, norm * 1.7, None, space)
+    assert all(torch.equal(a, b) for a, b in zip(first, outs))
+    bns.bns_grads_scale(gradients, squares * 4, norm * 0.3, norm2, space)       # as if three more devices had gradients like these
+    check(outs, kept, min(1.0, 0.3 * norm / (2 * norm + 1e-6)))
+    assert abs(float(norm2[0]) - 2 * norm) <= 3 * U * norm
+
+
+@pytest.mark.parametrize("types", [(torch.float32,), (torch.bfloat16,), (torch.float32, torch.bfloat16)], ids=["f32", "bf16", "mixed"])
+def test_in_place(types):
+    print(f"[gpu-case] clip in place {types}", flush=True)
+    grads, _, _ = make([513, 20000, 3, 70001], types, seed=2)
+    kept, norm, one = [x.clone() for x in grads], whole_norm(grads), torch.empty(1, device="cuda")
+    gradients = bns.make_gradients(grads, grads)
+    space = torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda")
+    bns.bns_grads_clip(gradients, 2 * norm, one, space)
+    assert all(torch.equal(a, b) for a, b in zip(grads, kept))
+    bns.bns_grads_clip(gradients, norm / 3, one, space)
+    check(grads, kept, norm / 3 / (norm + 1e-6))
+    before = [x.clone() for x in grads]
+    bns.bns_grads_clip(gradients, 0.0, one, space)
+    assert all(bool((x == 0).all()) for x in grads) and not all(bool((x == 0).all()) for x in before)
+
+
+def test_a_gradient_that_comes_twice_counts_twice():
+    print("[gpu-case] clip the same gradient twice", flush=True)
+    x = torch.full((100,), 3.0, device="cuda")
+    outs, one = [torch.empty_like(x), torch.empty_like(x)], torch.empty(1, device="cuda")
+    gradients = bns.make_gradients([x, x], outs)
+    space = torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda")
+    bns.bns_grads_clip(gradients, 1.0, one, space)
+    assert abs(float(one[0]) - math.sqrt(1800)) < 1e-5
+    check(outs, [x, x], 1 / (math.sqrt(1800) + 1e-6))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_large_and_small_elements(dtype):
+    """Squares beyond what 32 bits hold, at both ends."""
+    print(f"[gpu-case] clip extremes {dtype}", flush=True)
+    one, squares = torch.empty(1, device="cuda"), torch.empty(1, dtype=torch.float64, device="cuda")
+    for value in (2.0 ** 100, 2.0 ** 126, 2.0 ** -100, 2.0 ** -126):
+        x = torch.full((1000,), value, dtype=dtype, device="cuda")
+        out = torch.empty_like(x)
+        gradients = bns.make_gradients([x], [out])
+        space = torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda")
+        bns.bns_grads_norm(gradients, squares, one, space)
+        assert abs(float(squares[0]) / (1000 * value * value) - 1) < 1e-12
+        assert float(one[0]) == math.inf if value * math.sqrt(1000) > 3.4e38 else abs(float(one[0]) / (value * math.sqrt(1000)) - 1) < 2 * U
+        bns.bns_grads_clip(gradients, 1.0, one, space)
+        check([out], [x], min(1.0, 1.0 / (value * math.sqrt(1000) + 1e-6)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_nan_and_infinity(dtype):
+    print(f"[gpu-case] clip NaN and infinity {dtype}", flush=True)
+    one = torch.empty(1, device="cuda")
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        grads = [torch.ones(300, dtype=dtype, device="cuda"), torch.ones(5, dtype=dtype, device="cuda")]
+        grads[1][2] = bad
+        outs = [torch.empty_like(x) for x in grads]
+        gradients = bns.make_gradients(grads, outs)
+        space = torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda")
+        bns.bns_grads_clip(gradients, 1.0, one, space)
+        if bad != bad:
+            assert bool(one.isnan().all()) and all(bool(o.isnan().all()) for o in outs)
+        else:
+            assert float(one[0]) == math.inf and bool((outs[0] == 0).all()) and bool(outs[1][2].isnan()) and int(outs[1].isnan().sum()) == 1
+
+
+def test_a_captured_clip_is_replayed():
+    """Kernels of several launches in a graph, replayed on new gradients with other work in between."""
+    print("[gpu-case] clip captured", flush=True)
+    grads, outs, _ = make([(i * 53) % 901 + 1 for i in range(150)], (torch.float32, torch.bfloat16), seed=4)
+    gradients, one = bns.make_gradients(grads, outs), torch.empty(1, device="cuda")
+    space = torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda")
+    bns.bns_grads_clip(gradients, 1.0, one, space)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bns.bns_grads_clip(gradients, 1.0, one, space)
+    for turn in range(4):
+        for x in grads:
+            x.mul_(1.5 if turn % 2 else 0.5)
+        space.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        norm = whole_norm(grads)
+        assert abs(float(one[0]) - norm) <= 2 * U * norm
+        check(outs, grads, min(1.0, 1.0 / (norm + 1e-6)))
