@@ -125,13 +125,6 @@ __device__ __forceinline__ void fix_entries(const Teacher& s, const DistillArgs&
     }
 }
 
-// Keeps the compiler from carrying the words' values, twice their size in bf16, from one use of the row to the next.
-template <int N>
-__device__ __forceinline__ void keep_packed(u4 (&w)[N]) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
-}
-
 // NV: 16-byte words per thread that hold the row, or with REST its beginning; what lies behind is read again (NV = 0: rows shorter than a word).  NT: with
 // the non-temporal hint (4096x131072 bf16 with its gradient 400 against 416 us, gradient of 2048x50304 fp32 162 against 172; 7x100003 bf16 6.7 against 6.4).
 template <typename T, int THREADS, int NV, bool REST, bool NT>

@@ -26,6 +26,8 @@ struct Words<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(w[i]);
     }
+    static __device__ __forceinline__ float lowest(u4 w) { return __uint_as_float(w[0]); }
+    static __device__ __forceinline__ u4 next(u4 w) { return u4{w[1], w[2], w[3], 0}; }      // (without its lowest element)
     template <bool NT>
     static __device__ __forceinline__ void store(float* p, int left, const float (&f)[4]) {
         if (left >= 4) {
@@ -59,9 +61,20 @@ struct Words<bf16_t> {
             f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
+    static __device__ __forceinline__ float lowest(u4 w) { return __uint_as_float(w[0] << 16); }
+    static __device__ __forceinline__ u4 next(u4 w) {
+        return u4{__builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16), __builtin_amdgcn_alignbit(w[3], w[2], 16), w[3] >> 16};
+    }
     template <bool NT>
     static __device__ __forceinline__ void store(bf16_t* p, int left, const float (&f)[8]) { Row8<bf16_t>::store<NT>(p, left, f); }
     static __device__ __forceinline__ void put_one(bf16_t* p, float f) { p->bits = uint16_t(f32_to_bf16(f)); }
 };
+
+// Keeps the compiler from carrying the words' values, twice their size in bf16, from one use of the row to the next.
+template <int N>
+__device__ __forceinline__ void keep_packed(u4 (&w)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm volatile("" : "+v"(w[j]));
+}
 
 }  // namespace bns
