@@ -127,7 +127,7 @@ inline bns_status check_gradients(const bns_gradient* g, int32_t count, bool sca
         if (!g[i].grad || !aligned_to(g[i].grad, dtype_bytes(g[i].dtype))) return BNS_EINVAL;
         if (scaled && (!g[i].out || !aligned_to(g[i].out, dtype_bytes(g[i].dtype)))) return BNS_EINVAL;
     }
-    return all < int64_t(1) << 44 ? BNS_OK : BNS_EUNSUPPORTED;
+    return all < int64_t(1) << 43 ? BNS_OK : BNS_EUNSUPPORTED;
 }
 
 // Whether a result shares bytes with another result or with a gradient that is not its own, in one pass over all of them by address.

@@ -152,7 +152,7 @@ def test_arguments_of_gradients():
         assert grads(call, [GOOD], ws=NULL) == grads(call, [GOOD], ws=WS + 8) == grads(call, [GOOD], norm=V + 2) == grads(call, [GOOD], count=-1) == bns.BNS_EINVAL
         assert grads(call, [GOOD], short=1) == grads(call, [(Q, QO + 4 * i, 1, 0, 0) for i in range(200)], short=1) == bns.BNS_EWORKSPACE
         assert grads(call, [(Q, QO, 2 ** 40, 0, 0)]) == bns.BNS_EUNSUPPORTED
-        assert grads(call, [(Q + (i << 42), Q + (i << 42), 2 ** 40 - 1, 0, 0) for i in range(17)]) == bns.BNS_EUNSUPPORTED
+        assert grads(call, [(Q + (i << 42), Q + (i << 42), 2 ** 40 - 1, 0, 0) for i in range(9)]) == bns.BNS_EUNSUPPORTED
         assert grads(call, [GOOD], count=65537) == bns.BNS_EUNSUPPORTED
     for call in ("norm", "scale"):
         assert grads(call, [GOOD], squares=NULL) == grads(call, [GOOD], squares=V + 4) == bns.BNS_EINVAL
