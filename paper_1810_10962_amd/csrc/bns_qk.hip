@@ -2,12 +2,19 @@
 // equations.
 //
 // Both read every element once and write once, so HBM bounds them where tokens are many and a launch where they are few.  A head of `width` elements belongs
-// to a group of G lanes; a lane holds one unit of it, two chunks of 16 bytes that contain both elements of every pair that it rotates (chunks
+// to a group of G lanes; a lane holds one unit of it, two chunks of up to 16 bytes that contain both elements of every pair that it rotates (chunks
 // rotated / 2 apart, or neighbours), so that the rotation needs no exchange and the sums one of log2 G steps.  The lanes of a wave take hs heads each of
-// 64 / (G hs) tokens at a time, go on to the next heads with the same angles, and queries and keys go to different blocks, so that a wave holds one weight.
+// 64 / (G hs) tokens at a time: a turn.  A wave walks a range of turns, one head group of a token after the other and one token after the other, and asks for the next turn's
+// elements before it works on those of this one.  Queries and keys go to different blocks, the queries' first.
 //
-// Angles: position * frequency is formed in quarter turns in fp64 and reduced exactly (the remainder of a fused multiply-add with the nearest whole
-// number); what is left, at most an eighth of a turn, is exact enough in fp32, and Taylor's series to x^9 and x^10 leave 2e-9 there.
+// Angles: each of the lanes that share a token works out a part of its angles, and all of them get them through LDS.  position * frequency is formed in quarter turns in fp64
+// and reduced exactly (the remainder of a fused multiply-add with the nearest whole number); what is left, at most an eighth of a turn, is exact enough in fp32, and Taylor's
+// series to x^9 and x^10 leave 2e-9 there.
+//
+// Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.6 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s); backward of 16 384 tokens 105 us (503 MB,
+// 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches.  A lane per pair of single elements instead of chunks took
+// 46 us and 2048 tokens' backward 20 us instead of 16.  An odd width, whose heads begin at every alignment, moves single elements: 9109 x (48 + 6) x 83 bf16
+// takes 102 us, 1.6 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,9 +33,10 @@ struct Heads {
     void* out;          // forward: y; backward: dx
     float* partial;     // backward: [blocks][width]
     HeadStrides xs, ds, os;
-    FastDiv splits;     // waves that share the heads of a token
-    int64_t jobs;       // pieces of work of a wave: groups of tokens times splits
-    int32_t heads, turns;   // turns: steps of a wave over the heads of its tokens
+    int64_t units;      // turns of all tokens
+    int32_t run;        // turns that a wave takes one after the other, then as many behind those of all others
+    FastDiv turns;      // of a wave over the heads of its tokens
+    int32_t heads;
     int32_t log_hs;     // heads of a token that a wave takes at a time
     int32_t blocks;
 };
@@ -41,6 +49,8 @@ struct QkArgs {
     int32_t width, rotated, weight_bf16, interleaved;
     float eps, inv_width;
 };
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
 
 // Elements of a lane: a chunk of E as it is stored, or a single element.
 template <typename T, int E>
@@ -55,6 +65,27 @@ struct Chunk<T, 1> {
     static __device__ __forceinline__ void store(T* p, const float (&v)[1]) { Vec<T, 1>{{v[0]}}.store(p); }
 };
 template <>
+struct Chunk<float, 2> {
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    typedef u2 u2e __attribute__((aligned(4)));
+    u2 w;
+    __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const u2e*>(p); }
+    __device__ __forceinline__ void clear() { w = u2{0, 0}; }
+    __device__ __forceinline__ void unpack(float (&v)[2]) const { v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y); }
+    template <bool NT>
+    static __device__ __forceinline__ void store(float* p, const float (&v)[2]) { *reinterpret_cast<u2e*>(p) = u2{__float_as_uint(v[0]), __float_as_uint(v[1])}; }
+};
+template <>
+struct Chunk<bf16_t, 2> {
+    typedef uint32_t u1e __attribute__((aligned(2)));
+    uint32_t w;
+    __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u1e*>(p); }
+    __device__ __forceinline__ void clear() { w = 0; }
+    __device__ __forceinline__ void unpack(float (&v)[2]) const { v[0] = __uint_as_float(w << 16), v[1] = __uint_as_float(w & 0xffff0000u); }
+    template <bool NT>
+    static __device__ __forceinline__ void store(bf16_t* p, const float (&v)[2]) { *reinterpret_cast<u1e*>(p) = pack_bf16x2(v[0], v[1]); }
+};
+template <>
 struct Chunk<float, 4> {
     words4_t w;
     __device__ __forceinline__ void load(const float* p) { w = get16<false>(p); }
@@ -67,6 +98,20 @@ struct Chunk<float, 4> {
     static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
         put16<NT>(p, words4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
     }
+};
+template <>
+struct Chunk<bf16_t, 4> {
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    typedef u2 u2e __attribute__((aligned(2)));
+    u2 w;
+    __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u2e*>(p); }
+    __device__ __forceinline__ void clear() { w = u2{0, 0}; }
+    __device__ __forceinline__ void unpack(float (&v)[4]) const {
+        v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xffff0000u);
+        v[2] = __uint_as_float(w.y << 16), v[3] = __uint_as_float(w.y & 0xffff0000u);
+    }
+    template <bool NT>
+    static __device__ __forceinline__ void store(bf16_t* p, const float (&v)[4]) { *reinterpret_cast<u2e*>(p) = u2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
 };
 template <>
 struct Chunk<bf16_t, 8> {
@@ -104,7 +149,7 @@ __device__ __forceinline__ float group_sum(float v) {
 }
 
 // cos and sin of `position` times an angle given in quarter turns.
-__device__ __forceinline__ void turn(double position, double quarters, float* c, float* s) {
+__device__ __forceinline__ void turn_by(double position, double quarters, float* c, float* s) {
     const double n = rint(position * quarters);
     const float x = float(fma(position, quarters, -n)) * 1.57079632679489662f;      // |x| <= pi / 4
     const int quadrant = int(fma(-4.0, rint(n * 0.25), n));                        // -2 .. 2
@@ -122,19 +167,14 @@ template <typename T, int E, int G, int UPL, bool NEIGHBOURS>
 struct Lane {
     int at[UPL][2];             // first elements of its chunks; -1: none
     bool turned[UPL][2];
-    float w[UPL][2][E];
-    double quarters[UPL][E];    // NEIGHBOURS: E / 2 of each chunk
 
     __device__ __forceinline__ void set(const QkArgs& a, const Heads& p, int l) {
 #pragma unroll
         for (int k = 0; k < UPL; ++k) {
             const int u = k * G + l;
-            int angle[2];
             if (NEIGHBOURS) {
                 at[k][0] = 2 * u * E;
                 at[k][1] = at[k][0] + E;
-                angle[0] = at[k][0] / 2;
-                angle[1] = at[k][1] / 2;
                 turned[k][0] = at[k][0] < a.rotated;
                 turned[k][1] = at[k][1] < a.rotated;
             } else {
@@ -147,46 +187,55 @@ struct Lane {
                     at[k][0] = t ? u * E : a.rotated + 2 * rest * E;
                     at[k][1] = t ? a.rotated / 2 + u * E : at[k][0] + E;
                 }
-                angle[0] = angle[1] = u * E;
                 turned[k][0] = turned[k][1] = t;
             }
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int c = 0; c < 2; ++c) {
                 if (at[k][c] >= a.width) at[k][c] = -1;
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const int c = NEIGHBOURS ? i / (E / 2 > 0 ? E / 2 : 1) : 0, j = NEIGHBOURS ? i % (E / 2 > 0 ? E / 2 : 1) : i;
-                quarters[k][i] = turned[k][c] && at[k][c] >= 0 ? a.frequencies[angle[c] + j] * 0.63661977236758134308 : 0.0;    // 2 / pi
             }
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const int e = at[k][c] + i;
-                    w[k][c][i] = at[k][c] < 0 ? 0.f : !p.weight ? 1.f : a.weight_bf16 ? load_scalar<bf16_t>(static_cast<const bf16_t*>(p.weight) + e) : static_cast<const float*>(p.weight)[e];
-                }
         }
     }
-    __device__ __forceinline__ void load(Chunk<T, E> (&c)[UPL][2], const T* head) const {
+    // Its elements' weights.
+    __device__ __forceinline__ void weights(float (&w)[UPL][2][E], const float* weight) const {
+#pragma unroll
+        for (int k = 0; k < UPL; ++k)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < E; ++i) w[k][c][i] = weight[max(at[k][c], 0) + i];
+    }
+    // Elements from a turn's base to the lane's chunks.
+    struct Offsets {
+        int64_t to[UPL][2];
+    };
+    __device__ __forceinline__ Offsets offsets(int64_t of_lane) const {
+        Offsets o;
+#pragma unroll
+        for (int k = 0; k < UPL; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) o.to[k][i] = of_lane + at[k][i];
+        return o;
+    }
+    __device__ __forceinline__ void load(Chunk<T, E> (&c)[UPL][2], const T* base, const Offsets& o) const {
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                if (at[k][i] >= 0) c[k][i].load(head + at[k][i]);
+                if (at[k][i] >= 0) c[k][i].load(base + o.to[k][i]);
                 else c[k][i].clear();
             }
     }
     template <bool NT>
-    __device__ __forceinline__ void store(T* head, const float (&v)[UPL][2][E]) const {
+    __device__ __forceinline__ void store(T* base, const Offsets& o, const float (&v)[UPL][2][E]) const {
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (at[k][i] >= 0) Chunk<T, E>::template store<NT>(head + at[k][i], v[k][i]);
+                if (at[k][i] >= 0) Chunk<T, E>::template store<NT>(base + o.to[k][i], v[k][i]);
     }
-    // BACK: by the negative angle
+    // BACK: by the negative angle.  `all`: every pair is turned.
     template <bool BACK>
-    __device__ __forceinline__ void rotate(float (&v)[UPL][2][E], const float (&cs)[UPL][E], const float (&sn)[UPL][E]) const {
+    __device__ __forceinline__ void rotate(float (&v)[UPL][2][E], const float (&cs)[UPL][E], const float (&sn)[UPL][E], bool all) const {
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
@@ -196,78 +245,184 @@ struct Lane {
                 float &x = NEIGHBOURS ? v[k][c][2 * j] : v[k][0][i], &y = NEIGHBOURS ? v[k][c][2 * j + 1] : v[k][1][i];
                 const float s = BACK ? -sn[k][i] : sn[k][i];
                 const float xr = fmaf(x, cs[k][i], -(y * s)), yr = fmaf(x, s, y * cs[k][i]);
-                x = turned[k][c] ? xr : x;
-                y = turned[k][c] ? yr : y;
+                x = all || turned[k][c] ? xr : x;
+                y = all || turned[k][c] ? yr : y;
             }
     }
 };
 
-// The work of a wave: one piece after another, each a group of tokens and some of their heads.  `step(token, head)` is called for one head at a time by
-// all lanes of it, or for none (head < 0).
+// What stays in LDS, as registers decide how many waves there are: the weight, angles in quarter turns by position, and cos and sin of those of the tokens that
+// a wave works on.
+template <int E, int UPL>
+struct Angles {
+    alignas(16) float cosine[kWaves][kWave * E * UPL], sine[kWaves][kWave * E * UPL];
+    alignas(16) float weight[512];
+    double quarters[256];
+};
+
+// The walk of a wave over its turns: runs of neighbouring ones, so that all waves work in one stretch of memory.
+template <typename T, int E, int G, int UPL, bool NEIGHBOURS>
+struct Walk {
+    const QkArgs& a;
+    const Heads& p;
+    Angles<E, UPL>& angles;
+    int lane, wave, block;
+    int hs, tokens_at_once, sharing;        // sharing: lanes of a token
+    int64_t unit, skip, group;              // skip: from the end of a run to the next one
+    int turn, left;                         // left: turns of the run
+    bool there;                             // whether this lane has a head in this turn
+    int64_t position;                       // of the next group of tokens, asked for early (as it is: a conversion would wait for it)
+
+    __device__ __forceinline__ Walk(const QkArgs& args, Angles<E, UPL>& lds)
+        : a(args), p(args.part[int(blockIdx.x) >= args.part[0].blocks]), angles(lds) {
+        lane = threadIdx.x % kWave;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        block = int(blockIdx.x) - (int(blockIdx.x) >= a.part[0].blocks ? a.part[0].blocks : 0);
+        hs = 1 << p.log_hs;
+        tokens_at_once = (kWave / G) >> p.log_hs;
+        sharing = G << p.log_hs;
+        const int64_t waves = int64_t(p.blocks) * kWaves;
+        unit = (int64_t(block) * kWaves + wave) * p.run;
+        skip = (waves - 1) * p.run;
+        left = p.run;
+        group = group_of(unit);
+        turn = int(unit - group * p.turns.d);
+        for (int i = threadIdx.x; i < a.rotated / 2; i += kThreads) angles.quarters[i] = a.frequencies[i] * 0.63661977236758134308;        // 2 / pi
+        if (p.weight) {
+            for (int i = threadIdx.x; i < a.width; i += kThreads)
+                angles.weight[i] = a.weight_bf16 ? load_scalar<bf16_t>(static_cast<const bf16_t*>(p.weight) + i) : static_cast<const float*>(p.weight)[i];
+        }
+        __syncthreads();
+        ask_position(group);
+        look();
+    }
+    __device__ __forceinline__ int64_t group_of(int64_t u) const { return u < (int64_t(1) << 31) ? int64_t(fdiv(uint32_t(u), p.turns)) : u / p.turns.d; }
+    __device__ __forceinline__ bool more() const { return unit < p.units; }
+    __device__ __forceinline__ void look() {
+        const int tokens_left = int(max(int64_t(0), min(a.tokens - group * tokens_at_once, int64_t(kWave))));
+        there = more() && lane / sharing < tokens_left && turn * hs + lane / G % hs < p.heads;
+    }
+    // Where the lane's head lies: the same for all lanes, and what the lane adds to that in every turn.
+    __device__ __forceinline__ int64_t base(const HeadStrides& s) const { return group * (tokens_at_once * s.token) + turn * (hs * s.head); }
+    __device__ __forceinline__ int64_t of_lane(const HeadStrides& s) const { return lane / sharing * s.token + lane / G % hs * s.head; }
+    __device__ __forceinline__ void ask_position(int64_t g) {
+        const int64_t t = g * tokens_at_once + lane / sharing;
+        position = 0;
+        if (a.rotated > 0 && t < a.tokens) position = a.positions[t];
+    }
+    __device__ __forceinline__ void next() {
+        ++unit;
+        if (--left == 0) {
+            unit += skip;
+            left = p.run;
+            group = group_of(unit);
+            turn = int(unit - group * p.turns.d);
+        } else if (++turn == int(p.turns.d)) {
+            turn = 0;
+            ++group;
+        }
+        look();
+    }
+    // The angles of the group whose position was asked for; asks for the next one's.
+    __device__ __forceinline__ void work_out() {
+        const int each = a.rotated / 2, base = lane / sharing * each;
+        float *c = angles.cosine[wave], *s = angles.sine[wave];
+        const double here = double(position);
+        asm volatile("" ::: "memory");      // (a wave's accesses to LDS are in order)
+        for (int i = lane % sharing; i < each; i += sharing) turn_by(here, angles.quarters[i], c + base + i, s + base + i);
+        asm volatile("" ::: "memory");
+        ask_position(left > int(p.turns.d) - turn ? group + 1 : group_of(unit + left + skip));
+    }
+    __device__ __forceinline__ void get(float (&cs)[UPL][E], float (&sn)[UPL][E]) const {
+        const int each = a.rotated / 2, base = lane / sharing * each;
+        const float *c = angles.cosine[wave], *s = angles.sine[wave];
+#pragma unroll
+        for (int k = 0; k < UPL; ++k) {
+            // (units that are not turned read the first angles and use none)
+            const int u = (k * G + lane % G) * E, from = base + (u < each ? u : 0);
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                cs[k][i] = c[from + i];
+                sn[k][i] = s[from + i];
+            }
+        }
+    }
+};
+
 template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool NT>
-__global__ void __launch_bounds__(256) qk_forward_kernel(QkArgs a) {
-    const int which = int(blockIdx.x) >= a.part[0].blocks;
-    const Heads& p = a.part[which];
-    const int lane = threadIdx.x % kWave, slot = lane / G;
-    const int hs = 1 << p.log_hs, tokens_at_once = (kWave / G) >> p.log_hs;
+__global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkArgs a) {
+    __shared__ Angles<E, UPL> angles;
+    Walk<T, E, G, UPL, NEIGHBOURS> at(a, angles);
+    const Heads& p = at.p;
     Lane<T, E, G, UPL, NEIGHBOURS> mine;
-    mine.set(a, p, lane % G);
-    const int64_t first = int64_t(int(blockIdx.x) - (which ? a.part[0].blocks : 0)) * 4 + threadIdx.x / kWave;
-    for (int64_t job = first; job < p.jobs; job += int64_t(p.blocks) * 4) {
-        const uint32_t group = fdiv(uint32_t(job), p.splits), split = uint32_t(job) - group * p.splits.d;
-        const int64_t token = int64_t(group) * tokens_at_once + (slot >> p.log_hs);
-        if (token >= a.tokens) continue;
-        const int from = int(int64_t(p.turns) * split / p.splits.d), to = int(int64_t(p.turns) * (split + 1) / p.splits.d);
-        const int h0 = slot & (hs - 1);
-        const T* x = static_cast<const T*>(p.x) + token * p.xs.token;
-        T* out = static_cast<T*>(p.out) + token * p.os.token;
-        Chunk<T, E> next[UPL][2];
-        int h = from * hs + h0;
-        if (h < p.heads) mine.load(next, x + int64_t(h) * p.xs.head);
-        float cs[UPL][E], sn[UPL][E];
-        const double position = a.positions ? double(a.positions[token]) : 0.0;
+    Chunk<T, E> next[UPL][2];
+    mine.set(a, p, at.lane % G);
+    const auto x_to = mine.offsets(at.of_lane(p.xs)), out_to = mine.offsets(at.of_lane(p.os));
+    const auto ask = [&]() {
+        if (at.there) mine.load(next, static_cast<const T*>(p.x) + at.base(p.xs), x_to);
+    };
+    ask();
+    const bool all = a.rotated == a.width;
+    int64_t group = -1;
+    while (at.more()) {
+        if (a.rotated > 0 && at.group != group) at.work_out();
+        group = at.group;
+        float v[UPL][2][E];
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
-            for (int i = 0; i < E; ++i) turn(position, mine.quarters[k][i], &cs[k][i], &sn[k][i]);
-        for (int t = from; t < to; ++t, h += hs) {
-            if (h >= p.heads) break;
-            float v[UPL][2][E];
+            for (int c = 0; c < 2; ++c) next[k][c].unpack(v[k][c]);
+        T* out = static_cast<T*>(p.out) + at.base(p.os);
+        const bool there = at.there;
+        at.next();
+        ask();
+        asm volatile("" ::: "memory");      // (nothing from LDS is kept in registers from turn to turn)
+        if (!there) continue;
+        if (p.weight) {
+            float squares = 0.f, w[UPL][2][E];
+            mine.weights(w, angles.weight);
 #pragma unroll
             for (int k = 0; k < UPL; ++k)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) next[k][c].unpack(v[k][c]);
-            if (t + 1 < to && h + hs < p.heads) mine.load(next, x + int64_t(h + hs) * p.xs.head);
-            if (p.weight) {
-                float squares = 0.f;
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int k = 0; k < UPL; ++k)
+                    for (int i = 0; i < E; ++i) squares = fmaf(v[k][c][i], v[k][c][i], squares);
+            const float rstd = rsqrtf(fmaf(group_sum<G>(squares), a.inv_width, a.eps));
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
+            for (int k = 0; k < UPL; ++k)
 #pragma unroll
-                        for (int i = 0; i < E; ++i) squares = fmaf(v[k][c][i], v[k][c][i], squares);
-                const float rstd = rsqrtf(fmaf(group_sum<G>(squares), a.inv_width, a.eps));
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int k = 0; k < UPL; ++k)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int i = 0; i < E; ++i) v[k][c][i] *= rstd * mine.w[k][c][i];
-            }
-            mine.template rotate<false>(v, cs, sn);
-            mine.template store<NT>(out + int64_t(h) * p.os.head, v);
+                    for (int i = 0; i < E; ++i) v[k][c][i] *= rstd * w[k][c][i];
         }
+        if (a.rotated > 0) {
+            float cs[UPL][E], sn[UPL][E];
+            at.get(cs, sn);
+            mine.template rotate<false>(v, cs, sn, all);
+        }
+        mine.template store<NT>(out, out_to, v);
     }
 }
 
 template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool NT>
-__global__ void __launch_bounds__(256) qk_backward_kernel(QkArgs a) {
-    const int which = int(blockIdx.x) >= a.part[0].blocks;
-    const Heads& p = a.part[which];
-    const int lane = threadIdx.x % kWave, slot = lane / G;
-    const int hs = 1 << p.log_hs, tokens_at_once = (kWave / G) >> p.log_hs;
+__global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
+    __shared__ union {
+        Angles<E, UPL> angles;
+        float sums[UPL * 2 * E][kThreads];
+    } lds;
+    Walk<T, E, G, UPL, NEIGHBOURS> at(a, lds.angles);
+    const Heads& p = at.p;
     Lane<T, E, G, UPL, NEIGHBOURS> mine;
-    mine.set(a, p, lane % G);
+    Chunk<T, E> next_x[UPL][2], next_g[UPL][2];
+    mine.set(a, p, at.lane % G);
+    const auto x_to = mine.offsets(at.of_lane(p.xs)), dy_to = mine.offsets(at.of_lane(p.ds)), out_to = mine.offsets(at.of_lane(p.os));
+    const auto ask = [&]() {
+        if (!at.there) return;
+        mine.load(next_g, static_cast<const T*>(p.dy) + at.base(p.ds), dy_to);
+        if (p.weight) mine.load(next_x, static_cast<const T*>(p.x) + at.base(p.xs), x_to);
+    };
+    ask();
+    const bool all = a.rotated == a.width;
     float dw[UPL][2][E];
 #pragma unroll
     for (int k = 0; k < UPL; ++k)
@@ -275,92 +430,81 @@ __global__ void __launch_bounds__(256) qk_backward_kernel(QkArgs a) {
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int i = 0; i < E; ++i) dw[k][c][i] = 0.f;
-    const int block = int(blockIdx.x) - (which ? a.part[0].blocks : 0);
-    for (int64_t job = int64_t(block) * 4 + threadIdx.x / kWave; job < p.jobs; job += int64_t(p.blocks) * 4) {
-        const uint32_t group = fdiv(uint32_t(job), p.splits), split = uint32_t(job) - group * p.splits.d;
-        const int64_t token = int64_t(group) * tokens_at_once + (slot >> p.log_hs);
-        if (token >= a.tokens) continue;
-        const int from = int(int64_t(p.turns) * split / p.splits.d), to = int(int64_t(p.turns) * (split + 1) / p.splits.d);
-        const int h0 = slot & (hs - 1);
-        const T *x = static_cast<const T*>(p.x) + token * p.xs.token, *dy = static_cast<const T*>(p.dy) + token * p.ds.token;
-        T* out = static_cast<T*>(p.out) + token * p.os.token;
-        Chunk<T, E> next_x[UPL][2], next_g[UPL][2];
-        int h = from * hs + h0;
-        const auto ask = [&](int head) {
-            mine.load(next_g, dy + int64_t(head) * p.ds.head);
-            if (p.weight) mine.load(next_x, x + int64_t(head) * p.xs.head);
-        };
-        if (h < p.heads) ask(h);
-        float cs[UPL][E], sn[UPL][E];
-        const double position = a.positions ? double(a.positions[token]) : 0.0;
+    int64_t group = -1;
+    while (at.more()) {
+        if (a.rotated > 0 && at.group != group) at.work_out();
+        group = at.group;
+        float g[UPL][2][E], v[UPL][2][E];
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
-            for (int i = 0; i < E; ++i) turn(position, mine.quarters[k][i], &cs[k][i], &sn[k][i]);
-        for (int t = from; t < to; ++t, h += hs) {
-            if (h >= p.heads) break;
-            float g[UPL][2][E], v[UPL][2][E];
+            for (int c = 0; c < 2; ++c) {
+                next_g[k][c].unpack(g[k][c]);
+                if (p.weight) next_x[k][c].unpack(v[k][c]);
+            }
+        T* out = static_cast<T*>(p.out) + at.base(p.os);
+        const bool there = at.there;
+        at.next();
+        ask();
+        asm volatile("" ::: "memory");      // (nothing from LDS is kept in registers from turn to turn)
+        if (!there) continue;
+        if (a.rotated > 0) {
+            float cs[UPL][E], sn[UPL][E];
+            at.get(cs, sn);
+            mine.template rotate<true>(g, cs, sn, all);
+        }
+        if (p.weight) {
+            float squares = 0.f, dot = 0.f, w[UPL][2][E];
+            mine.weights(w, lds.angles.weight);
 #pragma unroll
             for (int k = 0; k < UPL; ++k)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    next_g[k][c].unpack(g[k][c]);
-                    if (p.weight) next_x[k][c].unpack(v[k][c]);
-                }
-            if (t + 1 < to && h + hs < p.heads) ask(h + hs);
-            mine.template rotate<true>(g, cs, sn);
-            if (p.weight) {
-                float squares = 0.f, dot = 0.f;
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int k = 0; k < UPL; ++k)
+                    for (int i = 0; i < E; ++i) {
+                        squares = fmaf(v[k][c][i], v[k][c][i], squares);
+                        dot = fmaf(g[k][c][i] * w[k][c][i], v[k][c][i], dot);
+                    }
+            const float rstd = rsqrtf(fmaf(group_sum<G>(squares), a.inv_width, a.eps));
+            const float mean = group_sum<G>(dot) * rstd * a.inv_width;       // of weight * g * x^
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
+            for (int k = 0; k < UPL; ++k)
 #pragma unroll
-                        for (int i = 0; i < E; ++i) {
-                            squares = fmaf(v[k][c][i], v[k][c][i], squares);
-                            dot = fmaf(g[k][c][i] * mine.w[k][c][i], v[k][c][i], dot);
-                        }
-                const float rstd = rsqrtf(fmaf(group_sum<G>(squares), a.inv_width, a.eps));
-                const float mean = group_sum<G>(dot) * rstd * a.inv_width;       // of weight * g * x^
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int k = 0; k < UPL; ++k)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int i = 0; i < E; ++i) {
-                            const float xh = v[k][c][i] * rstd;
-                            dw[k][c][i] = fmaf(g[k][c][i], xh, dw[k][c][i]);
-                            g[k][c][i] = rstd * fmaf(g[k][c][i], mine.w[k][c][i], -xh * mean);
-                        }
-            }
-            mine.template store<NT>(out + int64_t(h) * p.os.head, g);
+                    for (int i = 0; i < E; ++i) {
+                        const float xh = v[k][c][i] * rstd;
+                        dw[k][c][i] = fmaf(g[k][c][i], xh, dw[k][c][i]);
+                        g[k][c][i] = rstd * fmaf(g[k][c][i], w[k][c][i], -xh * mean);
+                    }
         }
+        mine.template store<NT>(out, out_to, g);
     }
     if (!p.weight) return;
     // The block's sums: the lanes that hold the same elements, in their order.
-    constexpr int kSlots = 256 / G;
-    __shared__ float sums[UPL * 2 * E][256];
+    constexpr int kSlots = kThreads / G;
+    __syncthreads();        // (the angles are no longer needed)
 #pragma unroll
     for (int k = 0; k < UPL; ++k)
 #pragma unroll
         for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int i = 0; i < E; ++i) sums[(k * 2 + c) * E + i][threadIdx.x] = dw[k][c][i];
+            for (int i = 0; i < E; ++i) lds.sums[(k * 2 + c) * E + i][threadIdx.x] = dw[k][c][i];
     __syncthreads();
-    float* partial = p.partial + int64_t(block) * a.width;
+    float* partial = p.partial + int64_t(at.block) * a.width;
     // (element r of lane l: written by that lane's place among the first G threads, which knows where it goes)
     for (int r = threadIdx.x / G; r < UPL * 2 * E; r += kSlots) {
         const int l = threadIdx.x % G;
         float s = 0.f;
-        for (int j = 0; j < kSlots; ++j) s += sums[r][j * G + l];
+        for (int j = 0; j < kSlots; ++j) s += lds.sums[r][j * G + l];
         const int k = r / (2 * E), c = r / E % 2, i = r % E;
-        int at = -1;
+        int place = -1;
 #pragma unroll
         for (int kk = 0; kk < UPL; ++kk)
 #pragma unroll
             for (int cc = 0; cc < 2; ++cc)
-                if (kk == k && cc == c) at = mine.at[kk][cc];
-        if (at >= 0) partial[at + i] = s;
+                if (kk == k && cc == c) place = mine.at[kk][cc];
+        if (place >= 0) partial[place + i] = s;
     }
 }
 
@@ -379,7 +523,7 @@ __global__ void __launch_bounds__(kSumColumns * kSumLanes) qk_weight_sum_kernel(
     const int c = threadIdx.x % kSumColumns, l = threadIdx.x / kSumColumns, col = blockIdx.x * kSumColumns + c;
     float s = 0.f;
     if (col < a.width) {
-#pragma unroll 8
+#pragma unroll 16
         for (int i = l; i < a.count[which]; i += kSumLanes) s += partial[int64_t(i) * a.width + col];
     }
     lds[l][c] = s;
@@ -390,35 +534,41 @@ __global__ void __launch_bounds__(kSumColumns * kSumLanes) qk_weight_sum_kernel(
     }
 }
 
-// How a head lies in lanes.
+// How a head lies in lanes: chunks of 16 bytes, of four or two elements, or single ones, as the halves of what is rotated and the rest are whole chunks.
 struct QkPlan {
-    int chunk, group, per_lane;
+    int chunk, group;
 };
 QkPlan qk_plan(const QkDims& d, int32_t dtype, bool interleaved) {
-    const int e = dtype == BNS_F32 ? 4 : 8;
-    if (d.width % e || d.rotated % (interleaved ? e : 2 * e)) return (d.width + 1) / 2 <= 64 ? QkPlan{1, 16, 4} : QkPlan{1, 64, 4};
-    const int units = interleaved ? (d.width / e + 1) / 2 : d.rotated / (2 * e) + ((d.width - d.rotated) / e + 1) / 2;
-    int g = 4;
-    while (g < units) g *= 2;
-    return {e, g, 1};
+    for (int e : {dtype == BNS_F32 ? 4 : 8, 4, 2}) {
+        if (d.width % e || d.rotated % (interleaved ? e : 2 * e)) continue;
+        const int units = interleaved ? (d.width / e + 1) / 2 : d.rotated / (2 * e) + ((d.width - d.rotated) / e + 1) / 2;
+        const int of_lane = e == 2 ? 2 : 1;
+        int g = e == 2 ? 8 : 4;
+        while (g * of_lane < units) g *= 2;
+        return {e, g};
+    }
+    return (d.width + 1) / 2 <= 64 ? QkPlan{1, 16} : QkPlan{1, 64};
 }
 
-constexpr int kMostForwardBlocks = 256 * 8, kMostBackwardBlocks = 512;
+// Blocks of the queries and of the keys, each.  (us: forward, 16384 x (32 + 8) x 128 bf16, 512 blocks 68.5, 1024 65.1, 2048 64.3; backward 384 112, 448 111, 512 106, 768 108.)
+constexpr int kMostForwardBlocks = 2048, kMostBackwardBlocks = 512;
+// Turns that make a wave worth its beginning, where that leaves enough waves (2048 x (32 + 8) x 128 bf16 forward, a turn a wave 11.5 us, two 9.7).
+constexpr int64_t kTurnsOfWave = 2, kEnoughTurns = 4096;
 
-// Shares the tokens and heads of one tensor out: `most` blocks of four waves.
+// Shares the turns of a tensor out over at most `most` blocks.
 void share_out(Heads* p, const QkPlan& plan, int64_t tokens, int heads, int most) {
     const int slots = kWave / plan.group;
     p->heads = heads;
     p->log_hs = 0;
     while ((1 << p->log_hs) < heads && (2 << p->log_hs) <= slots) ++p->log_hs;
-    const int hs = 1 << p->log_hs, tokens_at_once = slots / hs;
-    p->turns = (heads + hs - 1) / hs;
-    const int64_t groups = (tokens + tokens_at_once - 1) / tokens_at_once;
-    // Few tokens: the turns over their heads go to different waves.  (Jobs are numbered in 32 bits: splits only where tokens are few.)
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(p->turns, groups > 0 ? int64_t(most) * 4 / groups : 1));
-    p->splits = make_fastdiv(uint32_t(splits));
-    p->jobs = heads > 0 ? groups * splits : 0;
-    p->blocks = int32_t(std::min<int64_t>((p->jobs + 3) / 4, most));
+    const int hs = 1 << p->log_hs, tokens_at_once = slots / hs, turns = std::max(1, (heads + hs - 1) / hs);
+    p->turns = make_fastdiv(uint32_t(turns));
+    p->units = heads > 0 ? (tokens + tokens_at_once - 1) / tokens_at_once * int64_t(turns) : 0;
+    // Runs: all turns of a token, so that its angles are worked out once, unless tokens are few.
+    const int64_t waves = int64_t(most) * kWaves, whole = turns * ((kTurnsOfWave + turns - 1) / turns);
+    p->run = int32_t(std::min(whole, std::max<int64_t>((p->units + waves - 1) / waves, p->units >= kEnoughTurns ? kTurnsOfWave : 1)));
+    const int64_t of_block = int64_t(p->run) * kWaves;
+    p->blocks = int32_t(std::min<int64_t>((p->units + of_block - 1) / of_block, most));
 }
 
 void fill(QkArgs* a, const bns_qk* qk, const QkDims& d, const QkPlan& plan, int most) {
@@ -434,29 +584,47 @@ void fill(QkArgs* a, const bns_qk* qk, const QkDims& d, const QkPlan& plan, int 
 
 #define BNS_QK_ONE(KERNEL, T, E, G, UPL, NB)                                                                                   \
     do {                                                                                                                       \
-        if (nt) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, true>), grid, dim3(256), 0, st, a);                                       \
-        else BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, false>), grid, dim3(256), 0, st, a);                                         \
+        if (nt) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, true>), grid, dim3(kThreads), 0, st, a);                                       \
+        else BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, false>), grid, dim3(kThreads), 0, st, a);                                         \
     } while (0)
 #define BNS_QK_CASE(KERNEL, T, E, G)                                    \
     do {                                                                \
         if (a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true);        \
         else BNS_QK_ONE(KERNEL, T, E, G, 1, false);                     \
     } while (0)
-#define BNS_QK_LAUNCH(KERNEL)                                                                       \
-    do {                                                                                            \
-        if (f32 && plan.chunk == 1 && plan.group == 16) BNS_LAUNCH((KERNEL<float, 1, 16, 4, false, false>), grid, dim3(256), 0, st, a); \
-        else if (f32 && plan.chunk == 1) BNS_LAUNCH((KERNEL<float, 1, 64, 4, false, false>), grid, dim3(256), 0, st, a);                \
-        else if (plan.chunk == 1 && plan.group == 16) BNS_LAUNCH((KERNEL<bf16_t, 1, 16, 4, false, false>), grid, dim3(256), 0, st, a);  \
-        else if (plan.chunk == 1) BNS_LAUNCH((KERNEL<bf16_t, 1, 64, 4, false, false>), grid, dim3(256), 0, st, a);                      \
-        else if (f32 && plan.group == 4) BNS_QK_CASE(KERNEL, float, 4, 4);                          \
-        else if (f32 && plan.group == 8) BNS_QK_CASE(KERNEL, float, 4, 8);                          \
-        else if (f32 && plan.group == 16) BNS_QK_CASE(KERNEL, float, 4, 16);                        \
-        else if (f32 && plan.group == 32) BNS_QK_CASE(KERNEL, float, 4, 32);                        \
-        else if (f32) BNS_QK_CASE(KERNEL, float, 4, 64);                                            \
-        else if (plan.group == 4) BNS_QK_CASE(KERNEL, bf16_t, 8, 4);                                \
-        else if (plan.group == 8) BNS_QK_CASE(KERNEL, bf16_t, 8, 8);                                \
-        else if (plan.group == 16) BNS_QK_CASE(KERNEL, bf16_t, 8, 16);                              \
-        else BNS_QK_CASE(KERNEL, bf16_t, 8, 32);                                                    \
+#define BNS_QK_SINGLE(KERNEL, T, E, G, UPL, NB) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, false>), grid, dim3(kThreads), 0, st, a)
+#define BNS_QK_FEW(KERNEL, T, E, G, UPL)                                \
+    do {                                                                \
+        if (a.interleaved) BNS_QK_SINGLE(KERNEL, T, E, G, UPL, true);   \
+        else BNS_QK_SINGLE(KERNEL, T, E, G, UPL, false);                \
+    } while (0)
+#define BNS_QK_SMALL(KERNEL, T)                                                     \
+    do {                                                                            \
+        if (plan.chunk == 1 && plan.group == 16) BNS_QK_SINGLE(KERNEL, T, 1, 16, 4, false); \
+        else if (plan.chunk == 1) BNS_QK_SINGLE(KERNEL, T, 1, 64, 4, false);        \
+        else if (plan.group == 8) BNS_QK_FEW(KERNEL, T, 2, 8, 2);                   \
+        else if (plan.group == 16) BNS_QK_FEW(KERNEL, T, 2, 16, 2);                 \
+        else if (plan.group == 32) BNS_QK_FEW(KERNEL, T, 2, 32, 2);                 \
+        else BNS_QK_FEW(KERNEL, T, 2, 64, 2);                                       \
+    } while (0)
+#define BNS_QK_LAUNCH(KERNEL)                                                       \
+    do {                                                                            \
+        if (plan.chunk <= 2 && f32) BNS_QK_SMALL(KERNEL, float);                    \
+        else if (plan.chunk <= 2) BNS_QK_SMALL(KERNEL, bf16_t);                     \
+        else if (f32 && plan.group == 4) BNS_QK_CASE(KERNEL, float, 4, 4);          \
+        else if (f32 && plan.group == 8) BNS_QK_CASE(KERNEL, float, 4, 8);          \
+        else if (f32 && plan.group == 16) BNS_QK_CASE(KERNEL, float, 4, 16);        \
+        else if (f32 && plan.group == 32) BNS_QK_CASE(KERNEL, float, 4, 32);        \
+        else if (f32) BNS_QK_CASE(KERNEL, float, 4, 64);                            \
+        else if (plan.chunk == 4 && plan.group == 4) BNS_QK_FEW(KERNEL, bf16_t, 4, 4, 1);   \
+        else if (plan.chunk == 4 && plan.group == 8) BNS_QK_FEW(KERNEL, bf16_t, 4, 8, 1);   \
+        else if (plan.chunk == 4 && plan.group == 16) BNS_QK_FEW(KERNEL, bf16_t, 4, 16, 1); \
+        else if (plan.chunk == 4 && plan.group == 32) BNS_QK_FEW(KERNEL, bf16_t, 4, 32, 1); \
+        else if (plan.chunk == 4) BNS_QK_FEW(KERNEL, bf16_t, 4, 64, 1);             \
+        else if (plan.group == 4) BNS_QK_CASE(KERNEL, bf16_t, 8, 4);                \
+        else if (plan.group == 8) BNS_QK_CASE(KERNEL, bf16_t, 8, 8);                \
+        else if (plan.group == 16) BNS_QK_CASE(KERNEL, bf16_t, 8, 16);              \
+        else BNS_QK_CASE(KERNEL, bf16_t, 8, 32);                                    \
     } while (0)
 
 // What both directions take: the weights, positions and frequencies.

@@ -85,6 +85,17 @@ CASES = [  # tokens, q heads, k heads, width, rotated, interleaved, norm, layout
     (50, 4, 2, 128, 128, False, False, "packed", 5000),
     (50, 4, 2, 60, 20, True, False, "loose", 5000),
     (1500, 3, 2, 48, 32, True, True, "dense", 2 ** 30),
+    (14, 3, 2, 390, 260, False, True, "loose", 5000),
+    (23, 5, 1, 130, 64, True, True, "packed", 5000),
+    (7, 2, 2, 514 - 4, 510, True, True, "dense", 5000),
+    (5, 40, 24, 6, 4, False, True, "dense", 5000),
+    (3000, 33, 1, 16, 16, False, True, "packed", 5000),
+    (31, 3, 3, 20, 8, False, True, "packed", 5000),
+    (31, 5, 2, 84, 40, False, True, "loose", 5000),
+    (12, 2, 1, 236, 236, True, True, "packed", 5000),
+    (12, 2, 1, 500, 252, True, True, "dense", 5000),
+    (19, 4, 2, 66, 34, True, True, "packed", 5000),
+    (8, 2, 1, 250, 250, True, True, "dense", 5000),
 ]
 
 
