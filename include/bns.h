@@ -539,7 +539,7 @@ size_t bns_qk_workspace_bytes(const bns_qk* qk);
 /* Gradients, with g the gradient of v (dq_out, dk_out turned back), r = 1 / sqrt(mean(x^2) + eps) and x^ = x r, worked out from x again:
  *   dx = r (weight * g - x^ mean(weight * g * x^))  (dx = g without a weight)      dweight = sum over tokens and heads of g * x^
  * in: q, k (NULL where there is no weight), the weights, positions, frequencies, dq_out, dk_out.  out: dq, dk, dq_weight[width], dk_weight[width] (float; NULL
- * exactly where the weight is).  In place: dq on dq_out, dk on dk_out. */
+ * exactly where the weight is; BNS_EINVAL where the two overlap).  In place: dq on dq_out, dk on dk_out. */
 bns_status bns_qk_backward(const bns_qk* qk, const void* q, const void* k, const void* q_weight, const void* k_weight, const int64_t* positions,
                            const double* frequencies, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight, float* dk_weight,
                            void* workspace, size_t workspace_bytes, void* stream);

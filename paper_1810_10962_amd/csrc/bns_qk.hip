@@ -50,7 +50,7 @@ struct QkArgs {
     float eps, inv_width;
 };
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 256, kWaves = kThreads / kWave, kMostWidth = 512;
 
 // Elements of a lane: a chunk of E as it is stored, or a single element.
 template <typename T, int E>
@@ -195,14 +195,14 @@ struct Lane {
             }
         }
     }
-    // Its elements' weights.
+    // Its elements' weights (0 for a chunk that is not there, behind the last one).
     __device__ __forceinline__ void weights(float (&w)[UPL][2][E], const float* weight) const {
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int i = 0; i < E; ++i) w[k][c][i] = weight[max(at[k][c], 0) + i];
+                for (int i = 0; i < E; ++i) w[k][c][i] = weight[(at[k][c] < 0 ? kMostWidth : at[k][c]) + i];
     }
     // Elements from a turn's base to the lane's chunks.
     struct Offsets {
@@ -233,7 +233,9 @@ struct Lane {
             for (int i = 0; i < 2; ++i)
                 if (at[k][i] >= 0) Chunk<T, E>::template store<NT>(base + o.to[k][i], v[k][i]);
     }
-    // BACK: by the negative angle.  `all`: every pair is turned.
+    // Whether every chunk is turned.  (A chunk that is not there has no angles: behind those of the head lies what an earlier kernel left, NaN perhaps.)
+    static __device__ __forceinline__ bool all_turned(const QkArgs& a) { return a.rotated == a.width && !(NEIGHBOURS && a.width % (2 * E)); }
+    // BACK: by the negative angle.  `all`: every chunk is turned.
     template <bool BACK>
     __device__ __forceinline__ void rotate(float (&v)[UPL][2][E], const float (&cs)[UPL][E], const float (&sn)[UPL][E], bool all) const {
 #pragma unroll
@@ -256,8 +258,8 @@ struct Lane {
 template <int E, int UPL>
 struct Angles {
     alignas(16) float cosine[kWaves][kWave * E * UPL], sine[kWaves][kWave * E * UPL];
-    alignas(16) float weight[512];
-    double quarters[256];
+    alignas(16) float weight[kMostWidth + 8];
+    double quarters[kMostWidth / 2];
 };
 
 // The walk of a wave over its turns: runs of neighbouring ones, so that all waves work in one stretch of memory.
@@ -291,6 +293,7 @@ struct Walk {
         if (p.weight) {
             for (int i = threadIdx.x; i < a.width; i += kThreads)
                 angles.weight[i] = a.weight_bf16 ? load_scalar<bf16_t>(static_cast<const bf16_t*>(p.weight) + i) : static_cast<const float*>(p.weight)[i];
+            if (threadIdx.x < 8) angles.weight[kMostWidth + threadIdx.x] = 0.f;
         }
         __syncthreads();
         ask_position(group);
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkArgs a) {
         if (at.there) mine.load(next, static_cast<const T*>(p.x) + at.base(p.xs), x_to);
     };
     ask();
-    const bool all = a.rotated == a.width;
+    const bool all = mine.all_turned(a);
     int64_t group = -1;
     while (at.more()) {
         if (a.rotated > 0 && at.group != group) at.work_out();
@@ -422,7 +425,7 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
         if (p.weight) mine.load(next_x, static_cast<const T*>(p.x) + at.base(p.xs), x_to);
     };
     ask();
-    const bool all = a.rotated == a.width;
+    const bool all = mine.all_turned(a);
     float dw[UPL][2][E];
 #pragma unroll
     for (int k = 0; k < UPL; ++k)
@@ -708,6 +711,7 @@ bns_status bns_qk_backward(const bns_qk* qk, const void* q, const void* k, const
     for (int i = 0; i < 2; ++i)
         if (collide(mo[i], mg[i], true) || collide(mo[i], mg[1 - i], false) || collide(mo[i], mx[0], false) || collide(mo[i], mx[1], false)) return BNS_EINVAL;
     if (collide(mo[0], mo[1], false)) return BNS_EINVAL;
+    if (dq_weight && dk_weight && dq_weight < dk_weight + d.width && dk_weight < dq_weight + d.width) return BNS_EINVAL;
     if (workspace_bytes < bns_qk_workspace_bytes(qk)) return BNS_EWORKSPACE;
     QkArgs a{};
     const QkPlan plan = qk_plan(d, qk->dtype, qk->interleaved);

@@ -66,6 +66,11 @@ def test_qk_backward_refuses(kw):
     assert qk_backward(**kw) == bns.BNS_EINVAL
 
 
+def test_weight_gradients_that_overlap_are_refused():
+    for off in (0, 4, 63 * 4):
+        assert qk_backward(dqw=V, dkw=V + off) == qk_backward(dqw=V + off, dkw=V) == bns.BNS_EINVAL
+
+
 def test_qk_limits():
     for kw in (dict(tokens=2 ** 31), dict(q_heads=2 ** 20), dict(k_heads=2 ** 20), dict(width=513, rotated=0)):
         assert qk_forward(**kw) == qk_backward(**kw) == bns.BNS_EUNSUPPORTED

@@ -140,6 +140,28 @@ def test_forward_and_backward(case, dtype):
     tail_is_whole(workspace, room)
 
 
+@pytest.mark.parametrize("dtype,width", [("f32", 4), ("f32", 12), ("bf16", 8), ("bf16", 24), ("bf16", 20), ("bf16", 4), ("bf16", 6), ("f32", 6)])
+def test_angles_of_an_earlier_call_that_are_nan(dtype, width):
+    """Neighbours paired and turned all, an odd number of chunks: the last lane has one chunk, and the other's angles are whatever lies behind those of the
+    head.  A call before whose angles are all NaN is what may lie there."""
+    tokens, heads, rotated = 2048, 64, width
+    print(f"[gpu-case] qk after NaN {dtype} {width}", flush=True)
+    wide = bns.make_qk(tokens, heads, heads, 512, dtype, rotated=512, interleaved=True)
+    x = torch.ones(tokens, heads, 512, dtype=TYPES[dtype], device="cuda")
+    bns.bns_qk_forward(wide, x, x, None, None, torch.ones(tokens, dtype=torch.int64, device="cuda"),
+                       torch.full((256,), float("nan"), dtype=torch.float64, device="cuda"), torch.empty_like(x), torch.empty_like(x))
+    f = frequencies(rotated)
+    data = [make(tokens, heads, width, dtype, seed, 5000) for seed in (0, 1)]
+    spec = bns.make_qk(tokens, heads, heads, width, dtype, rotated=rotated, interleaved=True, eps=EPS)
+    w = [d[1].cuda() for d in data]
+    dx = [torch.empty_like(d[0], device="cuda") for d in data]
+    dw = [torch.empty(width, device="cuda") for _ in data]
+    workspace = torch.empty(bns.bns_qk_workspace_bytes(spec), dtype=torch.uint8, device="cuda")
+    bns.bns_qk_backward(spec, *[d[0].cuda() for d in data], *w, data[0][2].cuda(), f.cuda(), *[d[3].cuda() for d in data], *dx, *dw, workspace)
+    for i in range(2):
+        assert_backward(dx[i], dw[i], data[i][0], data[i][1], data[0][2], f, data[i][3], rotated, True, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("width,rotated", [(128, 128), (64, 32), (50, 20)])
 def test_in_place_in_a_projection_s_result(width, rotated, dtype):
