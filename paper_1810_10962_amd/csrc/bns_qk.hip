@@ -11,10 +11,11 @@
 // and reduced exactly (the remainder of a fused multiply-add with the nearest whole number); what is left, at most an eighth of a turn, is exact enough in fp32, and Taylor's
 // series to x^9 and x^10 leave 2e-9 there.
 //
-// Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.6 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s); backward of 16 384 tokens 105 us (503 MB,
-// 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches.  A lane per pair of single elements instead of chunks took
-// 46 us and 2048 tokens' backward 20 us instead of 16.  An odd width, whose heads begin at every alignment, moves single elements: 9109 x (48 + 6) x 83 bf16
-// takes 102 us, 1.6 TB/s.
+// Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.4 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s); backward of 16 384 tokens 105 us (503 MB,
+// 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches.  Without the next turn's elements on their way: 46 us forward, and 2048 tokens'
+// backward 20 us instead of 16.
+// Heads that are no whole chunks: 9109 x (48 + 6) x 83 bf16 44.5 us (164 MB), by single elements 102; backward of 9537 x (23 + 23) x 46, of which 10 turn, 45.0 (121 MB),
+// by single elements 198.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -162,39 +163,60 @@ __device__ __forceinline__ void turn_by(double position, double quarters, float*
     *s = quadrant & 2 ? -b : b;             // 2, -2, -1 (as 3): negative
 }
 
-// What a lane holds of a head, the same for every head.
-template <typename T, int E, int G, int UPL, bool NEIGHBOURS>
+// What a lane holds of a head, the same for every head.  RAGGED: the halves of what is rotated (or all of it, for neighbours) and the rest need not be whole chunks: the
+// last chunk of each begins further down, so that it ends where they do, and its first elements are another lane's too.  Both lanes work them out and write the same;
+// one counts them.  A rest shorter than a chunk begins among the rotated elements, which only their own lanes write.
+template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool RAGGED>
 struct Lane {
     int at[UPL][2];             // first elements of its chunks; -1: none
+    int own[UPL][2];            // from which one on they count
     bool turned[UPL][2];
+    bool short_rest;
 
-    __device__ __forceinline__ void set(const QkArgs& a, const Heads& p, int l) {
+    // Chunk q of the rest.
+    __device__ __forceinline__ void set_rest(const QkArgs& a, int k, int c, int q) {
+        const int from = a.rotated + q * E;
+        at[k][c] = from >= a.width ? -1 : !RAGGED ? from : min(from, a.width - E);
+        own[k][c] = RAGGED ? from - at[k][c] : 0;
+        turned[k][c] = false;
+    }
+    __device__ __forceinline__ void set(const QkArgs& a, int l) {
+        short_rest = RAGGED && a.rotated < a.width && a.width - a.rotated < E;
 #pragma unroll
         for (int k = 0; k < UPL; ++k) {
             const int u = k * G + l;
             if (NEIGHBOURS) {
-                at[k][0] = 2 * u * E;
-                at[k][1] = at[k][0] + E;
-                turned[k][0] = at[k][0] < a.rotated;
-                turned[k][1] = at[k][1] < a.rotated;
-            } else {
-                const int units = a.rotated / (2 * E), rest = u - units;
-                const bool t = rest < 0;
-                if (E == 1 && a.interleaved) {
-                    at[k][0] = 2 * u;
-                    at[k][1] = 2 * u + 1;
-                } else {
-                    at[k][0] = t ? u * E : a.rotated + 2 * rest * E;
-                    at[k][1] = t ? a.rotated / 2 + u * E : at[k][0] + E;
-                }
-                turned[k][0] = turned[k][1] = t;
-            }
+                const int chunks = RAGGED ? (a.rotated + E - 1) / E : a.rotated / E;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (at[k][c] >= a.width) at[k][c] = -1;
+                for (int c = 0; c < 2; ++c) {
+                    const int j = 2 * u + c;
+                    if (j < chunks) {
+                        at[k][c] = RAGGED ? min(j * E, a.rotated - E) : j * E;
+                        own[k][c] = j * E - at[k][c];
+                        turned[k][c] = true;
+                    } else {
+                        set_rest(a, k, c, j - chunks);
+                    }
+                }
+            } else {
+                const int half = a.rotated / 2, chunks = RAGGED ? (half + E - 1) / E : half / E;
+                if (u < chunks) {
+                    const int o = RAGGED ? min(u * E, half - E) : u * E;
+                    at[k][0] = E == 1 && a.interleaved ? 2 * o : o;
+                    at[k][1] = E == 1 && a.interleaved ? 2 * o + 1 : half + o;
+                    own[k][0] = own[k][1] = u * E - o;
+                    turned[k][0] = turned[k][1] = true;
+                } else {
+                    set_rest(a, k, 0, 2 * (u - chunks));
+                    set_rest(a, k, 1, 2 * (u - chunks) + 1);
+                }
             }
         }
     }
+    // Whether element i of a chunk counts here.
+    __device__ __forceinline__ bool counts(int k, int c, int i) const { return !RAGGED || i >= own[k][c]; }
+    // Place of the first angle of chunk c (0, or halves) among a token's angles (0 where it is not turned).
+    __device__ __forceinline__ int angle(const QkArgs& a, int k, int c) const { return !turned[k][c] ? 0 : NEIGHBOURS || (E == 1 && a.interleaved) ? at[k][c] / 2 : at[k][c]; }
     // Its elements' weights (0 for a chunk that is not there, behind the last one).
     __device__ __forceinline__ void weights(float (&w)[UPL][2][E], const float* weight) const {
 #pragma unroll
@@ -231,10 +253,20 @@ struct Lane {
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (at[k][i] >= 0) Chunk<T, E>::template store<NT>(base + o.to[k][i], v[k][i]);
+                if (at[k][i] >= 0 && !(short_rest && !turned[k][i])) Chunk<T, E>::template store<NT>(base + o.to[k][i], v[k][i]);
+        if (!short_rest) return;
+#pragma unroll
+        for (int k = 0; k < UPL; ++k)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                if (at[k][c] < 0 || turned[k][c]) continue;
+#pragma unroll
+                for (int i = 1; i < E; ++i)
+                    if (i >= own[k][c]) Vec<T, 1>{{v[k][c][i]}}.store(base + o.to[k][c] + i);
+            }
     }
     // Whether every chunk is turned.  (A chunk that is not there has no angles: behind those of the head lies what an earlier kernel left, NaN perhaps.)
-    static __device__ __forceinline__ bool all_turned(const QkArgs& a) { return a.rotated == a.width && !(NEIGHBOURS && a.width % (2 * E)); }
+    static __device__ __forceinline__ bool all_turned(const QkArgs& a) { return !RAGGED && a.rotated == a.width && !(NEIGHBOURS && a.width % (2 * E)); }
     // BACK: by the negative angle.  `all`: every chunk is turned.
     template <bool BACK>
     __device__ __forceinline__ void rotate(float (&v)[UPL][2][E], const float (&cs)[UPL][E], const float (&sn)[UPL][E], bool all) const {
@@ -336,15 +368,17 @@ struct Walk {
         asm volatile("" ::: "memory");
         ask_position(left > int(p.turns.d) - turn ? group + 1 : group_of(unit + left + skip));
     }
-    __device__ __forceinline__ void get(float (&cs)[UPL][E], float (&sn)[UPL][E]) const {
-        const int each = a.rotated / 2, base = lane / sharing * each;
+    template <typename Lane>
+    __device__ __forceinline__ void get(float (&cs)[UPL][E], float (&sn)[UPL][E], const Lane& mine) const {
+        const int base = lane / sharing * (a.rotated / 2);
         const float *c = angles.cosine[wave], *s = angles.sine[wave];
 #pragma unroll
         for (int k = 0; k < UPL; ++k) {
-            // (units that are not turned read the first angles and use none)
-            const int u = (k * G + lane % G) * E, from = base + (u < each ? u : 0);
+            // (chunks that are not turned read the first angles and use none)
+            const int first = base + mine.angle(a, k, 0), second = NEIGHBOURS ? base + mine.angle(a, k, 1) - E / 2 : first;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
+                const int from = NEIGHBOURS && i >= E / 2 ? second : first;
                 cs[k][i] = c[from + i];
                 sn[k][i] = s[from + i];
             }
@@ -352,14 +386,14 @@ struct Walk {
     }
 };
 
-template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool NT>
+template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool RAGGED, bool NT>
 __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkArgs a) {
     __shared__ Angles<E, UPL> angles;
     Walk<T, E, G, UPL, NEIGHBOURS> at(a, angles);
     const Heads& p = at.p;
-    Lane<T, E, G, UPL, NEIGHBOURS> mine;
+    Lane<T, E, G, UPL, NEIGHBOURS, RAGGED> mine;
     Chunk<T, E> next[UPL][2];
-    mine.set(a, p, at.lane % G);
+    mine.set(a, at.lane % G);
     const auto x_to = mine.offsets(at.of_lane(p.xs)), out_to = mine.offsets(at.of_lane(p.os));
     const auto ask = [&]() {
         if (at.there) mine.load(next, static_cast<const T*>(p.x) + at.base(p.xs), x_to);
@@ -389,7 +423,10 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkArgs a) {
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int i = 0; i < E; ++i) squares = fmaf(v[k][c][i], v[k][c][i], squares);
+                    for (int i = 0; i < E; ++i) {
+                        const float x = mine.counts(k, c, i) ? v[k][c][i] : 0.f;
+                        squares = fmaf(x, x, squares);
+                    }
             const float rstd = rsqrtf(fmaf(group_sum<G>(squares), a.inv_width, a.eps));
 #pragma unroll
             for (int k = 0; k < UPL; ++k)
@@ -400,14 +437,14 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkArgs a) {
         }
         if (a.rotated > 0) {
             float cs[UPL][E], sn[UPL][E];
-            at.get(cs, sn);
+            at.get(cs, sn, mine);
             mine.template rotate<false>(v, cs, sn, all);
         }
         mine.template store<NT>(out, out_to, v);
     }
 }
 
-template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool NT>
+template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool RAGGED, bool NT>
 __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
     __shared__ union {
         Angles<E, UPL> angles;
@@ -415,9 +452,9 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
     } lds;
     Walk<T, E, G, UPL, NEIGHBOURS> at(a, lds.angles);
     const Heads& p = at.p;
-    Lane<T, E, G, UPL, NEIGHBOURS> mine;
+    Lane<T, E, G, UPL, NEIGHBOURS, RAGGED> mine;
     Chunk<T, E> next_x[UPL][2], next_g[UPL][2];
-    mine.set(a, p, at.lane % G);
+    mine.set(a, at.lane % G);
     const auto x_to = mine.offsets(at.of_lane(p.xs)), dy_to = mine.offsets(at.of_lane(p.ds)), out_to = mine.offsets(at.of_lane(p.os));
     const auto ask = [&]() {
         if (!at.there) return;
@@ -453,7 +490,7 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
         if (!there) continue;
         if (a.rotated > 0) {
             float cs[UPL][E], sn[UPL][E];
-            at.get(cs, sn);
+            at.get(cs, sn, mine);
             mine.template rotate<true>(g, cs, sn, all);
         }
         if (p.weight) {
@@ -465,8 +502,9 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
-                        squares = fmaf(v[k][c][i], v[k][c][i], squares);
-                        dot = fmaf(g[k][c][i] * w[k][c][i], v[k][c][i], dot);
+                        const float x = mine.counts(k, c, i) ? v[k][c][i] : 0.f;
+                        squares = fmaf(x, x, squares);
+                        dot = fmaf(mine.counts(k, c, i) ? g[k][c][i] * w[k][c][i] : 0.f, x, dot);
                     }
             const float rstd = rsqrtf(fmaf(group_sum<G>(squares), a.inv_width, a.eps));
             const float mean = group_sum<G>(dot) * rstd * a.inv_width;       // of weight * g * x^
@@ -501,13 +539,13 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
         float s = 0.f;
         for (int j = 0; j < kSlots; ++j) s += lds.sums[r][j * G + l];
         const int k = r / (2 * E), c = r / E % 2, i = r % E;
-        int place = -1;
+        int place = -1, own = 0;
 #pragma unroll
         for (int kk = 0; kk < UPL; ++kk)
 #pragma unroll
             for (int cc = 0; cc < 2; ++cc)
-                if (kk == k && cc == c) place = mine.at[kk][cc];
-        if (place >= 0) partial[place + i] = s;
+                if (kk == k && cc == c) place = mine.at[kk][cc], own = mine.own[kk][cc];
+        if (place >= 0 && i >= own) partial[place + i] = s;
     }
 }
 
@@ -537,20 +575,24 @@ __global__ void __launch_bounds__(kSumColumns * kSumLanes) qk_weight_sum_kernel(
     }
 }
 
-// How a head lies in lanes: chunks of 16 bytes, of four or two elements, or single ones, as the halves of what is rotated and the rest are whole chunks.
+// How a head lies in lanes: chunks of 16 bytes where what is rotated and the rest are whole ones (`ragged` 0), or at least hold one; of four or two elements, or single
+// ones, where they are shorter.
 struct QkPlan {
     int chunk, group;
+    bool ragged;
 };
 QkPlan qk_plan(const QkDims& d, int32_t dtype, bool interleaved) {
-    for (int e : {dtype == BNS_F32 ? 4 : 8, 4, 2}) {
-        if (d.width % e || d.rotated % (interleaved ? e : 2 * e)) continue;
-        const int units = interleaved ? (d.width / e + 1) / 2 : d.rotated / (2 * e) + ((d.width - d.rotated) / e + 1) / 2;
-        const int of_lane = e == 2 ? 2 : 1;
-        int g = e == 2 ? 8 : 4;
-        while (g * of_lane < units) g *= 2;
-        return {e, g};
+    const int rest = d.width - d.rotated, part = interleaved ? d.rotated : d.rotated / 2, whole = dtype == BNS_F32 ? 4 : 8;
+    for (int e = whole; e > 1; e /= 2) {
+        if (d.width < e || (d.rotated > 0 && part < e)) continue;
+        const int turned = (part + e - 1) / e, others = (rest + e - 1) / e, units = interleaved ? (turned + others + 1) / 2 : turned + (others + 1) / 2;
+        if (units > kWave * (e == 2 ? 2 : 1)) continue;
+        if (e < whole) return {e, e == 4 && units <= 8 ? 8 : units <= (e == 2 ? 32 : 16) ? 16 : 64, true};
+        int g = 4;
+        while (g < units) g *= 2;
+        return {e, g, part % e || rest % e};
     }
-    return (d.width + 1) / 2 <= 64 ? QkPlan{1, 16} : QkPlan{1, 64};
+    return {1, (d.width + 1) / 2 <= 64 ? 16 : 64, false};
 }
 
 // Blocks of the queries and of the keys, each.  (us: forward, 16384 x (32 + 8) x 128 bf16, 512 blocks 68.5, 1024 65.1, 2048 64.3; backward 384 112, 448 111, 512 106, 768 108.)
@@ -585,49 +627,53 @@ void fill(QkArgs* a, const bns_qk* qk, const QkDims& d, const QkPlan& plan, int 
     for (int i = 0; i < 2; ++i) share_out(&a->part[i], plan, d.tokens, d.heads[i], most);
 }
 
-#define BNS_QK_ONE(KERNEL, T, E, G, UPL, NB)                                                                                   \
-    do {                                                                                                                       \
-        if (nt) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, true>), grid, dim3(kThreads), 0, st, a);                                       \
-        else BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, false>), grid, dim3(kThreads), 0, st, a);                                         \
+#define BNS_QK_ONE(KERNEL, T, E, G, UPL, NB, RAGGED, NT) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, RAGGED, NT>), grid, dim3(kThreads), 0, st, a)
+#define BNS_QK_CASE(KERNEL, T, E, G)                                                \
+    do {                                                                            \
+        if (plan.group != G) break;                                                 \
+        if (plan.ragged && a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true, true, false);    \
+        else if (plan.ragged) BNS_QK_ONE(KERNEL, T, E, G, 1, false, true, false);   \
+        else if (a.interleaved && nt) BNS_QK_ONE(KERNEL, T, E, G, 1, true, false, true);        \
+        else if (a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true, false, false); \
+        else if (nt) BNS_QK_ONE(KERNEL, T, E, G, 1, false, false, true);            \
+        else BNS_QK_ONE(KERNEL, T, E, G, 1, false, false, false);                   \
     } while (0)
-#define BNS_QK_CASE(KERNEL, T, E, G)                                    \
-    do {                                                                \
-        if (a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true);        \
-        else BNS_QK_ONE(KERNEL, T, E, G, 1, false);                     \
-    } while (0)
-#define BNS_QK_SINGLE(KERNEL, T, E, G, UPL, NB) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, false>), grid, dim3(kThreads), 0, st, a)
-#define BNS_QK_FEW(KERNEL, T, E, G, UPL)                                \
-    do {                                                                \
-        if (a.interleaved) BNS_QK_SINGLE(KERNEL, T, E, G, UPL, true);   \
-        else BNS_QK_SINGLE(KERNEL, T, E, G, UPL, false);                \
+#define BNS_QK_FEW(KERNEL, T, E, G, UPL)                                            \
+    do {                                                                            \
+        if (plan.chunk != E || plan.group != G) break;                              \
+        if (a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, UPL, true, true, false);     \
+        else BNS_QK_ONE(KERNEL, T, E, G, UPL, false, true, false);                  \
     } while (0)
 #define BNS_QK_SMALL(KERNEL, T)                                                     \
     do {                                                                            \
-        if (plan.chunk == 1 && plan.group == 16) BNS_QK_SINGLE(KERNEL, T, 1, 16, 4, false); \
-        else if (plan.chunk == 1) BNS_QK_SINGLE(KERNEL, T, 1, 64, 4, false);        \
-        else if (plan.group == 8) BNS_QK_FEW(KERNEL, T, 2, 8, 2);                   \
-        else if (plan.group == 16) BNS_QK_FEW(KERNEL, T, 2, 16, 2);                 \
-        else if (plan.group == 32) BNS_QK_FEW(KERNEL, T, 2, 32, 2);                 \
-        else BNS_QK_FEW(KERNEL, T, 2, 64, 2);                                       \
+        BNS_QK_FEW(KERNEL, T, 2, 16, 2);                                            \
+        BNS_QK_FEW(KERNEL, T, 2, 64, 2);                                            \
+        if (plan.chunk == 1 && plan.group == 16) BNS_QK_ONE(KERNEL, T, 1, 16, 4, false, false, false);  \
+        else if (plan.chunk == 1) BNS_QK_ONE(KERNEL, T, 1, 64, 4, false, false, false);     \
     } while (0)
 #define BNS_QK_LAUNCH(KERNEL)                                                       \
     do {                                                                            \
-        if (plan.chunk <= 2 && f32) BNS_QK_SMALL(KERNEL, float);                    \
-        else if (plan.chunk <= 2) BNS_QK_SMALL(KERNEL, bf16_t);                     \
-        else if (f32 && plan.group == 4) BNS_QK_CASE(KERNEL, float, 4, 4);          \
-        else if (f32 && plan.group == 8) BNS_QK_CASE(KERNEL, float, 4, 8);          \
-        else if (f32 && plan.group == 16) BNS_QK_CASE(KERNEL, float, 4, 16);        \
-        else if (f32 && plan.group == 32) BNS_QK_CASE(KERNEL, float, 4, 32);        \
-        else if (f32) BNS_QK_CASE(KERNEL, float, 4, 64);                            \
-        else if (plan.chunk == 4 && plan.group == 4) BNS_QK_FEW(KERNEL, bf16_t, 4, 4, 1);   \
-        else if (plan.chunk == 4 && plan.group == 8) BNS_QK_FEW(KERNEL, bf16_t, 4, 8, 1);   \
-        else if (plan.chunk == 4 && plan.group == 16) BNS_QK_FEW(KERNEL, bf16_t, 4, 16, 1); \
-        else if (plan.chunk == 4 && plan.group == 32) BNS_QK_FEW(KERNEL, bf16_t, 4, 32, 1); \
-        else if (plan.chunk == 4) BNS_QK_FEW(KERNEL, bf16_t, 4, 64, 1);             \
-        else if (plan.group == 4) BNS_QK_CASE(KERNEL, bf16_t, 8, 4);                \
-        else if (plan.group == 8) BNS_QK_CASE(KERNEL, bf16_t, 8, 8);                \
-        else if (plan.group == 16) BNS_QK_CASE(KERNEL, bf16_t, 8, 16);              \
-        else BNS_QK_CASE(KERNEL, bf16_t, 8, 32);                                    \
+        if (plan.chunk <= 2 && f32) {                                               \
+            BNS_QK_SMALL(KERNEL, float);                                            \
+        } else if (plan.chunk <= 2) {                                               \
+            BNS_QK_SMALL(KERNEL, bf16_t);                                           \
+        } else if (f32) {                                                           \
+            BNS_QK_CASE(KERNEL, float, 4, 4);                                       \
+            BNS_QK_CASE(KERNEL, float, 4, 8);                                       \
+            BNS_QK_CASE(KERNEL, float, 4, 16);                                      \
+            BNS_QK_CASE(KERNEL, float, 4, 32);                                      \
+            BNS_QK_CASE(KERNEL, float, 4, 64);                                      \
+        } else if (plan.chunk == 4) {                                               \
+            BNS_QK_FEW(KERNEL, bf16_t, 4, 8, 1);                                    \
+            BNS_QK_FEW(KERNEL, bf16_t, 4, 16, 1);                                   \
+            BNS_QK_FEW(KERNEL, bf16_t, 4, 64, 1);                                   \
+        } else {                                                                    \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 4);                                      \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 8);                                      \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 16);                                     \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 32);                                     \
+            BNS_QK_FEW(KERNEL, bf16_t, 8, 64, 1);                                   \
+        }                                                                           \
     } while (0)
 
 // What both directions take: the weights, positions and frequencies.

@@ -96,6 +96,22 @@ CASES = [  # tokens, q heads, k heads, width, rotated, interleaved, norm, layout
     (12, 2, 1, 500, 252, True, True, "dense", 5000),
     (19, 4, 2, 66, 34, True, True, "packed", 5000),
     (8, 2, 1, 250, 250, True, True, "dense", 5000),
+    (70, 6, 2, 83, 40, True, True, "dense", 5000),
+    (70, 6, 2, 83, 40, False, True, "packed", 5000),
+    (90, 23, 5, 46, 10, False, True, "dense", 5000),
+    (33, 30, 30, 47, 46, False, True, "loose", 5000),
+    (33, 7, 3, 47, 46, True, False, "dense", 5000),
+    (12, 5, 2, 213, 212, True, True, "packed", 5000),
+    (12, 5, 2, 243, 242, False, True, "head_major", 5000),
+    (9, 2, 1, 507, 10, False, True, "dense", 5000),
+    (9, 2, 1, 511, 36, False, True, "packed", 5000),
+    (9, 2, 1, 509, 18, True, True, "head_major_loose", 5000),
+    (1, 3, 1, 31, 30, False, True, "dense", 5000),
+    (40, 3, 2, 9, 8, True, True, "packed", 5000),
+    (40, 3, 2, 17, 16, False, True, "dense", 5000),
+    (40, 3, 2, 26, 0, False, True, "dense", 5000),
+    (40, 3, 2, 14, 12, True, True, "loose", 5000),
+    (600, 16, 16, 25, 18, False, True, "dense", 5000),
 ]
 
 
@@ -140,11 +156,11 @@ def test_forward_and_backward(case, dtype):
     tail_is_whole(workspace, room)
 
 
-@pytest.mark.parametrize("dtype,width", [("f32", 4), ("f32", 12), ("bf16", 8), ("bf16", 24), ("bf16", 20), ("bf16", 4), ("bf16", 6), ("f32", 6)])
+@pytest.mark.parametrize("dtype,width", [("f32", 4), ("f32", 12), ("bf16", 8), ("bf16", 24), ("bf16", 20), ("bf16", 4), ("bf16", 6), ("f32", 6), ("bf16", 9), ("bf16", 22), ("f32", 10)])
 def test_angles_of_an_earlier_call_that_are_nan(dtype, width):
     """Neighbours paired and turned all, an odd number of chunks: the last lane has one chunk, and the other's angles are whatever lies behind those of the
     head.  A call before whose angles are all NaN is what may lie there."""
-    tokens, heads, rotated = 2048, 64, width
+    tokens, heads, rotated = 2048, 64, width // 2 * 2
     print(f"[gpu-case] qk after NaN {dtype} {width}", flush=True)
     wide = bns.make_qk(tokens, heads, heads, 512, dtype, rotated=512, interleaved=True)
     x = torch.ones(tokens, heads, 512, dtype=TYPES[dtype], device="cuda")
@@ -163,7 +179,7 @@ def test_angles_of_an_earlier_call_that_are_nan(dtype, width):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("width,rotated", [(128, 128), (64, 32), (50, 20)])
+@pytest.mark.parametrize("width,rotated", [(128, 128), (64, 32), (50, 20), (37, 34), (75, 22)])
 def test_in_place_in_a_projection_s_result(width, rotated, dtype):
     """Queries and keys beside their values, replaced where they are; the values stay.  Then the same backward, gradients in place."""
     tokens, hq, hk = 45, 6, 2
