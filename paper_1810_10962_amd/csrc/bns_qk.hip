@@ -12,7 +12,8 @@
 // series to x^9 and x^10 leave 2e-9 there.
 //
 // Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.4 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s); backward of 16 384 tokens 105 us (503 MB,
-// 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches.  Without the next turn's elements on their way: 46 us forward, and 2048 tokens'
+// 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches,
+// of one or two tokens 5 to 6 in one.  Without the next turn's elements on their way: 46 us forward, and 2048 tokens'
 // backward 20 us instead of 16.
 // Heads that are no whole chunks: 9109 x (48 + 6) x 83 bf16 44.5 us (164 MB), by single elements 102; backward of 9537 x (23 + 23) x 46, of which 10 turn, 45.0 (121 MB),
 // by single elements 198.
@@ -600,6 +601,10 @@ constexpr int kMostForwardBlocks = 2048, kMostBackwardBlocks = 512;
 // Turns that make a wave worth its beginning, where that leaves enough waves (2048 x (32 + 8) x 128 bf16 forward, a turn a wave 11.5 us, two 9.7).
 constexpr int64_t kTurnsOfWave = 2, kEnoughTurns = 4096;
 
+// Backward: turns of a tensor that one block takes, so that there are no other blocks' sums to add and no second launch: two a wave.  (us, in one launch against two: (32 + 8) x 128
+// bf16, 1 token 4.9 against 8.2, 2 tokens, 8 turns, 6.0 against 9.4, 4 tokens 8.4 against 8.3, 8 tokens 13.5 against 9.2; (4 + 4) x 16, 32 tokens, 8 turns, 7.0 against 8.8.)
+constexpr int64_t kTurnsAtOnce = 2 * kWaves;
+
 // Shares the turns of a tensor out over at most `most` blocks.
 void share_out(Heads* p, const QkPlan& plan, int64_t tokens, int heads, int most) {
     const int slots = kWave / plan.group;
@@ -775,13 +780,23 @@ bns_status bns_qk_backward(const bns_qk* qk, const void* q, const void* k, const
         a.part[i].os = d.dx[i];
     }
     const bool f32 = qk->dtype == BNS_F32, nt = size_t(d.tokens) * (size_t(d.heads[0]) + d.heads[1]) * d.width * e * 3 > kStreamBytes;
+    const bool at_once = std::max(a.part[0].units, a.part[1].units) <= kTurnsAtOnce;
+    if (at_once) {
+        for (int i = 0; i < 2; ++i) {
+            Heads& p = a.part[i];
+            if (!dweight[i]) continue;
+            p.run = std::max(1, int(p.units + kWaves - 1) / kWaves);
+            p.blocks = 1;           // (of no heads, too: its sums are zero)
+            p.partial = dweight[i];
+        }
+    }
     const dim3 grid{uint32_t(a.part[0].blocks + a.part[1].blocks)};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (grid.x > 0) {
         BNS_QK_LAUNCH(qk_backward_kernel);
         if (hipGetLastError() != hipSuccess) return BNS_EDEVICE;
     }
-    if (!dq_weight && !dk_weight) return BNS_OK;
+    if (at_once || (!dq_weight && !dk_weight)) return BNS_OK;
     SumArgs sum{};
     for (int i = 0; i < 2; ++i) {
         sum.partial[i] = a.part[i].partial;

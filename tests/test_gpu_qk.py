@@ -112,6 +112,12 @@ CASES = [  # tokens, q heads, k heads, width, rotated, interleaved, norm, layout
     (40, 3, 2, 26, 0, False, True, "dense", 5000),
     (40, 3, 2, 14, 12, True, True, "loose", 5000),
     (600, 16, 16, 25, 18, False, True, "dense", 5000),
+    (2, 32, 8, 128, 128, False, True, "packed", 5000),      # (the sums of one block: up to 8 turns of a wave)
+    (3, 32, 8, 128, 128, False, True, "packed", 5000),
+    (2, 0, 8, 64, 64, True, True, "dense", 5000),
+    (1, 5, 0, 243, 242, False, True, "dense", 5000),
+    (32, 4, 4, 16, 16, False, True, "dense", 5000),
+    (33, 4, 4, 16, 16, False, True, "dense", 5000),
 ]
 
 
@@ -176,6 +182,27 @@ def test_angles_of_an_earlier_call_that_are_nan(dtype, width):
     bns.bns_qk_backward(spec, *[d[0].cuda() for d in data], *w, data[0][2].cuda(), f.cuda(), *[d[3].cuda() for d in data], *dx, *dw, workspace)
     for i in range(2):
         assert_backward(dx[i], dw[i], data[i][0], data[i][1], data[0][2], f, data[i][3], rotated, True, dtype)
+
+
+def test_one_weight_and_no_tokens():
+    """Weights on one side only, of few and of many tokens; without tokens the weights' gradients are zero."""
+    print("[gpu-case] qk one weight", flush=True)
+    for tokens in (0, 2, 300):
+        x, dy = (torch.randn(tokens, 4, 64, device="cuda") for _ in range(2))
+        weight, turns = torch.rand(64, device="cuda") + 0.5, frequencies(64).cuda()
+        positions = torch.arange(tokens, device="cuda")
+        spec = bns.make_qk(tokens, 4, 4, 64, "f32", eps=EPS)
+        workspace = torch.empty(bns.bns_qk_workspace_bytes(spec), dtype=torch.uint8, device="cuda")
+        results = []
+        for weights in ((weight, None), (None, weight), (weight, weight)):
+            dx = [torch.empty_like(x) for _ in "qk"]
+            dw = [None if w is None else torch.full((64,), 7.0, device="cuda") for w in weights]
+            bns.bns_qk_backward(spec, x, x, *weights, positions, turns, dy, dy, *dx, *dw, workspace)
+            results.append((dx, dw))
+        (a, da), (b, db), (both, dboth) = results
+        assert torch.equal(a[0], both[0]) and torch.equal(b[1], both[1]) and torch.equal(both[0], both[1]) and torch.equal(a[1], b[0])
+        assert torch.equal(da[0], dboth[0]) and torch.equal(db[1], dboth[1]) and torch.equal(dboth[0], dboth[1])
+        assert da[1] is None and (tokens > 0 or not bool(dboth[0].any()))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
