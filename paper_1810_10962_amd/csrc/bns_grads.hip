@@ -7,6 +7,9 @@
 // from the last to the first: what the norm has read last is still in the memory-side cache (242 MB: 117 us instead of 121).
 //
 // The list comes with the kernel's arguments where it is short, else through the workspace, written there by launches that carry it.
+//
+// Measured: 1.3e9 bf16 elements in 194 tensors 1263 us, 388 the norm (2.6 GB, 6.8 TB/s) and 862 the scaling (5.2 GB, 6.1 TB/s); 13.7 MB of fp32 in 34 tensors 13.4 us, two launches that
+// find it in the memory-side cache.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -26,8 +26,10 @@ struct Words<float> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(w[i]);
     }
-    static __device__ __forceinline__ float lowest(u4 w) { return __uint_as_float(w[0]); }
-    static __device__ __forceinline__ u4 next(u4 w) { return u4{w[1], w[2], w[3], 0}; }      // (without its lowest element)
+    static __device__ __forceinline__ float element(u4 w, int i) {
+        const uint32_t a = i & 1 ? w[1] : w[0], b = i & 1 ? w[3] : w[2];
+        return __uint_as_float(i & 2 ? b : a);
+    }
     template <bool NT>
     static __device__ __forceinline__ void store(float* p, int left, const float (&f)[4]) {
         if (left >= 4) {
@@ -61,9 +63,9 @@ struct Words<bf16_t> {
             f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
-    static __device__ __forceinline__ float lowest(u4 w) { return __uint_as_float(w[0] << 16); }
-    static __device__ __forceinline__ u4 next(u4 w) {
-        return u4{__builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16), __builtin_amdgcn_alignbit(w[3], w[2], 16), w[3] >> 16};
+    static __device__ __forceinline__ float element(u4 w, int i) {
+        const uint32_t a = i & 2 ? w[1] : w[0], b = i & 2 ? w[3] : w[2], both = i & 4 ? b : a;
+        return __uint_as_float(i & 1 ? both & 0xffff0000u : both << 16);
     }
     template <bool NT>
     static __device__ __forceinline__ void store(bf16_t* p, int left, const float (&f)[8]) { Row8<bf16_t>::store<NT>(p, left, f); }
