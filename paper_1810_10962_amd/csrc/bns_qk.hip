@@ -15,8 +15,8 @@
 // 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches,
 // of one or two tokens 5 to 6 in one.  Without the next turn's elements on their way: 46 us forward, and 2048 tokens'
 // backward 20 us instead of 16.
-// Heads that are no whole chunks: 9109 x (48 + 6) x 83 bf16 44.5 us (164 MB), by single elements 102; backward of 9537 x (23 + 23) x 46, of which 10 turn, 45.0 (121 MB),
-// by single elements 198.
+// Heads that are no whole chunks: 9109 x (48 + 6) x 83 bf16 44.5 us (164 MB), by single elements 102; backward of 9537 x (23 + 23) x 46, of which 10 turn, 45.6 (121 MB),
+// by single elements 198; backward of 2905 x (119 + 17) x 16, of which 4 turn, 32.5, by chunks of two elements 77.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -164,60 +164,66 @@ __device__ __forceinline__ void turn_by(double position, double quarters, float*
     *s = quadrant & 2 ? -b : b;             // 2, -2, -1 (as 3): negative
 }
 
-// What a lane holds of a head, the same for every head.  RAGGED: the halves of what is rotated (or all of it, for neighbours) and the rest need not be whole chunks: the
-// last chunk of each begins further down, so that it ends where they do, and its first elements are another lane's too.  Both lanes work them out and write the same;
-// one counts them.  A rest shorter than a chunk begins among the rotated elements, which only their own lanes write.
-template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool RAGGED>
+// What a lane holds of a head, the same for every head.  RAGGED: what is rotated (its halves; all of it, for neighbours) and the rest need not be whole chunks.  The last chunk
+// of each begins further down, so that it ends where they do, and its first elements are another lane's too: both work them out and write the same, one counts them.
+// Where that is not so, a rest shorter than a chunk that begins among the rotated elements, it writes its own only.  Neighbours' last chunk goes on into the rest instead, where the
+// head is long enough.  INNER: halves that lie in one chunk together are rotated there.
+enum Form { WHOLE = 0, RAGGED = 1, INNER = 2 };
+template <typename T, int E, int G, int UPL, bool NEIGHBOURS, int FORM>
 struct Lane {
+    static constexpr bool kOverlap = FORM != WHOLE, kInner = FORM == INNER;
     int at[UPL][2];             // first elements of its chunks; -1: none
     int own[UPL][2];            // from which one on they count
     bool turned[UPL][2];
-    bool short_rest;
+    bool alone;                 // the last chunk writes its own elements only
 
-    // Chunk q of the rest.
-    __device__ __forceinline__ void set_rest(const QkArgs& a, int k, int c, int q) {
-        const int from = a.rotated + q * E;
-        at[k][c] = from >= a.width ? -1 : !RAGGED ? from : min(from, a.width - E);
-        own[k][c] = RAGGED ? from - at[k][c] : 0;
+    // Chunk q of what lies behind `begin` and is not rotated.
+    __device__ __forceinline__ void set_rest(const QkArgs& a, int k, int c, int q, int begin) {
+        const int from = begin + q * E;
+        at[k][c] = from >= a.width ? -1 : !kOverlap ? from : min(from, a.width - E);
+        own[k][c] = kOverlap ? from - at[k][c] : 0;
         turned[k][c] = false;
     }
     __device__ __forceinline__ void set(const QkArgs& a, int l) {
-        short_rest = RAGGED && a.rotated < a.width && a.width - a.rotated < E;
+        const int half = a.rotated / 2;
+        const int chunks = kInner ? 0 : ((NEIGHBOURS ? a.rotated : half) + E - 1) / E;       // that are rotated (halves: each)
+        int begin = kInner ? 0 : a.rotated;
+        if (kOverlap && NEIGHBOURS && chunks * E <= a.width) begin = chunks * E;
+        alone = kOverlap && a.width - E < a.rotated && (a.width - begin) % E != 0;
 #pragma unroll
         for (int k = 0; k < UPL; ++k) {
             const int u = k * G + l;
             if (NEIGHBOURS) {
-                const int chunks = RAGGED ? (a.rotated + E - 1) / E : a.rotated / E;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int j = 2 * u + c;
                     if (j < chunks) {
-                        at[k][c] = RAGGED ? min(j * E, a.rotated - E) : j * E;
+                        at[k][c] = kOverlap ? min(j * E, begin - E) : j * E;
                         own[k][c] = j * E - at[k][c];
                         turned[k][c] = true;
                     } else {
-                        set_rest(a, k, c, j - chunks);
+                        set_rest(a, k, c, j - chunks, begin);
                     }
                 }
+            } else if (u < chunks) {
+                const int o = kOverlap ? min(u * E, half - E) : u * E;
+                at[k][0] = o;
+                at[k][1] = half + o;
+                own[k][0] = own[k][1] = u * E - o;
+                turned[k][0] = turned[k][1] = true;
             } else {
-                const int half = a.rotated / 2, chunks = RAGGED ? (half + E - 1) / E : half / E;
-                if (u < chunks) {
-                    const int o = RAGGED ? min(u * E, half - E) : u * E;
-                    at[k][0] = E == 1 && a.interleaved ? 2 * o : o;
-                    at[k][1] = E == 1 && a.interleaved ? 2 * o + 1 : half + o;
-                    own[k][0] = own[k][1] = u * E - o;
-                    turned[k][0] = turned[k][1] = true;
-                } else {
-                    set_rest(a, k, 0, 2 * (u - chunks));
-                    set_rest(a, k, 1, 2 * (u - chunks) + 1);
-                }
+                set_rest(a, k, 0, 2 * (u - chunks), begin);
+                set_rest(a, k, 1, 2 * (u - chunks) + 1, begin);
             }
         }
+        if (kInner && l == 0) turned[0][0] = true;
     }
     // Whether element i of a chunk counts here.
-    __device__ __forceinline__ bool counts(int k, int c, int i) const { return !RAGGED || i >= own[k][c]; }
+    __device__ __forceinline__ bool counts(int k, int c, int i) const { return !kOverlap || i >= own[k][c]; }
+    // Whether a chunk may be written as a whole.
+    __device__ __forceinline__ bool whole(const QkArgs& a, int k, int c) const { return !(alone && !turned[k][c] && at[k][c] < a.rotated); }
     // Place of the first angle of chunk c (0, or halves) among a token's angles (0 where it is not turned).
-    __device__ __forceinline__ int angle(const QkArgs& a, int k, int c) const { return !turned[k][c] ? 0 : NEIGHBOURS || (E == 1 && a.interleaved) ? at[k][c] / 2 : at[k][c]; }
+    __device__ __forceinline__ int angle(const QkArgs& a, int k, int c) const { return !turned[k][c] ? 0 : NEIGHBOURS ? at[k][c] / 2 : at[k][c]; }
     // Its elements' weights (0 for a chunk that is not there, behind the last one).
     __device__ __forceinline__ void weights(float (&w)[UPL][2][E], const float* weight) const {
 #pragma unroll
@@ -249,39 +255,58 @@ struct Lane {
             }
     }
     template <bool NT>
-    __device__ __forceinline__ void store(T* base, const Offsets& o, const float (&v)[UPL][2][E]) const {
+    __device__ __forceinline__ void store(const QkArgs& a, T* base, const Offsets& o, const float (&v)[UPL][2][E]) const {
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (at[k][i] >= 0 && !(short_rest && !turned[k][i])) Chunk<T, E>::template store<NT>(base + o.to[k][i], v[k][i]);
-        if (!short_rest) return;
+                if (at[k][i] >= 0 && whole(a, k, i)) Chunk<T, E>::template store<NT>(base + o.to[k][i], v[k][i]);
+        if (!alone) return;
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                if (at[k][c] < 0 || turned[k][c]) continue;
+                if (at[k][c] < 0 || whole(a, k, c)) continue;
 #pragma unroll
-                for (int i = 1; i < E; ++i)
+                for (int i = 0; i < E; ++i)
                     if (i >= own[k][c]) Vec<T, 1>{{v[k][c][i]}}.store(base + o.to[k][c] + i);
             }
     }
     // Whether every chunk is turned.  (A chunk that is not there has no angles: behind those of the head lies what an earlier kernel left, NaN perhaps.)
-    static __device__ __forceinline__ bool all_turned(const QkArgs& a) { return !RAGGED && a.rotated == a.width && !(NEIGHBOURS && a.width % (2 * E)); }
+    static __device__ __forceinline__ bool all_turned(const QkArgs& a) { return !kOverlap && a.rotated == a.width && !(NEIGHBOURS && a.width % (2 * E)); }
     // BACK: by the negative angle.  `all`: every chunk is turned.
     template <bool BACK>
-    __device__ __forceinline__ void rotate(float (&v)[UPL][2][E], const float (&cs)[UPL][E], const float (&sn)[UPL][E], bool all) const {
+    __device__ __forceinline__ void rotate(const QkArgs& a, float (&v)[UPL][2][E], const float (&cs)[UPL][E], const float (&sn)[UPL][E], bool all) const {
+        const auto turn = [](float& x, float& y, float c, float s, bool here) {
+            s = BACK ? -s : s;
+            const float xr = fmaf(x, c, -(y * s)), yr = fmaf(x, s, y * c);
+            x = here ? xr : x;
+            y = here ? yr : y;
+        };
+        if constexpr (kInner) {     // (the first chunk's pairs: i and i + half)
+            const auto turn_all = [&](auto half) {
+#pragma unroll
+                for (int i = 0; i < half.value; ++i) turn(v[0][0][i], v[0][0][i + half.value], cs[0][i], sn[0][i], turned[0][0]);
+            };
+            if (a.rotated == 2) turn_all(std::integral_constant<int, 1>());
+            if constexpr (E >= 4) {
+                if (a.rotated == 4) turn_all(std::integral_constant<int, 2>());
+            }
+            if constexpr (E >= 8) {
+                if (a.rotated == 6) turn_all(std::integral_constant<int, 3>());
+                if (a.rotated == 8) turn_all(std::integral_constant<int, 4>());
+            }
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < UPL; ++k)
 #pragma unroll
             for (int i = 0; i < E; ++i) {
                 constexpr int H = E / 2 > 0 ? E / 2 : 1;
                 const int c = NEIGHBOURS ? i / H : 0, j = NEIGHBOURS ? i % H : i;
-                float &x = NEIGHBOURS ? v[k][c][2 * j] : v[k][0][i], &y = NEIGHBOURS ? v[k][c][2 * j + 1] : v[k][1][i];
-                const float s = BACK ? -sn[k][i] : sn[k][i];
-                const float xr = fmaf(x, cs[k][i], -(y * s)), yr = fmaf(x, s, y * cs[k][i]);
-                x = all || turned[k][c] ? xr : x;
-                y = all || turned[k][c] ? yr : y;
+                const bool here = all || (turned[k][c] && (!(kOverlap && NEIGHBOURS) || at[k][c] + 2 * j < a.rotated));
+                if (NEIGHBOURS) turn(v[k][c][2 * j], v[k][c][2 * j + 1], cs[k][i], sn[k][i], here);
+                else turn(v[k][0][i], v[k][1][i], cs[k][i], sn[k][i], here);
             }
     }
 };
@@ -387,12 +412,12 @@ struct Walk {
     }
 };
 
-template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool RAGGED, bool NT>
+template <typename T, int E, int G, int UPL, bool NEIGHBOURS, int FORM, bool NT>
 __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkArgs a) {
     __shared__ Angles<E, UPL> angles;
     Walk<T, E, G, UPL, NEIGHBOURS> at(a, angles);
     const Heads& p = at.p;
-    Lane<T, E, G, UPL, NEIGHBOURS, RAGGED> mine;
+    Lane<T, E, G, UPL, NEIGHBOURS, FORM> mine;
     Chunk<T, E> next[UPL][2];
     mine.set(a, at.lane % G);
     const auto x_to = mine.offsets(at.of_lane(p.xs)), out_to = mine.offsets(at.of_lane(p.os));
@@ -439,21 +464,21 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkArgs a) {
         if (a.rotated > 0) {
             float cs[UPL][E], sn[UPL][E];
             at.get(cs, sn, mine);
-            mine.template rotate<false>(v, cs, sn, all);
+            mine.template rotate<false>(a, v, cs, sn, all);
         }
-        mine.template store<NT>(out, out_to, v);
+        mine.template store<NT>(a, out, out_to, v);
     }
 }
 
-template <typename T, int E, int G, int UPL, bool NEIGHBOURS, bool RAGGED, bool NT>
-__global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
+template <typename T, int E, int G, int UPL, bool NEIGHBOURS, int FORM, bool NT>
+__global__ void __launch_bounds__(kThreads, UPL == 1 ? 4 : 1) qk_backward_kernel(QkArgs a) {       // (four waves a SIMD: 128 registers)
     __shared__ union {
         Angles<E, UPL> angles;
         float sums[UPL * 2 * E][kThreads];
     } lds;
     Walk<T, E, G, UPL, NEIGHBOURS> at(a, lds.angles);
     const Heads& p = at.p;
-    Lane<T, E, G, UPL, NEIGHBOURS, RAGGED> mine;
+    Lane<T, E, G, UPL, NEIGHBOURS, FORM> mine;
     Chunk<T, E> next_x[UPL][2], next_g[UPL][2];
     mine.set(a, at.lane % G);
     const auto x_to = mine.offsets(at.of_lane(p.xs)), dy_to = mine.offsets(at.of_lane(p.ds)), out_to = mine.offsets(at.of_lane(p.os));
@@ -492,7 +517,7 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
         if (a.rotated > 0) {
             float cs[UPL][E], sn[UPL][E];
             at.get(cs, sn, mine);
-            mine.template rotate<true>(g, cs, sn, all);
+            mine.template rotate<true>(a, g, cs, sn, all);
         }
         if (p.weight) {
             float squares = 0.f, dot = 0.f, w[UPL][2][E];
@@ -520,7 +545,7 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkArgs a) {
                         g[k][c][i] = rstd * fmaf(g[k][c][i], w[k][c][i], -xh * mean);
                     }
         }
-        mine.template store<NT>(out, out_to, g);
+        mine.template store<NT>(a, out, out_to, g);
     }
     if (!p.weight) return;
     // The block's sums: the lanes that hold the same elements, in their order.
@@ -576,24 +601,26 @@ __global__ void __launch_bounds__(kSumColumns * kSumLanes) qk_weight_sum_kernel(
     }
 }
 
-// How a head lies in lanes: chunks of 16 bytes where what is rotated and the rest are whole ones (`ragged` 0), or at least hold one; of four or two elements, or single
-// ones, where they are shorter.
+// How a head lies in lanes: chunks of 16 bytes, RAGGED where what is rotated and the rest are not whole ones; of fewer elements where halves are shorter and too long to
+// lie in one together, and where ragged heads would need more lanes than there are.
 struct QkPlan {
-    int chunk, group;
-    bool ragged;
+    int chunk, group, form;
 };
 QkPlan qk_plan(const QkDims& d, int32_t dtype, bool interleaved) {
-    const int rest = d.width - d.rotated, part = interleaved ? d.rotated : d.rotated / 2, whole = dtype == BNS_F32 ? 4 : 8;
-    for (int e = whole; e > 1; e /= 2) {
-        if (d.width < e || (d.rotated > 0 && part < e)) continue;
-        const int turned = (part + e - 1) / e, others = (rest + e - 1) / e, units = interleaved ? (turned + others + 1) / 2 : turned + (others + 1) / 2;
+    const int half = d.rotated / 2, largest = dtype == BNS_F32 ? 4 : 8;
+    for (int e = largest; e > 1; e /= 2) {
+        const bool inner = !interleaved && d.rotated > 0 && d.rotated <= e;
+        if (d.width < e || (!interleaved && !inner && d.rotated > 0 && half < e)) continue;
+        const int turned = inner ? 0 : ((interleaved ? d.rotated : half) + e - 1) / e;
+        const int begin = inner ? 0 : interleaved && turned * e <= d.width ? turned * e : d.rotated, others = (d.width - begin + e - 1) / e;
+        const int units = interleaved ? (turned + others + 1) / 2 : turned + (others + 1) / 2;
         if (units > kWave * (e == 2 ? 2 : 1)) continue;
-        if (e < whole) return {e, e == 4 && units <= 8 ? 8 : units <= (e == 2 ? 32 : 16) ? 16 : 64, true};
+        if (e < largest) return {e, e == 4 && units <= 8 ? 8 : units <= (e == 2 ? 32 : 16) ? 16 : 64, inner ? INNER : RAGGED};
         int g = 4;
         while (g < units) g *= 2;
-        return {e, g, part % e || rest % e};
+        return {e, g, inner ? INNER : d.width % e != 0 || d.rotated % (interleaved ? e : 2 * e) != 0 ? RAGGED : WHOLE};
     }
-    return {1, (d.width + 1) / 2 <= 64 ? 16 : 64, false};
+    return {1, (d.width + 1) / 2 <= 64 ? 16 : 64, WHOLE};
 }
 
 // Blocks of the queries and of the keys, each.  (us: forward, 16384 x (32 + 8) x 128 bf16, 512 blocks 68.5, 1024 65.1, 2048 64.3; backward 384 112, 448 111, 512 106, 768 108.)
@@ -632,53 +659,61 @@ void fill(QkArgs* a, const bns_qk* qk, const QkDims& d, const QkPlan& plan, int 
     for (int i = 0; i < 2; ++i) share_out(&a->part[i], plan, d.tokens, d.heads[i], most);
 }
 
-#define BNS_QK_ONE(KERNEL, T, E, G, UPL, NB, RAGGED, NT) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, RAGGED, NT>), grid, dim3(kThreads), 0, st, a)
-#define BNS_QK_CASE(KERNEL, T, E, G)                                                \
-    do {                                                                            \
-        if (plan.group != G) break;                                                 \
-        if (plan.ragged && a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true, true, false);    \
-        else if (plan.ragged) BNS_QK_ONE(KERNEL, T, E, G, 1, false, true, false);   \
-        else if (a.interleaved && nt) BNS_QK_ONE(KERNEL, T, E, G, 1, true, false, true);        \
-        else if (a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true, false, false); \
-        else if (nt) BNS_QK_ONE(KERNEL, T, E, G, 1, false, false, true);            \
-        else BNS_QK_ONE(KERNEL, T, E, G, 1, false, false, false);                   \
+#define BNS_QK_ONE(KERNEL, T, E, G, UPL, NB, FORM, NT) BNS_LAUNCH((KERNEL<T, E, G, UPL, NB, FORM, NT>), grid, dim3(kThreads), 0, st, a)
+// Chunks of 16 bytes, E of the largest.
+#define BNS_QK_CASE(KERNEL, T, E, G)                                                                                            \
+    do {                                                                                                                        \
+        if (plan.group != G) break;                                                                                             \
+        if (plan.form == INNER) BNS_QK_ONE(KERNEL, T, E, G, 1, false, INNER, false);                                            \
+        else if (plan.form == RAGGED && a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true, RAGGED, false);                     \
+        else if (plan.form == RAGGED) BNS_QK_ONE(KERNEL, T, E, G, 1, false, RAGGED, false);                                     \
+        else if (a.interleaved && nt) BNS_QK_ONE(KERNEL, T, E, G, 1, true, WHOLE, true);                                        \
+        else if (a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, 1, true, WHOLE, false);                                             \
+        else if (nt) BNS_QK_ONE(KERNEL, T, E, G, 1, false, WHOLE, true);                                                        \
+        else BNS_QK_ONE(KERNEL, T, E, G, 1, false, WHOLE, false);                                                               \
     } while (0)
-#define BNS_QK_FEW(KERNEL, T, E, G, UPL)                                            \
-    do {                                                                            \
-        if (plan.chunk != E || plan.group != G) break;                              \
-        if (a.interleaved) BNS_QK_ONE(KERNEL, T, E, G, UPL, true, true, false);     \
-        else BNS_QK_ONE(KERNEL, T, E, G, UPL, false, true, false);                  \
+// One kernel, if the plan is its.
+#define BNS_QK_IF(KERNEL, T, E, G, UPL, NB, FORM)                                                                               \
+    do {                                                                                                                        \
+        if (plan.chunk == E && plan.group == G && plan.form == FORM && (NB == bool(a.interleaved) || E == 1))                   \
+            BNS_QK_ONE(KERNEL, T, E, G, UPL, NB, FORM, false);                                                                  \
     } while (0)
-#define BNS_QK_SMALL(KERNEL, T)                                                     \
-    do {                                                                            \
-        BNS_QK_FEW(KERNEL, T, 2, 16, 2);                                            \
-        BNS_QK_FEW(KERNEL, T, 2, 64, 2);                                            \
-        if (plan.chunk == 1 && plan.group == 16) BNS_QK_ONE(KERNEL, T, 1, 16, 4, false, false, false);  \
-        else if (plan.chunk == 1) BNS_QK_ONE(KERNEL, T, 1, 64, 4, false, false, false);     \
+#define BNS_QK_SMALL(KERNEL, T)                                                                                                 \
+    do {                                                                                                                        \
+        BNS_QK_IF(KERNEL, T, 2, 16, 2, false, RAGGED);                                                                          \
+        BNS_QK_IF(KERNEL, T, 2, 64, 2, false, RAGGED);                                                                          \
+        BNS_QK_IF(KERNEL, T, 2, 16, 2, true, RAGGED);                                                                           \
+        BNS_QK_IF(KERNEL, T, 2, 16, 2, false, INNER);                                                                           \
+        BNS_QK_IF(KERNEL, T, 1, 16, 4, false, WHOLE);                                                                           \
+        BNS_QK_IF(KERNEL, T, 1, 64, 4, false, WHOLE);                                                                           \
     } while (0)
-#define BNS_QK_LAUNCH(KERNEL)                                                       \
-    do {                                                                            \
-        if (plan.chunk <= 2 && f32) {                                               \
-            BNS_QK_SMALL(KERNEL, float);                                            \
-        } else if (plan.chunk <= 2) {                                               \
-            BNS_QK_SMALL(KERNEL, bf16_t);                                           \
-        } else if (f32) {                                                           \
-            BNS_QK_CASE(KERNEL, float, 4, 4);                                       \
-            BNS_QK_CASE(KERNEL, float, 4, 8);                                       \
-            BNS_QK_CASE(KERNEL, float, 4, 16);                                      \
-            BNS_QK_CASE(KERNEL, float, 4, 32);                                      \
-            BNS_QK_CASE(KERNEL, float, 4, 64);                                      \
-        } else if (plan.chunk == 4) {                                               \
-            BNS_QK_FEW(KERNEL, bf16_t, 4, 8, 1);                                    \
-            BNS_QK_FEW(KERNEL, bf16_t, 4, 16, 1);                                   \
-            BNS_QK_FEW(KERNEL, bf16_t, 4, 64, 1);                                   \
-        } else {                                                                    \
-            BNS_QK_CASE(KERNEL, bf16_t, 8, 4);                                      \
-            BNS_QK_CASE(KERNEL, bf16_t, 8, 8);                                      \
-            BNS_QK_CASE(KERNEL, bf16_t, 8, 16);                                     \
-            BNS_QK_CASE(KERNEL, bf16_t, 8, 32);                                     \
-            BNS_QK_FEW(KERNEL, bf16_t, 8, 64, 1);                                   \
-        }                                                                           \
+#define BNS_QK_LAUNCH(KERNEL)                                                                                                   \
+    do {                                                                                                                        \
+        if (plan.chunk <= 2 && f32) {                                                                                           \
+            BNS_QK_SMALL(KERNEL, float);                                                                                        \
+            BNS_QK_IF(KERNEL, float, 2, 64, 2, true, RAGGED);                                                                   \
+        } else if (plan.chunk <= 2) {                                                                                           \
+            BNS_QK_SMALL(KERNEL, bf16_t);                                                                                       \
+        } else if (f32) {                                                                                                       \
+            BNS_QK_CASE(KERNEL, float, 4, 4);                                                                                   \
+            BNS_QK_CASE(KERNEL, float, 4, 8);                                                                                   \
+            BNS_QK_CASE(KERNEL, float, 4, 16);                                                                                  \
+            BNS_QK_CASE(KERNEL, float, 4, 32);                                                                                  \
+            BNS_QK_CASE(KERNEL, float, 4, 64);                                                                                  \
+        } else if (plan.chunk == 4) {                                                                                           \
+            BNS_QK_IF(KERNEL, bf16_t, 4, 8, 1, false, RAGGED);                                                                  \
+            BNS_QK_IF(KERNEL, bf16_t, 4, 16, 1, false, RAGGED);                                                                 \
+            BNS_QK_IF(KERNEL, bf16_t, 4, 64, 1, false, RAGGED);                                                                 \
+            BNS_QK_IF(KERNEL, bf16_t, 4, 8, 1, true, RAGGED);                                                                   \
+            BNS_QK_IF(KERNEL, bf16_t, 4, 8, 1, false, INNER);                                                                   \
+        } else {                                                                                                                \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 4);                                                                                  \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 8);                                                                                  \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 16);                                                                                 \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 32);                                                                                 \
+            BNS_QK_IF(KERNEL, bf16_t, 8, 64, 1, false, RAGGED);                                                                 \
+            BNS_QK_IF(KERNEL, bf16_t, 8, 64, 1, true, RAGGED);                                                                  \
+        }                                                                                                                       \
     } while (0)
 
 // What both directions take: the weights, positions and frequencies.

@@ -118,6 +118,22 @@ CASES = [  # tokens, q heads, k heads, width, rotated, interleaved, norm, layout
     (1, 5, 0, 243, 242, False, True, "dense", 5000),
     (32, 4, 4, 16, 16, False, True, "dense", 5000),
     (33, 4, 4, 16, 16, False, True, "dense", 5000),
+    (40, 9, 3, 16, 4, False, True, "dense", 5000),
+    (40, 9, 3, 16, 4, True, True, "packed", 5000),
+    (40, 9, 3, 16, 8, False, True, "dense", 5000),
+    (40, 9, 3, 9, 8, False, True, "dense", 5000),
+    (40, 9, 3, 9, 2, False, True, "packed", 5000),
+    (40, 9, 3, 9, 6, True, True, "dense", 5000),
+    (40, 5, 3, 11, 10, True, True, "dense", 5000),
+    (40, 5, 3, 10, 6, False, True, "dense", 5000),
+    (40, 5, 3, 7, 6, False, True, "loose", 5000),
+    (40, 5, 3, 5, 4, True, True, "dense", 5000),
+    (40, 5, 3, 13, 6, False, False, "dense", 5000),
+    (20, 5, 3, 101, 2, True, True, "dense", 5000),
+    (20, 5, 3, 101, 2, False, True, "dense", 5000),
+    (20, 5, 3, 509, 6, False, True, "dense", 5000),
+    (20, 5, 3, 2, 0, False, True, "dense", 5000),
+    (20, 5, 3, 12, 12, True, True, "dense", 5000),
 ]
 
 
