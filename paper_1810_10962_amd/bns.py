@@ -502,7 +502,8 @@ class Gradients:
     def __init__(self, grads, outs=None):
         import torch
         types = {torch.float32: BNS_F32, torch.bfloat16: BNS_BF16}
-        self.grads, self.outs, self.count = list(grads), None if outs is None else list(outs), len(grads)
+        self.grads, self.outs = list(grads), None if outs is None else list(outs)
+        self.count, self.device = len(self.grads), self.grads[0].get_device() if self.grads else None
         if outs is not None and len(self.outs) != self.count:
             raise ValueError(f"{self.count} gradients and {len(self.outs)} results")
         self.array = (bns_gradient * max(1, self.count))()
@@ -511,6 +512,8 @@ class Gradients:
             for t in (g,) if out is None else (g, out):
                 if t.dtype not in types or not t.is_contiguous():
                     raise ValueError(f"gradient {i}: float32 or bfloat16 and contiguous is wanted")
+                if t.get_device() != self.device:
+                    raise ValueError(f"gradient {i}: it lies on another device than the first one (bns_grads_norm and bns_grads_scale take each device's)")
             if out is not None and (out.dtype != g.dtype or out.numel() != g.numel()):
                 raise ValueError(f"gradient {i}: its result has another type or size")
             self.array[i] = bns_gradient(g.data_ptr(), None if out is None else out.data_ptr(), g.numel(), types[g.dtype], 0)
@@ -566,16 +569,23 @@ def bns_grads_workspace_bytes(gradients) -> int:
     return int(load().bns_grads_workspace_bytes(gradients.count))
 
 
+def _grads_call(name, gradients, workspace, *args):
+    device = getattr(gradients, "device", None)         # (a caller's own list, with `count` and data_ptr(), may not say)
+    if device is not None and device != workspace.get_device():
+        raise ValueError("the gradients lie on another device than the workspace")
+    _answers_call(name, workspace, gradients, gradients.count, *args, workspace, workspace.nbytes)
+
+
 def bns_grads_norm(gradients, squares, norm, workspace):
-    _answers_call("grads_norm", workspace, gradients, gradients.count, squares, norm, workspace, workspace.nbytes)
+    _grads_call("grads_norm", gradients, workspace, squares, norm)
 
 
 def bns_grads_scale(gradients, squares, max_norm, norm, workspace):
-    _answers_call("grads_scale", workspace, gradients, gradients.count, squares, max_norm, norm, workspace, workspace.nbytes)
+    _grads_call("grads_scale", gradients, workspace, squares, max_norm, norm)
 
 
 def bns_grads_clip(gradients, max_norm, norm, workspace):
-    _answers_call("grads_clip", workspace, gradients, gradients.count, max_norm, norm, workspace, workspace.nbytes)
+    _grads_call("grads_clip", gradients, workspace, max_norm, norm)
 
 
 # --------------------------------------------------------------------------------------

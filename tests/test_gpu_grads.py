@@ -163,3 +163,21 @@ def test_a_captured_clip_is_replayed():
         norm = whole_norm(grads)
         assert abs(float(one[0]) - norm) <= 2 * U * norm
         check(outs, grads, min(1.0, 1.0 / (norm + 1e-6)))
+
+
+def test_gradients_of_several_devices_are_refused():
+    """Before anything is enqueued: host memory in a list of the device's, or with a workspace of the device's."""
+    print("[gpu-case] gradients of several devices", flush=True)
+    here, there = torch.ones(5, device="cuda"), torch.ones(5)
+    for grads in ([here, there], [there, here]):
+        with pytest.raises(ValueError):
+            bns.make_gradients(grads, grads)
+    with pytest.raises(ValueError):
+        bns.make_gradients([here], [there])
+    gradients = bns.make_gradients([there], [there])
+    workspace, one, squares = torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda"), torch.empty(1, device="cuda"), torch.empty(1, dtype=torch.float64, device="cuda")
+    for call in (lambda: bns.bns_grads_norm(gradients, squares, one, workspace), lambda: bns.bns_grads_scale(gradients, squares, 1.0, one, workspace),
+                 lambda: bns.bns_grads_clip(gradients, 1.0, one, workspace)):
+        with pytest.raises(ValueError):
+            call()
+    assert bns.make_gradients(iter([here])).count == 1 and bns.make_gradients([]).device is None
