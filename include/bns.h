@@ -588,7 +588,7 @@ typedef struct {
 } bns_gradient;
 
 /* The norm of all gradients together, and their scaling down to a largest norm.  `gradients` is a HOST array of `count` entries (at most 65536, fewer than 2^40
- * elements each and 2^43 together) that is read before the call returns; a captured call keeps what it said.
+ * elements each and 2^43 together, at addresses below 2^48) that is read before the call returns; a captured call keeps what it said.
  *   squares = sum over all elements of grad^2 (fp64: no gradient of finite elements overflows)      norm = sqrt(squares)
  *   c = min(1, max_norm / (norm + 1e-6))      out = grad * c, rounded to dtype
  * Where the norm is NaN so are c and what is scaled; where it is infinite, c = 0 (infinite elements become NaN).  Gradients in place with c = 1 are left as they are.

@@ -29,22 +29,22 @@ constexpr int kMostBlocks = 1024;       // of the norm
 // Pieces of a block of the scaling, neighbours.  Blocks start in order, so that all of them work in one stretch of memory; fewer blocks that each come by every 2048th piece
 // drift apart (1.3e9 bf16 elements, both passes: 1261 us, 1 piece 1291, 4 1323, 16 1392, every 2048th 1361).
 constexpr uint32_t kRun = 2;
-constexpr int kShort = 140;             // entries that travel with a launch, whose arguments take 4 KB at most
+constexpr int kShort = 200;             // entries that travel with a launch, whose arguments take 4 KB at most
 
-// Entries, each with the number of its first piece; those of fp32 have the lowest bit of `elements` set, above which is their number.
+// Entries: addresses, below 2^48, and the number of an entry's first piece.  Above the gradient's address: the elements of its last piece less one, and in the highest bit its type.
 struct List {
-    const void* grad[kShort];
-    void* out[kShort];
-    int64_t elements[kShort];
+    uint64_t grad[kShort], out[kShort];
     uint32_t first[kShort];
 };
 // The same of any length, in the workspace.
 struct LongList {
-    const void** grad;
-    void** out;
-    int64_t* elements;
+    uint64_t *grad, *out;
     uint32_t* first;
 };
+constexpr size_t kEntry = 20;
+constexpr int kAddressBits = 48;
+constexpr uint64_t kIsF32 = uint64_t(1) << 63;
+static_assert(kPiece / 2 <= 1 << (63 - kAddressBits), "the elements of a piece fit above an address");
 
 struct GradsArgs {
     double* partial;                    // [blocks] sums of squares
@@ -61,7 +61,6 @@ __global__ void __launch_bounds__(256) grads_list_kernel(List list, LongList out
     if (i >= entries) return;
     out.grad[at + i] = list.grad[i];
     out.out[at + i] = list.out[i];
-    out.elements[at + i] = list.elements[i];
     out.first[at + i] = list.first[i];
 }
 static_assert(kShort <= 256, "a thread for each entry");
@@ -82,11 +81,13 @@ __device__ __forceinline__ Piece piece_of(const GradsArgs& a, const L& list, uin
         if (list.first[mid] <= p) lo = mid;
         else hi = mid;
     }
-    const int64_t all = list.elements[lo];
-    const bool f32 = all & 1;
-    const int per = f32 ? kPiece / 4 : kPiece / 2;
-    const int64_t at = int64_t(p - list.first[lo]) * per, bytes = at * (f32 ? 4 : 2);
-    return {static_cast<const char*>(list.grad[lo]) + bytes, static_cast<char*>(list.out[lo]) + bytes, int(min(int64_t(per), (all >> 1) - at)), f32};
+    const uint64_t grad = list.grad[lo];
+    const bool f32 = grad & kIsF32;
+    const uint32_t first = list.first[lo], end = lo + 1 < a.entries ? list.first[lo + 1] : a.pieces;
+    const int64_t bytes = int64_t(p - first) * kPiece;
+    const int last = int(grad << 1 >> (kAddressBits + 1)) + 1;
+    return {reinterpret_cast<const char*>(grad & ((uint64_t(1) << kAddressBits) - 1)) + bytes, reinterpret_cast<char*>(list.out[lo]) + bytes,
+            p + 1 == end ? last : f32 ? kPiece / 4 : kPiece / 2, f32};
 }
 
 // What a thread has of a piece: words, and of the elements behind the last one, one of the first threads each one.
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(kThreads) grads_scale_kernel(GradsArgs a, L li
 }
 
 // Bytes of a long list's arrays, one behind the other in the workspace.
-size_t list_bytes(int32_t count) { return count > kShort ? size_t(round_up(int64_t(count) * 28, 256)) : 0; }
+size_t list_bytes(int32_t count) { return count > kShort ? size_t(round_up(int64_t(count) * int64_t(kEntry), 256)) : 0; }
 
 // The list as the kernels take it.
 struct Listed {
@@ -260,18 +261,17 @@ bns_status put_list(const bns_gradient* g, int32_t count, void* workspace, hipSt
     for (int32_t i = 0; i < count; ++i) entries += g[i].elements > 0;
     l->is_long = entries > kShort;
     char* const room = static_cast<char*>(workspace) + kMostBlocks * sizeof(double);
-    l->long_list.grad = reinterpret_cast<const void**>(room);
-    l->long_list.out = reinterpret_cast<void**>(room + size_t(entries) * 8);
-    l->long_list.elements = reinterpret_cast<int64_t*>(room + size_t(entries) * 16);
-    l->long_list.first = reinterpret_cast<uint32_t*>(room + size_t(entries) * 24);
+    l->long_list.grad = reinterpret_cast<uint64_t*>(room);
+    l->long_list.out = reinterpret_cast<uint64_t*>(room + size_t(entries) * 8);
+    l->long_list.first = reinterpret_cast<uint32_t*>(room + size_t(entries) * 16);
     uint32_t pieces = 0;        // (below 2^31 and one for every entry)
     size_t bytes = 0;
     int32_t at = 0, sent = 0;
     for (int32_t i = 0; i < count; ++i) {
         if (g[i].elements == 0) continue;
-        l->list.grad[at] = g[i].grad;
-        l->list.out[at] = g[i].out;
-        l->list.elements[at] = g[i].elements << 1 | (g[i].dtype == BNS_F32);
+        const int64_t per = kPiece / int64_t(dtype_bytes(g[i].dtype));
+        l->list.grad[at] = uint64_t(reinterpret_cast<uintptr_t>(g[i].grad)) | uint64_t((g[i].elements - 1) % per) << kAddressBits | (g[i].dtype == BNS_F32 ? kIsF32 : 0);
+        l->list.out[at] = uint64_t(reinterpret_cast<uintptr_t>(g[i].out));
         l->list.first[at++] = pieces;
         pieces += pieces_of(g[i]);
         bytes += size_t(g[i].elements) * dtype_bytes(g[i].dtype);

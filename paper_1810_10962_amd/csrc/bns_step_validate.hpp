@@ -114,6 +114,12 @@ inline bns_status check_logprob(const bns_logprob* s, LogprobDims* d) {
 
 constexpr int32_t kMostGradients = 65536;
 
+// Whether a tensor ends below 2^48 (the kernels keep more than the address in a word).
+inline bool low_address(const void* p, int64_t elements, int32_t dtype) {
+    const uint64_t most = uint64_t(1) << 48, at = reinterpret_cast<uintptr_t>(p);
+    return at < most && uint64_t(elements) * dtype_bytes(dtype) <= most - at;
+}
+
 // The entries of a list of gradients; `scaled`: with where they go.
 inline bns_status check_gradients(const bns_gradient* g, int32_t count, bool scaled) {
     if (count < 0 || (count > 0 && !g)) return BNS_EINVAL;
@@ -126,6 +132,7 @@ inline bns_status check_gradients(const bns_gradient* g, int32_t count, bool sca
         if (g[i].elements == 0) continue;
         if (!g[i].grad || !aligned_to(g[i].grad, dtype_bytes(g[i].dtype))) return BNS_EINVAL;
         if (scaled && (!g[i].out || !aligned_to(g[i].out, dtype_bytes(g[i].dtype)))) return BNS_EINVAL;
+        if (!low_address(g[i].grad, g[i].elements, g[i].dtype) || (scaled && !low_address(g[i].out, g[i].elements, g[i].dtype))) return BNS_EUNSUPPORTED;
     }
     return all < int64_t(1) << 43 ? BNS_OK : BNS_EUNSUPPORTED;
 }

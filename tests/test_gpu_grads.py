@@ -44,7 +44,8 @@ def check(got, grads, scale):
 
 
 SETS = {"one": [1], "none": [], "empty ones": [0, 5, 0, 0, 7, 0], "small": [1, 2, 3, 7, 8, 9, 15, 16, 17, 100], "ends of pieces": [8191, 8192, 8193, 16383, 16384, 16385, 32768, 32769],
-        "many": [(i * 37) % 501 + 1 for i in range(96)], "more than travel with a launch": [(i * 37) % 301 for i in range(330)], "large": [3_000_001, 5, 1_048_576]}
+        "many": [(i * 37) % 501 + 1 for i in range(96)], "more than travel with a launch": [(i * 37) % 301 for i in range(330)], "large": [3_000_001, 5, 1_048_576],
+        **{f"{n} entries": [(i * 53) % 9001 + 1 for i in range(n)] for n in (140, 199, 200, 201, 400, 401)}}
 
 
 @pytest.mark.parametrize("types", [(torch.float32,), (torch.bfloat16,), (torch.float32, torch.bfloat16, torch.bfloat16)], ids=["f32", "bf16", "mixed"])
