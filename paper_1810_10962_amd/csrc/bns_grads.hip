@@ -6,9 +6,10 @@
 // blocks' sums.  Every block of the scaling adds the blocks' sums up itself, while its first piece is on its way, so that a clip is two launches.  The scaling takes the pieces
 // from the last to the first: what the norm has read last is still in the memory-side cache (242 MB: 117 us instead of 121).
 //
-// The list comes with the kernel's arguments where it is short, else through the workspace, written there by launches that carry it.
+// The list comes with the kernel's arguments.  A longer one goes in parts, a launch each; of a clip only the norm does, whose launches leave the parts in the workspace for one launch
+// of the scaling (146 tensors of 2.2 MB 12.2 us; with more than 140 through the workspace in launches of their own 16.6, 242 tensors 16.5 against 19.5).
 //
-// Measured: 1.3e9 bf16 elements in 194 tensors 1263 us, 388 the norm (2.6 GB, 6.8 TB/s) and 862 the scaling (5.2 GB, 6.1 TB/s); 13.7 MB of fp32 in 34 tensors 13.4 us, two launches that
+// Measured: 1.3e9 bf16 elements in 194 tensors 1282 us, 390 the norm (2.6 GB, 6.7 TB/s) and 885 the scaling (5.2 GB, 5.9 TB/s); 13.7 MB of fp32 in 34 tensors 13.4 us, two launches that
 // find it in the memory-side cache.
 #include <hip/hip_runtime.h>
 
@@ -31,6 +32,10 @@ constexpr int kMostBlocks = 1024;       // of the norm
 constexpr uint32_t kRun = 2;
 constexpr int kShort = 200;             // entries that travel with a launch, whose arguments take 4 KB at most
 
+// Pieces up to which the scaling of a clip has a short list with its arguments; more blocks read it faster in the workspace, where the norm left it (us, arguments against workspace:
+// 864 pieces 13.5 against 14.0, 19000 166.5 against 166.2, 160000 1302 against 1282).
+constexpr uint32_t kFewPieces = 16384;
+
 // Entries: addresses, below 2^48, and the number of an entry's first piece.  Above the gradient's address: the elements of its last piece less one, and in the highest bit its type.
 struct List {
     uint64_t grad[kShort], out[kShort];
@@ -51,19 +56,11 @@ struct GradsArgs {
     double* squares;                    // norm: written (may be NULL); scaling: read where `partial` is NULL
     float* norm;
     float max_norm;
-    int32_t entries, blocks;            // blocks: of the norm's launch
-    uint32_t pieces, cold;              // pieces before `cold` are not in the memory-side cache when the scaling comes to them
+    int32_t entries, blocks;            // blocks: of the norm's launch, the largest one
+    uint32_t from, pieces, cold;        // pieces of the list: from `from` on; those before `cold` are not in the memory-side cache when the scaling comes to them
 };
-static_assert(sizeof(List) + sizeof(GradsArgs) <= 4096 && sizeof(List) + sizeof(LongList) + 16 <= 4096, "arguments of a launch");
-
-__global__ void __launch_bounds__(256) grads_list_kernel(List list, LongList out, int at, int entries) {
-    const int i = threadIdx.x;
-    if (i >= entries) return;
-    out.grad[at + i] = list.grad[i];
-    out.out[at + i] = list.out[i];
-    out.first[at + i] = list.first[i];
-}
-static_assert(kShort <= 256, "a thread for each entry");
+static_assert(sizeof(List) + sizeof(GradsArgs) + sizeof(LongList) + 8 <= 4096, "arguments of a launch");
+static_assert(kShort <= kThreads, "a thread for each entry");
 
 // A piece: its entry's tensors from its first element on.
 struct Piece {
@@ -160,11 +157,11 @@ __device__ __forceinline__ void put_scaled(const Held& h, const Piece& p, float 
     if (int(threadIdx.x) < left) Words<T>::put_one(out + p.n - left + threadIdx.x, h.rest * c * c2);
 }
 
-template <typename L>
-__global__ void __launch_bounds__(kThreads) grads_norm_kernel(GradsArgs a, L list) {
+// One part of a list, from entry `at` on: parts behind the first add to its sums.  `keep`: where the list is left for the scaling (may be empty).
+__global__ void __launch_bounds__(kThreads) grads_norm_kernel(GradsArgs a, List list, LongList keep, int at) {
     __shared__ double lds[kThreads / kWave];
     double s[4] = {0.0, 0.0, 0.0, 0.0};
-    uint32_t p = blockIdx.x;
+    uint32_t p = a.from + blockIdx.x;
     Held next;
     Piece piece = {};
     if (p < a.pieces) {
@@ -183,7 +180,13 @@ __global__ void __launch_bounds__(kThreads) grads_norm_kernel(GradsArgs a, L lis
         else add_squares<bf16_t>(now, s);
     }
     const double all = block_sum((s[0] + s[1]) + (s[2] + s[3]), lds);
-    if (threadIdx.x == 0) a.partial[blockIdx.x] = all;
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = at > 0 ? a.partial[blockIdx.x] + all : all;
+    if (blockIdx.x == 0 && keep.grad && int(threadIdx.x) < a.entries) {
+        const int i = threadIdx.x;
+        keep.grad[at + i] = list.grad[i];
+        keep.out[at + i] = list.out[i];
+        keep.first[at + i] = list.first[i];
+    }
 }
 
 // The sum of squares from the blocks' sums: every block of every launch adds them in the same order.
@@ -206,7 +209,7 @@ template <typename L>
 __global__ void __launch_bounds__(kThreads) grads_scale_kernel(GradsArgs a, L list) {
     __shared__ double lds[kThreads / kWave];
     uint32_t b = blockIdx.x * kRun;
-    const uint32_t b_end = min(b + kRun, a.pieces);
+    const uint32_t b_end = min(b + kRun, a.pieces - a.from);
     Held next;
     Piece piece = {};
     const auto ask_for = [&]() {
@@ -238,70 +241,75 @@ __global__ void __launch_bounds__(kThreads) grads_scale_kernel(GradsArgs a, L li
 }
 
 // Bytes of a long list's arrays, one behind the other in the workspace.
-size_t list_bytes(int32_t count) { return count > kShort ? size_t(round_up(int64_t(count) * int64_t(kEntry), 256)) : 0; }
-
-// The list as the kernels take it.
-struct Listed {
-    List list;                  // short ones
-    LongList long_list;
-    GradsArgs args;
-    bool is_long;
-};
+size_t list_bytes(int32_t count) { return size_t(round_up(int64_t(count) * int64_t(kEntry), 256)); }
 
 uint32_t pieces_of(const bns_gradient& g) {
     const int64_t per = kPiece / int64_t(dtype_bytes(g.dtype));
     return uint32_t((g.elements + per - 1) / per);      // (below 2^28)
 }
 
-// Puts the list where the kernels find it; long ones by launches on the stream.
-bns_status put_list(const bns_gradient* g, int32_t count, void* workspace, hipStream_t st, Listed* l) {
-    l->args = {};
-    l->args.partial = static_cast<double*>(workspace);
-    int32_t entries = 0;
-    for (int32_t i = 0; i < count; ++i) entries += g[i].elements > 0;
-    l->is_long = entries > kShort;
-    char* const room = static_cast<char*>(workspace) + kMostBlocks * sizeof(double);
-    l->long_list.grad = reinterpret_cast<uint64_t*>(room);
-    l->long_list.out = reinterpret_cast<uint64_t*>(room + size_t(entries) * 8);
-    l->long_list.first = reinterpret_cast<uint32_t*>(room + size_t(entries) * 16);
-    uint32_t pieces = 0;        // (below 2^31 and one for every entry)
+// What the launches have in common.
+struct Listed {
+    GradsArgs args;
+    int32_t entries;
+    uint32_t pieces;            // (below 2^31 and one for every entry)
+    LongList long_list;         // for the scaling of a clip, where it reads it
+};
+Listed look_at(const bns_gradient* g, int32_t count, void* workspace) {
+    Listed l{};
     size_t bytes = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (g[i].elements == 0) continue;
+        ++l.entries;
+        l.pieces += pieces_of(g[i]);
+        bytes += size_t(g[i].elements) * dtype_bytes(g[i].dtype);
+    }
+    char* const room = static_cast<char*>(workspace) + kMostBlocks * sizeof(double);
+    if (l.entries > kShort || l.pieces > kFewPieces)
+        l.long_list = {reinterpret_cast<uint64_t*>(room), reinterpret_cast<uint64_t*>(room + size_t(l.entries) * 8), reinterpret_cast<uint32_t*>(room + size_t(l.entries) * 16)};
+    l.args.partial = static_cast<double*>(workspace);
+    l.args.cold = bytes > kStreamBytes ? l.pieces - std::min<uint32_t>(l.pieces, uint32_t(kStreamBytes / kPiece)) : 0;
+    l.args.blocks = int32_t(std::min<uint32_t>(std::max<uint32_t>(l.pieces, 1), kMostBlocks));
+    return l;
+}
+
+// Calls launch(arguments, list, entries before it) for the list in parts of kShort entries (one part at least); BNS_EDEVICE if a launch fails.
+template <typename Launch>
+bns_status in_parts(const Listed& l, const bns_gradient* g, int32_t count, Launch launch) {
+    List list{};
+    GradsArgs a = l.args;
+    uint32_t pieces = 0;
     int32_t at = 0, sent = 0;
     for (int32_t i = 0; i < count; ++i) {
         if (g[i].elements == 0) continue;
         const int64_t per = kPiece / int64_t(dtype_bytes(g[i].dtype));
-        l->list.grad[at] = uint64_t(reinterpret_cast<uintptr_t>(g[i].grad)) | uint64_t((g[i].elements - 1) % per) << kAddressBits | (g[i].dtype == BNS_F32 ? kIsF32 : 0);
-        l->list.out[at] = uint64_t(reinterpret_cast<uintptr_t>(g[i].out));
-        l->list.first[at++] = pieces;
+        list.grad[at] = uint64_t(reinterpret_cast<uintptr_t>(g[i].grad)) | uint64_t((g[i].elements - 1) % per) << kAddressBits | (g[i].dtype == BNS_F32 ? kIsF32 : 0);
+        list.out[at] = uint64_t(reinterpret_cast<uintptr_t>(g[i].out));
+        list.first[at++] = pieces;
         pieces += pieces_of(g[i]);
-        bytes += size_t(g[i].elements) * dtype_bytes(g[i].dtype);
-        if (l->is_long && (at == kShort || sent + at == entries)) {
-            BNS_LAUNCH(grads_list_kernel, dim3(1), dim3(256), 0, st, l->list, l->long_list, sent, at);
-            if (hipGetLastError() != hipSuccess) return BNS_EDEVICE;
-            sent += at;
-            at = 0;
-        }
+        if (at < kShort || sent + at == l.entries) continue;
+        a.entries = at;
+        a.pieces = pieces;
+        launch(a, list, sent);
+        if (hipGetLastError() != hipSuccess) return BNS_EDEVICE;
+        a.from = pieces;
+        sent += at;
+        at = 0;
     }
-    l->args.entries = entries;
-    l->args.pieces = pieces;
-    l->args.cold = bytes > kStreamBytes ? pieces - std::min<uint32_t>(pieces, uint32_t(kStreamBytes / kPiece)) : 0;
-    l->args.blocks = int32_t(std::min<uint32_t>(std::max<uint32_t>(pieces, 1), kMostBlocks));
-    return BNS_OK;
-}
-
-bns_status launch_norm(const Listed& l, hipStream_t st) {
-    const dim3 grid{uint32_t(l.args.blocks)};
-    if (l.is_long) BNS_LAUNCH((grads_norm_kernel<LongList>), grid, dim3(kThreads), 0, st, l.args, l.long_list);
-    else BNS_LAUNCH((grads_norm_kernel<List>), grid, dim3(kThreads), 0, st, l.args, l.list);
+    a.entries = at;
+    a.pieces = pieces;
+    launch(a, list, sent);
     return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
 }
 
-bns_status launch_scale(const Listed& l, hipStream_t st) {
-    const dim3 grid{std::max<uint32_t>(1, (l.args.pieces + kRun - 1) / kRun)};
-    if (l.is_long) BNS_LAUNCH((grads_scale_kernel<LongList>), grid, dim3(kThreads), 0, st, l.args, l.long_list);
-    else BNS_LAUNCH((grads_scale_kernel<List>), grid, dim3(kThreads), 0, st, l.args, l.list);
-    return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
+bns_status launch_norm(const Listed& l, const bns_gradient* g, int32_t count, bool keep, hipStream_t st) {
+    return in_parts(l, g, count, [&](const GradsArgs& a, const List& list, int at) {
+        const uint32_t blocks = at > 0 ? std::min<uint32_t>(a.pieces - a.from, kMostBlocks) : uint32_t(a.blocks);      // (the first part writes all sums)
+        BNS_LAUNCH(grads_norm_kernel, dim3(blocks), dim3(kThreads), 0, st, a, list, keep ? l.long_list : LongList{}, at);
+    });
 }
+
+dim3 scale_grid(const GradsArgs& a) { return dim3(std::max<uint32_t>(1, (a.pieces - a.from + kRun - 1) / kRun)); }
 
 bns_status check_call(const bns_gradient* g, int32_t count, bool scaled, const void* workspace, size_t workspace_bytes) {
     bns_status s = check_gradients(g, count, scaled);
@@ -327,9 +335,8 @@ bns_status bns_grads_norm(const bns_gradient* gradients, int32_t count, double* 
     if (s != BNS_OK) return s;
     if (!squares || !aligned_all(8, squares) || !aligned_all(4, norm)) return BNS_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    Listed l{};
-    if ((s = put_list(gradients, count, workspace, st, &l)) != BNS_OK) return s;
-    if ((s = launch_norm(l, st)) != BNS_OK) return s;
+    Listed l = look_at(gradients, count, workspace);
+    if ((s = launch_norm(l, gradients, count, false, st)) != BNS_OK) return s;
     l.args.squares = squares;
     l.args.norm = norm;
     BNS_LAUNCH(grads_sum_kernel, dim3(1), dim3(kThreads), 0, st, l.args);
@@ -342,13 +349,14 @@ bns_status bns_grads_scale(const bns_gradient* gradients, int32_t count, const d
     if (s != BNS_OK) return s;
     if (!squares || !aligned_all(8, squares) || !aligned_all(4, norm) || !fine_norm(max_norm)) return BNS_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    Listed l{};
-    if ((s = put_list(gradients, count, workspace, st, &l)) != BNS_OK) return s;
+    Listed l = look_at(gradients, count, workspace);
     l.args.partial = nullptr;
     l.args.squares = const_cast<double*>(squares);
-    l.args.norm = norm;
     l.args.max_norm = max_norm;
-    return launch_scale(l, st);
+    return in_parts(l, gradients, count, [&](GradsArgs a, const List& list, int at) {
+        a.norm = at > 0 ? nullptr : norm;
+        BNS_LAUNCH((grads_scale_kernel<List>), scale_grid(a), dim3(kThreads), 0, st, a, list);
+    });
 }
 
 bns_status bns_grads_clip(const bns_gradient* gradients, int32_t count, float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
@@ -356,12 +364,19 @@ bns_status bns_grads_clip(const bns_gradient* gradients, int32_t count, float ma
     if (s != BNS_OK) return s;
     if (!norm || !aligned_all(4, norm) || !fine_norm(max_norm)) return BNS_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    Listed l{};
-    if ((s = put_list(gradients, count, workspace, st, &l)) != BNS_OK) return s;
-    if ((s = launch_norm(l, st)) != BNS_OK) return s;
+    Listed l = look_at(gradients, count, workspace);
+    if ((s = launch_norm(l, gradients, count, true, st)) != BNS_OK) return s;
     l.args.norm = norm;
     l.args.max_norm = max_norm;
-    return launch_scale(l, st);
+    if (!l.long_list.grad) {
+        return in_parts(l, gradients, count, [&](const GradsArgs& a, const List& list, int) {
+            BNS_LAUNCH((grads_scale_kernel<List>), scale_grid(a), dim3(kThreads), 0, st, a, list);
+        });
+    }
+    l.args.entries = l.entries;
+    l.args.pieces = l.pieces;
+    BNS_LAUNCH((grads_scale_kernel<LongList>), scale_grid(l.args), dim3(kThreads), 0, st, l.args, l.long_list);
+    return hipGetLastError() == hipSuccess ? BNS_OK : BNS_EDEVICE;
 }
 
 }  // extern "C"
