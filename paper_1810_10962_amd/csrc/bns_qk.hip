@@ -14,7 +14,8 @@
 // Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.4 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s), 46 without the next turn's elements on their way; backward of 16 384
 // tokens 105 us (503 MB, 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches, of one or two tokens 5 to 6, in one.
 // Heads that are no whole chunks: 9109 x (48 + 6) x 83 bf16 44.5 us (164 MB), by single elements 102; backward of 9537 x (23 + 23) x 46, of which 10 turn, 45.6 (121 MB),
-// by single elements 198; backward of 2905 x (119 + 17) x 16, of which 4 turn, 32.5, by chunks of two elements 77.
+// by single elements 198; backward of 2905 x (119 + 17) x 16, of which 4 turn, 18.1, by chunks of two elements 77,
+// with four lanes at least for a head 32.5.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -138,9 +139,9 @@ __device__ __forceinline__ float dpp_move(float x) {
 }
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
-    static_assert(G >= 4 && G <= 64, "groups of lanes");
-    v += dpp_move<0xb1>(v);                     // quad_perm: lane ^ 1
-    v += dpp_move<0x4e>(v);                     // quad_perm: lane ^ 2
+    static_assert(G >= 1 && G <= 64, "groups of lanes");
+    if (G >= 2) v += dpp_move<0xb1>(v);         // quad_perm: lane ^ 1
+    if (G >= 4) v += dpp_move<0x4e>(v);         // quad_perm: lane ^ 2
     if (G >= 8) v += dpp_move<0x141>(v);        // row_half_mirror: the other four of eight
     if (G >= 16) v += dpp_move<0x140>(v);       // row_mirror: the other eight of sixteen
     if (G >= 32) v += __shfl_xor(v, 16);
@@ -614,7 +615,7 @@ QkPlan qk_plan(const QkDims& d, int32_t dtype, bool interleaved) {
         const int units = interleaved ? (turned + others + 1) / 2 : turned + (others + 1) / 2;
         if (units > kWave * (e == 2 ? 2 : 1)) continue;
         if (e < largest) return {e, e == 4 && units <= 8 ? 8 : units <= (e == 2 ? 32 : 16) ? 16 : 64, inner ? INNER : RAGGED};
-        int g = 4;
+        int g = 1;
         while (g < units) g *= 2;
         return {e, g, inner ? INNER : d.width % e != 0 || d.rotated % (interleaved ? e : 2 * e) != 0 ? RAGGED : WHOLE};
     }
@@ -693,6 +694,8 @@ void fill(QkArgs* a, const bns_qk* qk, const QkDims& d, const QkPlan& plan, int 
         } else if (plan.chunk <= 2) {                                                                                           \
             BNS_QK_SMALL(KERNEL, bf16_t);                                                                                       \
         } else if (f32) {                                                                                                       \
+            BNS_QK_CASE(KERNEL, float, 4, 1);                                                                                   \
+            BNS_QK_CASE(KERNEL, float, 4, 2);                                                                                   \
             BNS_QK_CASE(KERNEL, float, 4, 4);                                                                                   \
             BNS_QK_CASE(KERNEL, float, 4, 8);                                                                                   \
             BNS_QK_CASE(KERNEL, float, 4, 16);                                                                                  \
@@ -705,6 +708,8 @@ void fill(QkArgs* a, const bns_qk* qk, const QkDims& d, const QkPlan& plan, int 
             BNS_QK_IF(KERNEL, bf16_t, 4, 8, 1, true, RAGGED);                                                                   \
             BNS_QK_IF(KERNEL, bf16_t, 4, 8, 1, false, INNER);                                                                   \
         } else {                                                                                                                \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 1);                                                                                  \
+            BNS_QK_CASE(KERNEL, bf16_t, 8, 2);                                                                                  \
             BNS_QK_CASE(KERNEL, bf16_t, 8, 4);                                                                                  \
             BNS_QK_CASE(KERNEL, bf16_t, 8, 8);                                                                                  \
             BNS_QK_CASE(KERNEL, bf16_t, 8, 16);                                                                                 \

@@ -20,7 +20,7 @@ def plan(width, rotated, f32, interleaved):
         if e < largest:
             group = 8 if e == 4 and units <= 8 else 16 if units <= 16 * of_lane else 64
         else:
-            group = max(4, 1 << (units - 1).bit_length())
+            group = 1 << (units - 1).bit_length()
         # every unit has a lane, every angle of a token a place, and chunks that begin further down begin in the head
         assert group <= 64 and units <= group * of_lane and rotated // 2 <= group * of_lane * e
         assert not interleaved or turned * e <= width or rotated >= e

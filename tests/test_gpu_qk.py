@@ -134,6 +134,11 @@ CASES = [  # tokens, q heads, k heads, width, rotated, interleaved, norm, layout
     (20, 5, 3, 509, 6, False, True, "dense", 5000),
     (20, 5, 3, 2, 0, False, True, "dense", 5000),
     (20, 5, 3, 12, 12, True, True, "dense", 5000),
+    (300, 70, 1, 16, 16, False, True, "packed", 5000),
+    (300, 64, 63, 8, 8, True, True, "dense", 5000),
+    (1000, 2, 1, 8, 0, False, True, "head_major", 5000),
+    (500, 33, 8, 32, 16, False, True, "loose", 5000),
+    (200, 130, 5, 15, 14, True, True, "dense", 5000),
 ]
 
 
