@@ -152,6 +152,14 @@ def test_results_that_overlap_are_refused(call, list_):
     assert grads(call, list_) == bns.BNS_EINVAL
 
 
+def test_gradients_at_addresses_that_do_not_fit_a_word_are_refused():
+    for call in ("norm", "scale", "clip"):
+        for at in (2 ** 48, 2 ** 48 - 16, 2 ** 63, 2 ** 64 - 64):
+            assert grads(call, [(at, at, 5, 0, 0)]) == bns.BNS_EUNSUPPORTED
+    for call in ("scale", "clip"):
+        assert grads(call, [(Q, 2 ** 48, 5, 0, 0)]) == bns.BNS_EUNSUPPORTED
+
+
 def test_arguments_of_gradients():
     for call in ("norm", "scale", "clip"):
         assert grads(call, [GOOD], ws=NULL) == grads(call, [GOOD], ws=WS + 8) == grads(call, [GOOD], norm=V + 2) == grads(call, [GOOD], count=-1) == bns.BNS_EINVAL
