@@ -529,7 +529,7 @@ typedef struct {
  * All in fp32 (squares and their mean as bns_rms_forward) and rounded once; w is formed and reduced in fp64, so that far positions (any whole number up to
  * 2^31 in magnitude) turn as exactly as near ones.
  * in: q, k, q_weight[width], k_weight[width] (NULL: no norm), positions[tokens], frequencies[rotated / 2] (fp64, radians per position; both may be
- * NULL where rotated is 0).  out: q_out, k_out.  In place: q_out on q, k_out on k (address and strides). */
+ * NULL where rotated is 0 or there are no tokens).  out: q_out, k_out.  In place: q_out on q, k_out on k (address and strides). */
 bns_status bns_qk_forward(const bns_qk* qk, const void* q, const void* k, const void* q_weight, const void* k_weight, const int64_t* positions,
                           const double* frequencies, void* q_out, void* k_out, void* stream);
 

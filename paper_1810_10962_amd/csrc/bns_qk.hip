@@ -818,7 +818,8 @@ bns_status bns_qk_backward(const bns_qk* qk, const void* q, const void* k, const
         a.part[i].os = d.dx[i];
     }
     const bool f32 = qk->dtype == BNS_F32, nt = size_t(d.tokens) * (size_t(d.heads[0]) + d.heads[1]) * d.width * e * 3 > kStreamBytes;
-    const bool at_once = std::max(a.part[0].units, a.part[1].units) <= kTurnsAtOnce;
+    // (without tokens there is nothing but the sums, of no rows: positions and frequencies may be NULL then and are not read)
+    const bool at_once = d.tokens > 0 && std::max(a.part[0].units, a.part[1].units) <= kTurnsAtOnce;
     if (at_once) {
         for (int i = 0; i < 2; ++i) {
             Heads& p = a.part[i];

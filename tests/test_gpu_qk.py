@@ -226,6 +226,25 @@ def test_one_weight_and_no_tokens():
         assert da[1] is None and (tokens > 0 or not bool(dboth[0].any()))
 
 
+@pytest.mark.parametrize("dtype,width,rotated,interleaved", [("f32", 64, 64, False), ("bf16", 128, 64, True), ("bf16", 83, 40, False), ("f32", 16, 4, False), ("bf16", 1, 0, False)])
+def test_without_tokens_only_the_weights_gradients_are_written(dtype, width, rotated, interleaved):
+    """No tokens: nothing is turned, so that positions and frequencies may be NULL as the tensors may; weights on either side have gradients of zero."""
+    print(f"[gpu-case] qk without tokens {dtype} {width} {rotated}", flush=True)
+    weight = torch.ones(width, device="cuda")
+    for hq, hk in ((4, 2), (4, 0), (0, 0)):
+        spec = bns.make_qk(0, hq, hk, width, dtype, rotated=rotated, interleaved=interleaved, eps=EPS)
+        workspace = torch.full((bns.bns_qk_workspace_bytes(spec),), 255, dtype=torch.uint8, device="cuda")
+        bns.bns_qk_forward(spec, None, None, weight, weight, None, None, None, None)
+        for both in ((weight, weight), (weight, None), (None, weight), (None, None)):
+            made = [None if w is None else written(width) for w in both]
+            dw = [None if m is None else m[1] for m in made]
+            bns.bns_qk_backward(spec, None, None, *both, None, None, None, None, None, None, *dw, workspace)
+            for m in made:
+                if m is not None:
+                    assert not bool(m[1].any())
+                    tail_is_whole(m[0], width)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("width,rotated", [(128, 128), (64, 32), (50, 20), (37, 34), (75, 22)])
 def test_in_place_in_a_projection_s_result(width, rotated, dtype):
