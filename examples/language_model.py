@@ -26,7 +26,7 @@ class AddNorm(torch.autograd.Function):
     def forward(ctx, delta, stream, weight):
         delta, stream, weight = delta.contiguous(), stream.contiguous(), weight.contiguous()      # (the library is handed addresses)
         rows, width = stream.shape
-        rms = bns.make_rms(rows, width, NAMES[stream.dtype], eps=EPS)
+        rms = bns.make_rms(rows, width, NAMES[stream.dtype], weight_dtype=NAMES[weight.dtype], eps=EPS)
         total, y, rstd = torch.empty_like(stream), torch.empty_like(stream), torch.empty(rows, device=stream.device)
         bns.bns_rms_forward(rms, delta, stream, weight, total, y, None, rstd)
         ctx.save_for_backward(total, weight, rstd)
@@ -37,10 +37,10 @@ class AddNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dtotal, dy):
         total, weight, rstd = ctx.saved_tensors
-        dx, dweight = torch.empty_like(total), torch.empty_like(weight)
+        dx, dweight = torch.empty_like(total), torch.empty(weight.shape, device=weight.device)      # (in 32 bits, whatever the weight's type)
         workspace = torch.empty(bns.bns_rms_workspace_bytes(ctx.rms), dtype=torch.uint8, device=total.device)
         bns.bns_rms_backward(ctx.rms, total, weight, rstd, dy.contiguous(), dtotal.contiguous(), dx, dweight, workspace)
-        return dx, dx, dweight          # the sum's gradient is both addends'
+        return dx, dx, dweight.to(weight.dtype)         # the sum's gradient is both addends'
 
 
 class HeadLoss(torch.autograd.Function):
@@ -114,7 +114,7 @@ class Model(torch.nn.Module):
         stream = self.embedding[tokens]
         delta = torch.zeros_like(stream)
         rows, width = stream.shape
-        rms = bns.make_rms(rows, width, NAMES[stream.dtype], out="e4m3", group=32, pow2_scales=True, eps=EPS)
+        rms = bns.make_rms(rows, width, NAMES[stream.dtype], weight_dtype=NAMES[self.norms[0].dtype], out="e4m3", group=32, pow2_scales=True, eps=EPS)
         y = torch.empty(rows, width, dtype=torch.float8_e4m3fn, device="cuda")
         scales = torch.empty(rows, -(-width // 32), device="cuda")
         for i, norm in enumerate(self.norms):

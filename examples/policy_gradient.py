@@ -35,10 +35,12 @@ class QueriesKeys(torch.autograd.Function):
     @staticmethod
     def forward(ctx, packed, q_weight, k_weight, positions, turns, heads, kv_heads):
         packed, q_weight, k_weight = packed.contiguous(), q_weight.contiguous(), k_weight.contiguous()
+        if q_weight.dtype != k_weight.dtype:
+            raise TypeError(f"weights of the queries' norm are {q_weight.dtype}, of the keys' {k_weight.dtype}")
         tokens, row = packed.shape
         width = q_weight.numel()
-        qk = bns.make_qk(tokens, heads, kv_heads, width, NAMES[packed.dtype], rotated=2 * turns.numel(), eps=EPS, q=(row, width), k=(row, width),
-                         dq=(row, width), dk=(row, width))
+        qk = bns.make_qk(tokens, heads, kv_heads, width, NAMES[packed.dtype], rotated=2 * turns.numel(), weight_dtype=NAMES[q_weight.dtype], eps=EPS,
+                         q=(row, width), k=(row, width), dq=(row, width), dk=(row, width))
         q = packed.new_empty(tokens, heads, width)
         k = packed.new_empty(tokens, kv_heads, width)
         bns.bns_qk_forward(qk, packed, packed[:, heads * width:], q_weight, k_weight, positions, turns, q, k)
@@ -53,11 +55,11 @@ class QueriesKeys(torch.autograd.Function):
         at, behind = ctx.qk.q_heads * ctx.qk.width, (ctx.qk.q_heads + ctx.qk.k_heads) * ctx.qk.width
         dpacked = torch.empty_like(packed)
         dpacked[:, behind:] = dv.reshape(dv.shape[0], -1)
-        dq_weight, dk_weight = torch.empty_like(q_weight), torch.empty_like(k_weight)
+        dq_weight, dk_weight = (torch.empty(w.shape, device=w.device) for w in (q_weight, k_weight))       # (in 32 bits, whatever the weights' type)
         workspace = torch.empty(bns.bns_qk_workspace_bytes(ctx.qk), dtype=torch.uint8, device=packed.device)
         bns.bns_qk_backward(ctx.qk, packed, packed[:, at:], q_weight, k_weight, positions, turns, dq.contiguous(), dk.contiguous(), dpacked, dpacked[:, at:],
                             dq_weight, dk_weight, workspace)
-        return dpacked, dq_weight, dk_weight, None, None, None, None
+        return dpacked, dq_weight.to(q_weight.dtype), dk_weight.to(k_weight.dtype), None, None, None, None
 
 
 class LogProb(torch.autograd.Function):
@@ -157,8 +159,8 @@ class Model(torch.nn.Module):
             row, width = packed.shape[1], self.width
             at, behind = self.heads * width, (self.heads + self.kv_heads) * width
             values[:, position] = packed[:, behind:].reshape(answers, self.kv_heads, width)
-            qk = bns.make_qk(answers, self.heads, self.kv_heads, width, NAMES[y.dtype], rotated=2 * self.turns.numel(), eps=EPS, q=(row, width), k=(row, width),
-                             q_out=(row, width), k_out=(keys.stride(0), width))
+            qk = bns.make_qk(answers, self.heads, self.kv_heads, width, NAMES[y.dtype], rotated=2 * self.turns.numel(),
+                             weight_dtype=NAMES[self.q_norms[i].dtype], eps=EPS, q=(row, width), k=(row, width), q_out=(row, width), k_out=(keys.stride(0), width))
             bns.bns_qk_forward(qk, packed, packed[:, at:], self.q_norms[i], self.k_norms[i], positions, self.turns, packed, keys[:, position])
             q = packed[:, :at].reshape(answers, 1, self.heads, width)
             delta = attend(q, keys[:, :position + 1], values[:, :position + 1], position).to(y.dtype) @ self.out[i]

@@ -95,6 +95,34 @@ def test_its_gradients_are_those_of_the_same_model_in_64_bits(example, dtype):
             assert float(((p.grad.double() - b * factor).abs() - (here + 5 * U) * (b * factor).abs()).max()) <= 1e-40
 
 
+def test_a_model_that_was_converted_as_a_whole(example):
+    """model.bfloat16() converts the norms' weights, too: gradients as those of the model in 64 bits (bounds as above), and answers token by token."""
+    print("[gpu-case] policy gradients of a converted model", flush=True)
+    vocab, g = 50, torch.Generator().manual_seed(7)
+    model = example.Model(vocab, 4, 2, 32, 16, 2, torch.float32, seed=5)
+    for norms in (model.norms, model.q_norms, model.k_norms):
+        for w in norms:
+            w.data.copy_(1 + 0.3 * torch.randn(w.shape, generator=g))
+    model.bfloat16()
+    assert all(p.dtype == torch.bfloat16 for p in model.parameters())
+    tokens = torch.randint(0, vocab, (7, 14), generator=g)
+    tokens[:, 4] = (tokens[:, 3] + 1) % vocab
+    lengths = torch.tensor([13, 1, 5, 9, 13, 10, 7])
+    example.loss_of(model, tokens.cuda(), lengths.cuda(), 1.5, vocab)[0].backward()
+    wide = {n: p.detach().double().cpu().requires_grad_() for n, p in model.named_parameters()}
+    wide_loss(example, model, wide, tokens, lengths, 1.5, vocab).backward()
+    for name, p in model.named_parameters():
+        assert p.grad.dtype == torch.bfloat16
+        want = wide[name].grad
+        assert float((p.grad.double().cpu() - want).norm() / want.norm()) < 40 * 2.0 ** -8, name
+    with torch.no_grad():
+        whole = model.logits(tokens[:, :5].cuda()).reshape(7, 5, vocab).double()
+        cache = model.cache(7, 5)
+        for position in range(5):
+            got = model.step(tokens[:, position].cuda(), position, cache).double()
+            assert float((got - whole[:, position]).norm() / whole[:, position].norm()) < 24 * 2.0 ** -8, position
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_token_by_token_is_all_at_once(example, dtype):
     """Logits of single tokens with a cache against those of whole answers: the same operations, products in another order (in bf16 a dozen roundings that may fall
