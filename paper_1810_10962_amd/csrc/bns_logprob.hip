@@ -95,10 +95,10 @@ __device__ __forceinline__ u4 masked(const bf16_t*, u4 w, int n) {
     return w;
 }
 
-// The upper half of a float's bits in the order of the floats.
+// The upper half of a float's bits in the order of the floats, with one zero, as ranks have it.
 constexpr uint32_t kNoKey = 0x007f;     // of -infinity
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.f);
     return (b >> 31 ? ~b : b | 0x80000000u) >> 16;
 }
 

@@ -214,6 +214,23 @@ def test_orders_and_masks(tokens, vocab, dtype):
             assert bool(((out[use].double() - want).abs() <= off).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,vocab", [(1, 5), (3, 1000), (2, 20000), (1, 131072), (300, 20001)])
+def test_zeros_of_both_signs_in_words_of_their_own_tie(tokens, vocab, dtype):
+    """Negative zeros in words that hold nothing as large, and positive ones in others, behind them and before them; the rest is negative.  A wave for a row, four, and several blocks."""
+    print(f"[gpu-case] logprob zeros apart {tokens}x{vocab} {dtype}", flush=True)
+    e = 4 if dtype == "f32" else 8
+    i = torch.arange(vocab)
+    lane, third = i // e % 64, i % e == min(3, vocab - 1)
+    x = -1.0 - i.float() / vocab
+    x = torch.where(third & (lane < 10), 0.0, x)
+    logits = torch.stack([torch.where((x == 0) & ((lane % 9 == 0) == (row % 2 == 0)), -0.0, x) for row in range(tokens)]).to(TYPES[dtype])
+    targets = torch.zeros(tokens, dtype=torch.int64)
+    for top in (1, 2, 5, 20):
+        if top <= vocab:
+            check_forward(run_forward(logits, targets, top, 1.0, dtype), logits, targets, top, 1.0)
+
+
 def test_rows_without_gradient_are_zero_whatever_they_hold():
     vocab, tokens = 3000, 4
     print("[gpu-case] logprob rows without gradient", flush=True)
