@@ -48,7 +48,7 @@ class HeadLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, hidden, weight, targets):
-        hidden, weight, targets = hidden.contiguous(), weight.contiguous(), targets.contiguous()
+        hidden, weight, targets = hidden.contiguous(), weight.contiguous(), targets.long().contiguous()
         head = bns.make_head(hidden.shape[0], hidden.shape[1], weight.shape[0], NAMES[hidden.dtype])
         workspace = torch.empty(bns.bns_head_workspace_bytes(head), dtype=torch.uint8, device=hidden.device)
         loss, lse = torch.empty(hidden.shape[0], device=hidden.device), torch.empty(hidden.shape[0], device=hidden.device)
@@ -74,7 +74,7 @@ class DistillLoss(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, ids, teacher, temperature):
-        logits, ids, teacher = logits.contiguous(), ids.contiguous(), teacher.contiguous()
+        logits, ids, teacher = logits.contiguous(), ids.long().contiguous(), teacher.float().contiguous()
         tokens, vocab = logits.shape
         distill = bns.make_distill(tokens, vocab, ids.shape[1], NAMES[logits.dtype], temperature=temperature)
         loss, lse, dlogits = torch.empty(tokens, device=logits.device), torch.empty(tokens, device=logits.device), torch.empty_like(logits)

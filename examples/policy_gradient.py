@@ -35,6 +35,7 @@ class QueriesKeys(torch.autograd.Function):
     @staticmethod
     def forward(ctx, packed, q_weight, k_weight, positions, turns, heads, kv_heads):
         packed, q_weight, k_weight = packed.contiguous(), q_weight.contiguous(), k_weight.contiguous()
+        positions, turns = positions.long().contiguous(), turns.double().contiguous()
         if q_weight.dtype != k_weight.dtype:
             raise TypeError(f"weights of the queries' norm are {q_weight.dtype}, of the keys' {k_weight.dtype}")
         tokens, row = packed.shape
@@ -67,7 +68,7 @@ class LogProb(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, targets, temperature):
-        logits, targets = logits.contiguous(), targets.contiguous()
+        logits, targets = logits.contiguous(), targets.long().contiguous()
         spec = bns.make_logprob(*logits.shape, NAMES[logits.dtype], temperature=temperature)
         logp, entropy = (torch.empty(len(targets), device=logits.device) for _ in range(2))
         stats = torch.empty(len(targets), 2, device=logits.device)

@@ -38,6 +38,11 @@ def calls(monkeypatch):
     stand_in("rms_backward", ["same", "weight", torch.float32, "same", "same", "same", torch.float32])
     stand_in("qk_forward", ["any", "any", "weight", "weight", torch.int64, torch.float64])
     stand_in("qk_backward", ["any", "any", "weight", "weight", torch.int64, torch.float64, "same", "same", "any", "any", torch.float32, torch.float32])
+    stand_in("logprob_forward", ["same", torch.int64, torch.float32, torch.float32, torch.float32])
+    stand_in("logprob_backward", ["same", torch.int64, torch.float32, torch.float32, torch.float32, torch.float32, "same"])
+    stand_in("head_forward", ["same", "same", torch.int64, torch.float32, torch.float32])
+    stand_in("head_backward", ["same", "same", torch.int64, torch.float32, torch.float32, "same", "same"])
+    stand_in("distill_forward", ["same", torch.int64, torch.float32, torch.float32, torch.float32, torch.float32, "same"])
     return made
 
 
@@ -63,3 +68,18 @@ def test_weights_of_two_types_are_refused(calls):
     with pytest.raises(TypeError):
         example.QueriesKeys.apply(torch.randn(5, 6 * 16), torch.ones(16), torch.ones(16).bfloat16(), torch.arange(5), torch.rand(8, dtype=torch.float64), 4, 1)
     assert calls == []
+
+
+@pytest.mark.parametrize("whole", [torch.int32, torch.int64])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_whole_numbers_of_either_size(calls, dtype, whole):
+    """Targets, ids and positions as a data loader has them, in 32 bits too; a teacher in the student's type."""
+    example, language_model = _load("policy_gradient"), _load("language_model")
+    logits, targets = torch.randn(5, 30, dtype=dtype, requires_grad=True), torch.arange(10, dtype=whole)[::2]
+    logp, entropy = example.LogProb.apply(logits, targets, 1.0)
+    (logp.sum() + entropy.sum()).backward()
+    example.QueriesKeys.apply(torch.randn(5, 6 * 16, dtype=dtype), torch.ones(16), torch.ones(16), torch.arange(10, dtype=whole)[::2], torch.rand(8), 4, 1)
+    hidden, weight = torch.randn(5, 64, dtype=dtype, requires_grad=True), torch.randn(30, 64, dtype=dtype)
+    language_model.HeadLoss.apply(hidden, weight, targets).backward()
+    language_model.DistillLoss.apply(torch.randn(5, 30, dtype=dtype), torch.zeros(5, 3, dtype=whole), torch.randn(5, 3, dtype=dtype), 2.0)
+    assert calls == ["logprob_forward", "logprob_backward", "qk_forward", "head_forward", "head_backward", "distill_forward"]
