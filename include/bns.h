@@ -526,8 +526,8 @@ typedef struct {
  *   v = weight * x / sqrt(mean(x^2) + eps)      (v = x where the weight is NULL)
  *   y_a = v_a cos(w) - v_b sin(w),  y_b = v_a sin(w) + v_b cos(w)      for pair i = (a, b) of the rotated elements, w = positions[t] * frequencies[i]
  *   y = v for the others.
- * All in fp32 (squares and their mean as bns_rms_forward) and rounded once; w is formed and reduced in fp64, so that far positions (any whole number up to
- * 2^31 in magnitude) turn as exactly as near ones.
+ * All in fp32 (squares and their mean as bns_rms_forward) and rounded once; w is formed from more than 64 bits and reduced before it is rounded, so that far positions
+ * (any whole number up to 2^31 in magnitude, frequencies up to 2^16) turn as exactly as near ones.
  * in: q, k, q_weight[width], k_weight[width] (NULL: no norm), positions[tokens], frequencies[rotated / 2] (fp64, radians per position; both may be
  * NULL where rotated is 0 or there are no tokens).  out: q_out, k_out.  In place: q_out on q, k_out on k (address and strides). */
 bns_status bns_qk_forward(const bns_qk* qk, const void* q, const void* k, const void* q_weight, const void* k_weight, const int64_t* positions,

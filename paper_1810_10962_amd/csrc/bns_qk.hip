@@ -8,8 +8,8 @@
 // elements before it works on those of this one.  Queries and keys go to different blocks, the queries' first.
 //
 // Angles: each of the lanes that share a token works out a part of its angles, and all of them get them through LDS.  position * frequency is formed in quarter turns in fp64
-// and reduced exactly (the remainder of a fused multiply-add with the nearest whole number); what is left, at most an eighth of a turn, is exact enough in fp32, and Taylor's
-// series to x^9 and x^10 leave 2e-9 there.
+// and reduced exactly (the remainder of a fused multiply-add with the nearest whole number); what frequency * 2 / pi loses as a number of 53 bits, times 2^31 as much as fp32
+// tells apart, is a second, small factor.  What is left, at most an eighth of a turn, is exact enough in fp32, and Taylor's series to x^9 and x^10 leave 2e-9 there.
 //
 // Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.4 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s), 46 without the next turn's elements on their way; backward of 16 384
 // tokens 105 us (503 MB, 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches, of one or two tokens 5 to 6, in one.
@@ -149,10 +149,10 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
-// cos and sin of `position` times an angle given in quarter turns.
-__device__ __forceinline__ void turn_by(double position, double quarters, float* c, float* s) {
+// cos and sin of `position` times an angle of `quarters` + `less` quarter turns.
+__device__ __forceinline__ void turn_by(double position, double quarters, float less, float* c, float* s) {
     const double n = rint(position * quarters);
-    const float x = float(fma(position, quarters, -n)) * 1.57079632679489662f;      // |x| <= pi / 4
+    const float x = float(fma(position, double(less), fma(position, quarters, -n))) * 1.57079632679489662f;      // |x| <= pi / 4
     const int quadrant = int(fma(-4.0, rint(n * 0.25), n));                        // -2 .. 2
     const float x2 = x * x;
     const float sine = x * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.f / 362880, -1.f / 5040), 1.f / 120), -1.f / 6), 1.f);
@@ -317,6 +317,7 @@ struct Angles {
     alignas(16) float cosine[kWaves][kWave * E * UPL], sine[kWaves][kWave * E * UPL];
     alignas(16) float weight[kMostWidth + 8];
     double quarters[kMostWidth / 2];
+    float less[kMostWidth / 2];         // what is left of them
 };
 
 // The walk of a wave over its turns: runs of neighbouring ones, so that all waves work in one stretch of memory.
@@ -346,7 +347,12 @@ struct Walk {
         left = p.run;
         group = group_of(unit);
         turn = int(unit - group * p.turns.d);
-        for (int i = threadIdx.x; i < a.rotated / 2; i += kThreads) angles.quarters[i] = a.frequencies[i] * 0.63661977236758134308;        // 2 / pi
+        for (int i = threadIdx.x; i < a.rotated / 2; i += kThreads) {
+            constexpr double kUpper = 0.63661977236758138, kLower = -3.9357353350364971e-17;        // 2 / pi
+            const double f = a.frequencies[i], quarters = f * kUpper;
+            angles.quarters[i] = quarters;
+            angles.less[i] = float(fma(f, kLower, fma(f, kUpper, -quarters)));
+        }
         if (p.weight) {
             for (int i = threadIdx.x; i < a.width; i += kThreads)
                 angles.weight[i] = a.weight_bf16 ? load_scalar<bf16_t>(static_cast<const bf16_t*>(p.weight) + i) : static_cast<const float*>(p.weight)[i];
@@ -389,7 +395,7 @@ struct Walk {
         float *c = angles.cosine[wave], *s = angles.sine[wave];
         const double here = double(position);
         asm volatile("" ::: "memory");      // (a wave's accesses to LDS are in order)
-        for (int i = lane % sharing; i < each; i += sharing) turn_by(here, angles.quarters[i], c + base + i, s + base + i);
+        for (int i = lane % sharing; i < each; i += sharing) turn_by(here, angles.quarters[i], angles.less[i], c + base + i, s + base + i);
         asm volatile("" ::: "memory");
         ask_position(left > int(p.turns.d) - turn ? group + 1 : group_of(unit + left + skip));
     }

@@ -5,6 +5,9 @@ Tolerances, with u = 2^-24.  A head's sum of squares has 16 terms a lane in turn
 0.79), as are its factor and their product (0.79 * 3 u), and the series have 2 u each of rounding and 0.03 u of truncation: C = 5 u absolute for cos and sin, besides
 four roundings of the product in fp64, here and in the reference, 2^-51 of the angle.  A rotated element is then off by (|v_a| + |v_b|) (V + C + 3 u), and by
 half a unit of its type.  Backward: g the same without V (G = C + 3 u); x^ 16 u; the mean of weight g x^ its terms' errors and 28 u of their magnitudes."""
+import math
+from fractions import Fraction
+
 import pytest
 import torch
 
@@ -321,6 +324,28 @@ def test_far_positions_turn_exactly():
         part = slice(t, t + 1)
         assert_forward(out[part], x[part], None, positions[part], f, width, False, "f32")
     assert torch.equal(out[-1].cpu(), x[-1])
+
+
+def test_far_positions_turn_as_exactly_as_near_ones():
+    """cos and sin alone, (1, 0) turned, against angles that are reduced as fractions with 70 digits of pi: C = 5 u of the docstring, without a part that grows with the position."""
+    print("[gpu-case] qk angles of far positions", flush=True)
+    pi = Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899")
+    positions = [2 ** 31, -2 ** 31, 2 ** 31 - 1, 2 ** 30 + 1, 10 ** 9 + 7, 2 ** 24 + 1, 12345, 1, -1, 0]
+    g = torch.Generator().manual_seed(11)
+    f = torch.cat([0.5 + 2.5 * torch.rand(128, generator=g, dtype=torch.float64), 10000.0 ** (-torch.arange(120, dtype=torch.float64) / 120),
+                   2.0 ** 16 * torch.rand(8, generator=g, dtype=torch.float64)])
+    want = torch.empty(len(positions), 2, len(f), dtype=torch.float64)
+    for t, position in enumerate(positions):
+        for i, frequency in enumerate(f.tolist()):
+            angle = position * Fraction(frequency)
+            left = float(angle - round(angle / (2 * pi)) * 2 * pi)
+            want[t, 0, i], want[t, 1, i] = math.cos(left), math.sin(left)
+    x = torch.zeros(len(positions), 1, 512)
+    x[:, :, :256] = 1
+    out = torch.empty_like(x, device="cuda")
+    bns.bns_qk_forward(bns.make_qk(len(positions), 1, 0, 512, "f32"), x.cuda(), None, None, None, torch.tensor(positions).cuda(), f.cuda(), out, None)
+    worst = (out.double().cpu().reshape(want.shape) - want).abs().amax((1, 2)) / U
+    assert bool((worst <= 5).all()), worst
 
 
 def test_gradients_against_differences():
