@@ -166,6 +166,34 @@ def test_a_captured_clip_is_replayed():
         check(outs, grads, min(1.0, 1.0 / (norm + 1e-6)))
 
 
+@pytest.mark.parametrize("count", [200, 201, 450])
+def test_a_captured_clip_of_several_parts_is_replayed(count):
+    """Lists that travel with one launch, two and three: later launches of the norm add to the sums of the first, and leave the list in the workspace for the scaling.
+    Captured, and replayed on new gradients with the workspace overwritten and eager calls with another one in between."""
+    print(f"[gpu-case] clip captured {count}", flush=True)
+    grads, outs, _ = make([(i * 53) % 901 + 1 + (i == 3) * 3_000_000 for i in range(count)], (torch.float32, torch.bfloat16), seed=5)
+    gradients, one, other = bns.make_gradients(grads, outs), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    copies = [torch.empty_like(x) for x in grads]
+    eager = bns.make_gradients(grads, copies)
+    space, second = (torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda") for _ in range(2))
+    bns.bns_grads_clip(gradients, 1.0, one, space)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bns.bns_grads_clip(gradients, 1.0, one, space)
+    for turn in range(4):
+        for x in grads:
+            x.mul_(1.5 if turn % 2 else 0.5)
+        space.fill_(255)
+        bns.bns_grads_clip(eager, 1.0, other, second)
+        graph.replay()
+        torch.cuda.synchronize()
+        norm = whole_norm(grads)
+        assert abs(float(one[0]) - norm) <= 2 * U * norm
+        check(outs, grads, min(1.0, 1.0 / (norm + 1e-6)))
+        assert torch.equal(one, other) and all(torch.equal(a, b) for a, b in zip(outs, copies))
+
+
 def test_gradients_of_several_devices_are_refused():
     """Before anything is enqueued: host memory in a list of the device's, or with a workspace of the device's."""
     print("[gpu-case] gradients of several devices", flush=True)
