@@ -47,6 +47,28 @@ def test_many_tokens_of_queries():
         assert torch.equal(q[at:at + chunk], want), at
 
 
+def test_the_weight_s_gradient_of_many_tokens():
+    """2^31 elements and some, the gradient along the result itself, so that no term has another's sign and a part that is missing shows: g = weight x^ and its rounding.
+    Terms: x^ 16 u, g (|g_a| + |g_b|) (5 + 3 u and an angle's 2^-51 of 10^6, the reference's); their sum 1025 in turn in a lane, then 32, 16 and 32 in turn."""
+    tokens, heads, width = (1 << 31) // (16 * 128) + 1000, 16, 128
+    print(f"[gpu-case] qk weight's gradient of {tokens} tokens", flush=True)
+    x = fill(torch.empty(tokens, heads, width, dtype=torch.bfloat16, device="cuda"), 4)
+    weight, turns = 1 + 0.1 * torch.randn(width, device="cuda"), 10000.0 ** (-torch.arange(64, dtype=torch.float64, device="cuda") / 64)
+    positions, spec = torch.arange(tokens, device="cuda"), bns.make_qk(tokens, heads, 0, width, rotated=width)
+    dy, dw = torch.empty_like(x), torch.empty(width, device="cuda")
+    bns.bns_qk_forward(spec, x, None, weight, None, positions, turns, dy, None)
+    want, off = (torch.zeros(width, dtype=torch.float64, device="cuda") for _ in range(2))
+    for at in range(0, tokens, 1 << 15):
+        part = slice(at, at + (1 << 15))
+        _, dw_part, g, r = ref.qk_backward(x[part].double(), weight.double(), positions[part], turns, dy[part].double(), width, False, 1e-6)
+        want += dw_part
+        xh = (x[part].double() * r).abs()
+        off += (xh * ref.beside(g, width, False)).sum((0, 1)) * (8 * U + 2.0 ** -51 * 1e6) + (xh * g.abs()).sum((0, 1)) * (17 + 1025 + 80) * U
+    bns.bns_qk_backward(spec, x, None, weight, None, positions, turns, dy, None, dy, None, dw, None,
+                        torch.empty(bns.bns_qk_workspace_bytes(spec), dtype=torch.uint8, device="cuda"))
+    assert float(((dw.double() - want).abs() - off).max()) <= 0 and float((off / want).max()) < 1 / 2048       # (a block's part is 1 / 512)
+
+
 @pytest.mark.parametrize("kind", ["token", "head"])
 def test_far_apart(kind):
     """Strides that pass 2^31 elements between neighbours, with bytes beyond 2^33 (a long head-major cache)."""
