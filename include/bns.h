@@ -591,7 +591,8 @@ typedef struct {
  * elements each and 2^43 together, at addresses below 2^48) that is read before the call returns; a captured call keeps what it said.
  *   squares = sum over all elements of grad^2 (fp64: no gradient of finite elements overflows)      norm = sqrt(squares)
  *   c = min(1, max_norm / (norm + 1e-6))      out = grad * c, rounded to dtype
- * Where the norm is NaN so are c and what is scaled; where it is infinite, c = 0 (infinite elements become NaN).  Gradients in place with c = 1 are left as they are.
+ * c comes from the norm in fp64, which only an infinite element makes infinite; what is reported in fp32 is infinite from 3.4e38 on, too.  Where the norm is NaN so are c
+ * and what is scaled; where an element is infinite, c = 0 (infinite elements become NaN).  Gradients in place with c = 1 are left as they are.
  * bns_grads_clip does it all.  bns_grads_norm and bns_grads_scale are its two halves, for a caller whose gradients lie on several devices: squares are added up between.
  * An `out` may be its own grad, and overlaps no other grad or out; a grad may occur more than once, and counts as often.
  * max_norm: >= 0, finite.  squares[1], norm[1]: device; norm may be NULL in bns_grads_norm and bns_grads_scale. */
