@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, UPL == 1 ? 4 : 1) qk_backward_kernel
         mine.template store<NT>(a, out, out_to, g);
     }
     if (!p.weight) return;
-    // The block's sums: the lanes that hold the same elements, in their order.
+    // The block's sums: the lanes that hold the same elements, in their order; in fp64 and rounded once, as those of the blocks are.  (A lane's own, of some tens of terms, are fp32.)
     constexpr int kSlots = kThreads / G;
     __syncthreads();        // (the angles are no longer needed)
 #pragma unroll
@@ -567,8 +567,8 @@ __global__ void __launch_bounds__(kThreads, UPL == 1 ? 4 : 1) qk_backward_kernel
     // (element r of lane l: written by that lane's place among the first G threads, which knows where it goes)
     for (int r = threadIdx.x / G; r < UPL * 2 * E; r += kSlots) {
         const int l = threadIdx.x % G;
-        float s = 0.f;
-        for (int j = 0; j < kSlots; ++j) s += lds.sums[r][j * G + l];
+        double s = 0.0;
+        for (int j = 0; j < kSlots; ++j) s += double(lds.sums[r][j * G + l]);
         const int k = r / (2 * E), c = r / E % 2, i = r % E;
         int place = -1, own = 0;
 #pragma unroll
@@ -576,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, UPL == 1 ? 4 : 1) qk_backward_kernel
 #pragma unroll
             for (int cc = 0; cc < 2; ++cc)
                 if (kk == k && cc == c) place = mine.at[kk][cc], own = mine.own[kk][cc];
-        if (place >= 0 && i >= own) partial[place + i] = s;
+        if (place >= 0 && i >= own) partial[place + i] = float(s);
     }
 }
 
@@ -588,21 +588,21 @@ struct SumArgs {
     int32_t count[2], width;
 };
 __global__ void __launch_bounds__(kSumColumns * kSumLanes) qk_weight_sum_kernel(SumArgs a) {
-    __shared__ float lds[kSumLanes][kSumColumns];
+    __shared__ double lds[kSumLanes][kSumColumns];
     const int which = blockIdx.y;
     if (!a.out[which]) return;
     const float* partial = a.partial[which];
     const int c = threadIdx.x % kSumColumns, l = threadIdx.x / kSumColumns, col = blockIdx.x * kSumColumns + c;
-    float s = 0.f;
+    double s = 0.0;
     if (col < a.width) {
 #pragma unroll 16
-        for (int i = l; i < a.count[which]; i += kSumLanes) s += partial[int64_t(i) * a.width + col];
+        for (int i = l; i < a.count[which]; i += kSumLanes) s += double(partial[int64_t(i) * a.width + col]);
     }
     lds[l][c] = s;
     __syncthreads();
     if (l == 0 && col < a.width) {
         for (int i = 1; i < kSumLanes; ++i) s += lds[i][c];
-        a.out[which][col] = s;
+        a.out[which][col] = float(s);
     }
 }
 

@@ -249,6 +249,33 @@ def test_without_tokens_only_the_weights_gradients_are_written(dtype, width, rot
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens", [8, 1000])
+def test_sums_of_the_weights_gradients_lose_nothing_small(tokens, dtype):
+    """Terms that are whole numbers (x of one everywhere has r = 1): 2^25 and -2^25 in different lanes of one block, or in different blocks, and ones between them, which fp32
+    drops beside those.  A lane has one term of a large magnitude and else zeros, so that its sum is exact, and so is a block's in fp64.  Blocks' sums are rounded to fp32, where numbers
+    from 2^25 on are 4 apart: the two that have a large term and ones (blocks of bf16 have eight tokens, of fp32 four) may each be off by 2."""
+    print(f"[gpu-case] qk sums of large and small terms {tokens} {dtype}", flush=True)
+    heads, width = 8, 64
+    dy = torch.zeros(tokens, heads, width)
+    if tokens == 8:         # (one block)
+        dy[:, 1:7] = 1
+        dy[0, 0], dy[0, 7] = 2.0 ** 25, -2.0 ** 25
+    else:
+        dy[5::4, 3] = 1
+        dy[0, 0], dy[tokens - 1, 7] = 2.0 ** 25, -2.0 ** 25
+        dy[tokens - 3, 3] = 0
+    want = dy.double().sum((0, 1))
+    x = torch.ones(tokens, heads, width, dtype=TYPES[dtype], device="cuda")
+    dw = [torch.empty(width, device="cuda") for _ in "qk"]
+    spec = bns.make_qk(tokens, heads, heads, width, dtype, rotated=0, eps=0.0)
+    ones, dy = torch.ones(width, device="cuda"), dy.to(TYPES[dtype]).cuda()
+    bns.bns_qk_backward(spec, x, x, ones, ones, None, None, dy, dy, torch.empty_like(x), torch.empty_like(x), *dw,
+                        torch.empty(bns.bns_qk_workspace_bytes(spec), dtype=torch.uint8, device="cuda"))
+    for got in dw:
+        assert float((got.double().cpu() - want).abs().max()) <= (0 if tokens == 8 else 2 * 2), (float(got[0]), float(want[0]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("width,rotated", [(128, 128), (64, 32), (50, 20), (37, 34), (75, 22)])
 def test_in_place_in_a_projection_s_result(width, rotated, dtype):
     """Queries and keys beside their values, replaced where they are; the values stay.  Then the same backward, gradients in place."""
