@@ -495,9 +495,16 @@ def make_logprob(tokens, vocab, dtype="bf16", *, top=0, temperature=1.0, logits_
     return bns_logprob(tokens, logits_stride, dlogits_stride, vocab, top, _dtype(dtype), temperature)
 
 
+def _channels_last(t):
+    """Whether a tensor's elements are neighbours with the channels last."""
+    import torch
+    last = {4: torch.channels_last, 5: torch.channels_last_3d}.get(t.dim())
+    return last is not None and t.is_contiguous(memory_format=last)
+
+
 class Gradients:
-    """Gradients as bns_grads_* take them, with where they go (``outs``; None: nowhere, for bns_grads_norm).  Holds the tensors, whose addresses it has: a program
-    that gets new tensors makes a new one."""
+    """Gradients as bns_grads_* take them, with where they go (``outs``; None: nowhere, for bns_grads_norm): contiguous, or with the channels last, results in the same
+    order.  Holds the tensors, whose addresses it has: a program that gets new tensors makes a new one."""
 
     def __init__(self, grads, outs=None):
         import torch
@@ -509,13 +516,16 @@ class Gradients:
         self.array = (bns_gradient * max(1, self.count))()
         for i, g in enumerate(self.grads):
             out = None if outs is None else self.outs[i]
-            for t in (g,) if out is None else (g, out):
-                if t.dtype not in types or not t.is_contiguous():
-                    raise ValueError(f"gradient {i}: float32 or bfloat16 and contiguous is wanted")
+            for t in (g,) if out is None or out is g else (g, out):
+                if t.dtype not in types or not (t.is_contiguous() or _channels_last(t)):
+                    raise ValueError(f"gradient {i}: float32 or bfloat16 and contiguous, or with the channels last, is wanted")
                 if t.get_device() != self.device:
                     raise ValueError(f"gradient {i}: it lies on another device than the first one (bns_grads_norm and bns_grads_scale take each device's)")
-            if out is not None and (out.dtype != g.dtype or out.numel() != g.numel()):
-                raise ValueError(f"gradient {i}: its result has another type or size")
+            if out is not None and out is not g:
+                if out.dtype != g.dtype or out.numel() != g.numel():
+                    raise ValueError(f"gradient {i}: its result has another type or size")
+                if not (g.is_contiguous() and out.is_contiguous()) and not (g.shape == out.shape and _channels_last(g) and _channels_last(out)):
+                    raise ValueError(f"gradient {i}: its result has another memory order")
             self.array[i] = bns_gradient(g.data_ptr(), None if out is None else out.data_ptr(), g.numel(), types[g.dtype], 0)
 
     def data_ptr(self):

@@ -194,3 +194,18 @@ def test_the_binding_checks_gradients():
     for grads_, outs in (([a.double()], None), ([a.t()], None), ([a], [a.bfloat16()]), ([a], [torch.zeros(5)]), ([a], []), ([a], [torch.zeros(6, 4).t()])):
         with pytest.raises(ValueError):
             bns.make_gradients(grads_, outs)
+
+
+def test_gradients_with_the_channels_last():
+    """Weights of convolutions in the order of N x H x W x C tensors: dense, so that their elements are taken as they lie, where the results have the same order."""
+    a = torch.zeros(4, 6, 3, 3).to(memory_format=torch.channels_last)
+    b, solid = torch.zeros(2, 4, 3, 3, 3).to(memory_format=torch.channels_last_3d), torch.zeros(4, 6, 3, 3)
+    assert bns.make_gradients([a, b, solid]).count == 3
+    got = bns.make_gradients([a, b], [torch.empty_like(a), b])
+    assert got.array[0].elements == a.numel() and got.array[0].grad == a.data_ptr() and got.array[1].out == b.data_ptr()
+    point = torch.zeros(4, 6, 1, 1).to(memory_format=torch.channels_last)          # (in either order)
+    assert bns.make_gradients([point], [torch.zeros(24)]).count == 1
+    for grads_, outs in (([a], [solid]), ([solid], [a]), ([a], [torch.zeros(a.numel())]), ([a], [torch.zeros(4, 3, 6, 3).to(memory_format=torch.channels_last)]),
+                         ([a[:, :, :2]], None), ([a[:, ::2]], None), ([a.expand(2, 4, 6, 3, 3)], None), ([solid.permute(1, 0, 2, 3)], None)):
+        with pytest.raises(ValueError):
+            bns.make_gradients(grads_, outs)

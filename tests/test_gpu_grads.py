@@ -99,6 +99,22 @@ def test_in_place(types):
     assert all(bool((x == 0).all()) for x in grads) and not all(bool((x == 0).all()) for x in before)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_channels_last(dtype):
+    """A convolution's weights in the order of its N x H x W x C activations, in place and to tensors of the same order, beside a contiguous one."""
+    print(f"[gpu-case] clip channels last {dtype}", flush=True)
+    g = torch.Generator().manual_seed(3)
+    grads = [torch.randn(33, 17, 3, 3, generator=g).to(dtype).cuda().contiguous(memory_format=torch.channels_last), torch.randn(19, 5, generator=g).to(dtype).cuda(),
+             torch.randn(4, 3, 2, 3, 3, generator=g).to(dtype).cuda().contiguous(memory_format=torch.channels_last_3d)]
+    kept, norm, one = [x.clone() for x in grads], whole_norm(grads), torch.empty(1, device="cuda")
+    for outs in ([torch.empty_like(x) for x in grads], grads):
+        gradients = bns.make_gradients(grads, outs)
+        space = torch.empty(bns.bns_grads_workspace_bytes(gradients), dtype=torch.uint8, device="cuda")
+        bns.bns_grads_clip(gradients, norm / 3, one, space)
+        assert abs(float(one[0]) - norm) <= 2 * U * norm
+        check(outs, kept, norm / 3 / (norm + 1e-6))
+
+
 def test_a_gradient_that_comes_twice_counts_twice():
     print("[gpu-case] clip the same gradient twice", flush=True)
     x = torch.full((100,), 3.0, device="cuda")
