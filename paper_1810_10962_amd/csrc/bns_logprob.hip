@@ -95,10 +95,10 @@ __device__ __forceinline__ u4 masked(const bf16_t*, u4 w, int n) {
     return w;
 }
 
-// The upper half of a float's bits in the order of the floats, with one zero, as ranks have it.
+// The upper half of a float's bits in the order of the floats; that of +0 is one above that of -0.
 constexpr uint32_t kNoKey = 0x007f;     // of -infinity
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x + 0.f);
+    const uint32_t b = __float_as_uint(x);
     return (b >> 31 ? ~b : b | 0x80000000u) >> 16;
 }
 
@@ -173,7 +173,7 @@ struct Top {
     __device__ __forceinline__ int find_chunks(int w, int slots, float at_least) {
         const uint16_t* keys = reinterpret_cast<const uint16_t*>(list + w * kRegion);
         const int lane = threadIdx.x % kWave;
-        const uint32_t least_key = key_of(at_least);
+        const uint32_t least_key = key_of(at_least) - (at_least == 0.f);        // (-0 reaches +0, as ranks have one zero)
         int n = 0;
         asm volatile("" ::: "memory");      // (a wave's accesses to LDS are in order; nothing is exchanged with other waves)
         for (int i = 0; i < slots; ++i) {
