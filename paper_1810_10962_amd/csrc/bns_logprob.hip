@@ -9,12 +9,13 @@
 // Alternatives: what a thread has as its largest logit bounds the k-th largest of the row from below, if enough threads have such a one: the j-th largest of
 // each wave's 64, j = ceil(k / waves), the least of all waves' taken.  On the way each thread leaves the largest logit of every chunk of its words in LDS (its upper 16
 // bits), nothing else.  Afterwards the chunks that reach the bound, some two for each alternative, are read again (from the L2), and their elements that do go to the wave's
-// list, where the place of one is the number of larger ones.  Rows that put more on the lists than they hold (many equal logits) are searched by halving the range of values.
+// list, where the place of one is the number of larger ones.  Rows that put more on the lists than they hold (many equal logits) are searched by halving the range of values,
+// some 25 passes over the row by single elements: one row of 131072 equal bf16 logits 340 us, 4096 of them 23 ms.
 //
 // Few rows are cut into segments, one block each, and joined by a second launch.
 //
-// Measured: 4096 rows of 131072 bf16 forward 172 us (1.07 GB, 6.2 TB/s), backward 404 us (2.1 GB, 5.3 TB/s); 333 x 50257 fp32 with 5 alternatives 16.8 us (67 MB, from the
-// memory-side cache); one row of 131072 bf16 with 20 alternatives 12.4 us, of which some 4 are the join's launch.  With alternatives kept in a sorted list by
+// Measured: 4096 rows of 131072 bf16 forward 172 to 177 us (1.07 GB, 6.1 TB/s), backward 404 us (2.1 GB, 5.3 TB/s); 333 x 50257 fp32 with 5 alternatives 16.8 us (67 MB, from the
+// memory-side cache); one row of 131072 bf16 with 20 alternatives 12.2 to 12.6 us, of which some 4 are the join's launch.  With alternatives kept in a sorted list by
 // every thread on the way the same row took 22.7 us, and 4000 x 1500 with 5 alternatives 705 us instead of 10.3.
 #include <hip/hip_runtime.h>
 

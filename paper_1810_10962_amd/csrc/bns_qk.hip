@@ -11,10 +11,10 @@
 // and reduced exactly (the remainder of a fused multiply-add with the nearest whole number); what frequency * 2 / pi loses as a number of 53 bits, times 2^31 as much as fp32
 // tells apart, is a second, small factor.  What is left, at most an eighth of a turn, is exact enough in fp32, and Taylor's series to x^9 and x^10 leave 2e-9 there.
 //
-// Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.4 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s), 46 without the next turn's elements on their way; backward of 16 384
-// tokens 105 us (503 MB, 4.8 TB/s); a single token 4.4 us, what one launch takes; a small backward 8.3 us, two launches, of one or two tokens 5 to 6, in one.
-// Heads that are no whole chunks: 9109 x (48 + 6) x 83 bf16 44.5 us (164 MB), by single elements 102; backward of 9537 x (23 + 23) x 46, of which 10 turn, 45.6 (121 MB),
-// by single elements 198; backward of 2905 x (119 + 17) x 16, of which 4 turn, 18.1, by chunks of two elements 77,
+// Measured: 8192 tokens of (32 + 8) heads of 128, bf16, 37.5 us (168 MB, 4.5 TB/s; a large copy moves 5.1 TB/s), 46 without the next turn's elements on their way; backward of 16 384
+// tokens 105 us (503 MB, 4.8 TB/s); a single token 4.4 to 5 us, what one launch takes; a small backward 8.1 us, two launches, of one or two tokens 5 to 6, in one.
+// Heads that are no whole chunks: 9109 x (48 + 6) x 83 bf16 44.5 us (164 MB), by single elements 102; backward of 9537 x (23 + 23) x 46, of which 10 turn, 44.9 (121 MB),
+// by single elements 198; backward of 2905 x (119 + 17) x 16, of which 4 turn, 16.6, by chunks of two elements 77,
 // with four lanes at least for a head 32.5.
 #include <hip/hip_runtime.h>
 
