@@ -25,6 +25,8 @@ class AddNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, delta, stream, weight):
         delta, stream, weight = delta.contiguous(), stream.contiguous(), weight.contiguous()      # (the library is handed addresses)
+        if delta.dtype != stream.dtype:
+            raise TypeError(f"the addends of a residual are {delta.dtype} and {stream.dtype}")
         rows, width = stream.shape
         rms = bns.make_rms(rows, width, NAMES[stream.dtype], weight_dtype=NAMES[weight.dtype], eps=EPS)
         total, y, rstd = torch.empty_like(stream), torch.empty_like(stream), torch.empty(rows, device=stream.device)
@@ -49,6 +51,8 @@ class HeadLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, targets):
         hidden, weight, targets = hidden.contiguous(), weight.contiguous(), targets.long().contiguous()
+        if hidden.dtype != weight.dtype:
+            raise TypeError(f"hidden states are {hidden.dtype}, the vocabulary's weight {weight.dtype}")
         head = bns.make_head(hidden.shape[0], hidden.shape[1], weight.shape[0], NAMES[hidden.dtype])
         workspace = torch.empty(bns.bns_head_workspace_bytes(head), dtype=torch.uint8, device=hidden.device)
         loss, lse = torch.empty(hidden.shape[0], device=hidden.device), torch.empty(hidden.shape[0], device=hidden.device)

@@ -70,6 +70,16 @@ def test_weights_of_two_types_are_refused(calls):
     assert calls == []
 
 
+def test_operands_of_two_types_are_refused(calls):
+    """As a product under autocast leaves them beside a residual stream in 32 bits: the library has one type for both."""
+    example = _load("language_model")
+    with pytest.raises(TypeError):
+        example.AddNorm.apply(torch.randn(5, 64).bfloat16(), torch.randn(5, 64), torch.ones(64))
+    with pytest.raises(TypeError):
+        example.HeadLoss.apply(torch.randn(5, 64).bfloat16(), torch.randn(30, 64), torch.arange(5))
+    assert calls == []
+
+
 @pytest.mark.parametrize("whole", [torch.int32, torch.int64])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_whole_numbers_of_either_size(calls, dtype, whole):
