@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, UPL == 1 ? 4 : 1) qk_backward_kernel
         mine.template store<NT>(a, out, out_to, g);
     }
     if (!p.weight) return;
-    // The block's sums: the lanes that hold the same elements, in their order; in fp64 and rounded once, as those of the blocks are.  (A lane's own, of some tens of terms, are fp32.)
+    // The block's sums: the lanes that hold the same elements, in their order; in fp64 and rounded once, as those of the blocks are.  (A lane's own terms, one for each of its turns, are added in fp32.)
     constexpr int kSlots = kThreads / G;
     __syncthreads();        // (the angles are no longer needed)
 #pragma unroll
